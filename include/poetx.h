@@ -367,6 +367,74 @@ int poetx_linear_bwd(const poetx_linear_desc* desc, const void* X, const void* d
                      void* dX, float* dtheta_R, float* dtheta_P, int32_t accumulate,
                      void* ws, size_t ws_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Base weights in four bits.  The step after the INT8 weight of Sec. 3.6: 32 neighbouring elements of a row
+ * share one power of two, each keeps a sign, two exponent bits and one mantissa bit (the microscaled e2m1 format
+ * that gfx950's matrix instructions multiply):
+ *   value[i][k] = e2m1(code[i][k]) * 2^(scale[i][k/32] - 127),  e2m1 = 0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives
+ *                                                               (bit 3 of the code is the sign)
+ *   scale = clamp(floor(log2(max |x|)) - 2 + 127, 0, 254); 0 for 32 zeros; 255 where one of them is infinite or NaN:
+ *           all 32 then stand for NaN
+ *   code  = x 2^(127 - scale) rounded to the nearest e2m1, ties to the even code, beyond 6 to 6; the sign is kept.
+ * The elements of a last, shorter block are scaled among themselves.  A buffer (poetx_mx4_bytes bytes, 16-byte aligned):
+ * rows of cols rounded up to 128 codes, element 2i in the low half of byte i; from the next multiple of 256 bytes on
+ * the scale bytes, a row of (cols rounded up to 128) / 32 per row.  Codes and scales past cols are zeros, and have to
+ * be in a buffer that a caller builds itself.
+ * X / out: rows x cols, leading dimension ld >= cols, any alignment of the element type.  out: the values, exact in
+ * either type (bf16 and fp32 hold them all but for those beyond their largest, which become infinities; only scales
+ * above 252, which quantising never gives, have such).  out must not overlap Q. */
+size_t poetx_mx4_bytes(int64_t rows, int32_t cols);
+int poetx_mx4_quantize(const void* X, int32_t dtype, int64_t rows, int32_t cols, int64_t ld, void* Q, void* stream);
+int poetx_mx4_dequantize(const void* Q, int64_t rows, int32_t cols, int32_t dtype, void* out, int64_t ld, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Products of rows with the weight of their group (a layer of experts; one group is a plain linear):
+ *   forward          Z_r  = W_g X_r                for the rows r = offsets[g] .. offsets[g+1] - 1 of every group g
+ *   input gradient   dX_r = W_g^T dZ_r
+ *   weight gradient  dW_g = sum over its rows of dZ_r X_r^T        (weights that are not frozen)
+ * Rows are tokens: X and dX are rows x d_in, Z and dZ rows x d_out, row major with leading dimensions of their own (the
+ * TOKEN_MAJOR orientation, as groups are ranges of rows).  W: groups x d_out x d_in in `dtype`, or with
+ * POETX_GROUPED_W_MX4 one 4-bit buffer of groups * d_out rows of d_in; bf16 only.  offsets: groups + 1 int32 on the
+ * device, non-decreasing, 0 <= offsets <= rows.  They are read on the device alone, so a router's answer needs no
+ * copy to the host.  Groups may be empty.  Rows that no group has are neither read nor written; offsets outside
+ * 0 .. rows are taken as the nearer end and a decreasing pair as an empty group, so that nothing outside the tensors is
+ * ever touched.  Products of bf16 are exact and summed in fp32, and a result is rounded once.
+ * Every sum has one order, so results are reproducible run to run. */
+typedef struct {
+  int32_t d_in;        /* m */
+  int32_t d_out;       /* n */
+  int32_t groups;
+  int32_t dtype;       /* poetx_dtype of X, Z, dX, dZ and of a dense W */
+  int64_t rows;
+  int32_t flags;       /* POETX_GROUPED_* bits */
+  int32_t reserved;    /* 0 */
+} poetx_grouped_desc;
+
+#define POETX_GROUPED_W_MX4 1   /* W in four bits                                                                  */
+#define POETX_GROUPED_X_MX4 2   /* with W_MX4, forward only: the rows of X are rounded to four bits as well (by the rule
+                                   above, along d_in) and the codes are multiplied; the input gradient passes the rounding by */
+
+/* Scratch of the largest of the three calls below; 0 for an invalid descriptor. */
+size_t poetx_grouped_workspace_bytes(const poetx_grouped_desc* desc);
+
+int poetx_grouped_fwd(const poetx_grouped_desc* desc, const void* X, int64_t ldx, const void* W, const int32_t* offsets,
+                      void* Z, int64_t ldz, void* ws, size_t ws_bytes, void* stream);
+int poetx_grouped_bwd_input(const poetx_grouped_desc* desc, const void* dZ, int64_t lddz, const void* W, const int32_t* offsets,
+                            void* dX, int64_t lddx, void* ws, size_t ws_bytes, void* stream);
+/* dW: groups x d_out x d_in float, overwritten when accumulate == 0 (zeros for a group without rows), added to otherwise.
+ * Dense weights only: with POETX_GROUPED_W_MX4 the weight is frozen and the call is POETX_ERR_UNSUPPORTED. */
+int poetx_grouped_bwd_weight(const poetx_grouped_desc* desc, const void* X, int64_t ldx, const void* dZ, int64_t lddz,
+                             const int32_t* offsets, float* dW, int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* The order that puts rows group by group: ids[n] (int32, the group of each row; a value outside 0 .. groups - 1 is a
+ * row that no group takes) -> offsets[groups + 1], order[n]: order[offsets[g] .. offsets[g+1] - 1] are the rows of g,
+ * ascending; order past offsets[groups] is -1.  With several choices per token, row i of ids[n] is choice i % k of token i / k.
+ * ws: poetx_group_order_workspace_bytes(n, groups) bytes.  Up to POETX_GROUP_ORDER_MAX groups. */
+#define POETX_GROUP_ORDER_MAX 512
+size_t poetx_group_order_workspace_bytes(int64_t n, int32_t groups);
+int poetx_group_order(const int32_t* ids, int64_t n, int32_t groups, int32_t* offsets, int32_t* order, void* ws, size_t ws_bytes,
+                      void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,6 +21,7 @@ FLAG_RECOMPUTE_B = 1
 FLAG_W_INT8 = 2
 FLAG_W_INT8_FUSED = 8
 FLAG_BLOCK_GRADS = 4
+GROUPED_W_MX4, GROUPED_X_MX4 = 1, 2
 FEATURE_MAJOR, TOKEN_MAJOR = 0, 1
 
 EXPORTS = (
@@ -31,6 +32,9 @@ EXPORTS = (
     "poetx_linear_recompute_b", "poetx_linear_bwd",
     "poetx_weight_q8_bytes", "poetx_weight_quantize_q8", "poetx_weight_dequantize_q8",
     "poetx_profile_begin", "poetx_profile_end",
+    "poetx_mx4_bytes", "poetx_mx4_quantize", "poetx_mx4_dequantize",
+    "poetx_grouped_workspace_bytes", "poetx_grouped_fwd", "poetx_grouped_bwd_input", "poetx_grouped_bwd_weight",
+    "poetx_group_order_workspace_bytes", "poetx_group_order",
 )
 STAGES = ("cnp_fwd", "apply", "dense", "blockgrad", "cnp_bwd", "apply_grad", "layout", "dequant")
 
@@ -39,6 +43,11 @@ class LinearDesc(Structure):
     _fields_ = [("d_in", c_int32), ("d_out", c_int32), ("block", c_int32), ("neumann_k", c_int32),
                 ("n_tokens", c_int64), ("dtype", c_int32), ("cnp_precision", c_int32),
                 ("flags", c_int32), ("layout", c_int32)]
+
+
+class GroupedDesc(Structure):
+    _fields_ = [("d_in", c_int32), ("d_out", c_int32), ("groups", c_int32), ("dtype", c_int32), ("rows", c_int64),
+                ("flags", c_int32), ("reserved", c_int32)]
 
 
 class PoetxError(RuntimeError):
@@ -117,6 +126,25 @@ def load_library(path: str | None = None):
     lib.poetx_profile_begin.argtypes = [c_int32]
     lib.poetx_profile_end.restype = c_int
     lib.poetx_profile_end.argtypes = [POINTER(ctypes.c_double), POINTER(c_int64)]
+    lib.poetx_mx4_bytes.restype = c_size_t
+    lib.poetx_mx4_bytes.argtypes = [c_int64, c_int32]
+    lib.poetx_mx4_quantize.restype = c_int
+    lib.poetx_mx4_quantize.argtypes = [c_void_p, c_int32, c_int64, c_int32, c_int64, c_void_p, c_void_p]
+    lib.poetx_mx4_dequantize.restype = c_int
+    lib.poetx_mx4_dequantize.argtypes = [c_void_p, c_int64, c_int32, c_int32, c_void_p, c_int64, c_void_p]
+    lib.poetx_grouped_workspace_bytes.restype = c_size_t
+    lib.poetx_grouped_workspace_bytes.argtypes = [POINTER(GroupedDesc)]
+    for name in ("poetx_grouped_fwd", "poetx_grouped_bwd_input"):
+        f = getattr(lib, name)
+        f.restype = c_int
+        f.argtypes = [POINTER(GroupedDesc), c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_size_t, c_void_p]
+    lib.poetx_grouped_bwd_weight.restype = c_int
+    lib.poetx_grouped_bwd_weight.argtypes = [POINTER(GroupedDesc), c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_int32,
+                                             c_void_p, c_size_t, c_void_p]
+    lib.poetx_group_order_workspace_bytes.restype = c_size_t
+    lib.poetx_group_order_workspace_bytes.argtypes = [c_int64, c_int32]
+    lib.poetx_group_order.restype = c_int
+    lib.poetx_group_order.argtypes = [c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
     _lib = lib
     return lib
 
@@ -140,6 +168,16 @@ def _ptr(t):
         return None
     assert t.is_cuda and t.is_contiguous(), "device-resident contiguous tensors only"
     return c_void_p(t.data_ptr())
+
+
+def _rows_ptr(t):
+    """A matrix whose rows may be further apart than they are long."""
+    assert t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1 or t.shape[0] == 0), "device-resident matrices with contiguous rows only"
+    return c_void_p(t.data_ptr())
+
+
+def _ld(t):
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
 
 
 def _stream():
@@ -316,3 +354,81 @@ def poetx_profile_end() -> dict:
     cnt = (c_int64 * len(STAGES))()
     _check(load_library().poetx_profile_end(ms, cnt), "poetx_profile_end")
     return {s: (ms[i], cnt[i]) for i, s in enumerate(STAGES)}
+
+
+def poetx_mx4_bytes(rows: int, cols: int) -> int:
+    return load_library().poetx_mx4_bytes(rows, cols)
+
+
+def poetx_mx4_quantize(X, Q):
+    """X: rows x cols (f32 or bf16, rows may be strided) -> Q: uint8 buffer of poetx_mx4_bytes(rows, cols) bytes."""
+    rows, cols = X.shape
+    assert _ws_bytes(Q) >= poetx_mx4_bytes(rows, cols), "4-bit buffer too small"
+    _check(load_library().poetx_mx4_quantize(_rows_ptr(X), dtype_code(X), rows, cols, _ld(X), _ptr(Q), _stream()), "poetx_mx4_quantize")
+
+
+def poetx_mx4_dequantize(Q, out):
+    rows, cols = out.shape
+    assert _ws_bytes(Q) >= poetx_mx4_bytes(rows, cols), "4-bit buffer too small"
+    _check(load_library().poetx_mx4_dequantize(_ptr(Q), rows, cols, dtype_code(out), _rows_ptr(out), _ld(out), _stream()),
+           "poetx_mx4_dequantize")
+
+
+def make_grouped_desc(d_in, d_out, groups, rows, dtype, flags=0) -> GroupedDesc:
+    return GroupedDesc(d_in, d_out, groups, dtype, rows, flags, 0)
+
+
+def poetx_grouped_workspace_bytes(desc: GroupedDesc) -> int:
+    return load_library().poetx_grouped_workspace_bytes(ctypes.byref(desc))
+
+
+def _grouped_check(desc, W, offsets, *tensors):
+    """The tensors are those the descriptor speaks of: the library sees pointers only."""
+    torch = _torch()
+    dt = torch.float32 if desc.dtype == F32 else torch.bfloat16
+    for t, d in tensors:
+        assert t.dtype == dt and t.dim() == 2 and t.shape[0] == desc.rows and t.shape[1] == d, "a tensor is not the descriptor's"
+    assert offsets.dtype == torch.int32 and offsets.numel() == desc.groups + 1, "offsets: groups + 1 int32"
+    if W is None:
+        return
+    if desc.flags & GROUPED_W_MX4:
+        assert _ws_bytes(W) >= poetx_mx4_bytes(desc.groups * desc.d_out, desc.d_in), "4-bit weight buffer too small"
+    else:
+        assert W.dtype == dt and W.numel() == desc.groups * desc.d_out * desc.d_in, "W: groups x d_out x d_in"
+
+
+def poetx_grouped_fwd(desc, X, W, offsets, Z, ws=None):
+    """Z: rows x d_out = each row of X (rows x d_in) times its group's weight, transposed.  Rows of X and Z may be strided."""
+    _grouped_check(desc, W, offsets, (X, desc.d_in), (Z, desc.d_out))
+    _check(load_library().poetx_grouped_fwd(ctypes.byref(desc), _rows_ptr(X), _ld(X), _ptr(W), _ptr(offsets), _rows_ptr(Z), _ld(Z), _ptr(ws),
+                                            _ws_bytes(ws) if ws is not None else 0, _stream()),
+           "poetx_grouped_fwd")
+
+
+def poetx_grouped_bwd_input(desc, dZ, W, offsets, dX, ws=None):
+    _grouped_check(desc, W, offsets, (dZ, desc.d_out), (dX, desc.d_in))
+    _check(load_library().poetx_grouped_bwd_input(ctypes.byref(desc), _rows_ptr(dZ), _ld(dZ), _ptr(W), _ptr(offsets), _rows_ptr(dX), _ld(dX),
+                                                  _ptr(ws), _ws_bytes(ws) if ws is not None else 0, _stream()),
+           "poetx_grouped_bwd_input")
+
+
+def poetx_grouped_bwd_weight(desc, X, dZ, offsets, dW, accumulate, ws=None):
+    """dW: groups x d_out x d_in float32."""
+    _grouped_check(desc, None, offsets, (X, desc.d_in), (dZ, desc.d_out))
+    assert dW.dtype == _torch().float32 and dW.numel() == desc.groups * desc.d_out * desc.d_in, "dW: groups x d_out x d_in float32"
+    _check(load_library().poetx_grouped_bwd_weight(ctypes.byref(desc), _rows_ptr(X), _ld(X), _rows_ptr(dZ), _ld(dZ), _ptr(offsets), _ptr(dW),
+                                                   int(bool(accumulate)), _ptr(ws), _ws_bytes(ws) if ws is not None else 0, _stream()),
+           "poetx_grouped_bwd_weight")
+
+
+def poetx_group_order_workspace_bytes(n: int, groups: int) -> int:
+    return load_library().poetx_group_order_workspace_bytes(n, groups)
+
+
+def poetx_group_order(ids, offsets, order, ws=None):
+    """ids: n int32 group numbers -> offsets: groups + 1 int32, order: n int32 (rows group by group, -1 past the last)."""
+    torch = _torch()
+    assert ids.dtype == offsets.dtype == order.dtype == torch.int32 and order.numel() == ids.numel(), "int32 ids, offsets and order"
+    _check(load_library().poetx_group_order(_ptr(ids), ids.numel(), offsets.numel() - 1, _ptr(offsets), _ptr(order), _ptr(ws),
+                                            _ws_bytes(ws) if ws is not None else 0, _stream()),
+           "poetx_group_order")

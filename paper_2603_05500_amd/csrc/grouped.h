@@ -1,0 +1,99 @@
+// Products of rows with their group's weight: what the kernels share.
+#pragma once
+
+#include "poetx_kernels.h"
+
+namespace poetx {
+namespace grouped {
+
+// Which product.  FWD: Z = X W^T, INPUT: dX = dZ W, WEIGHT: dW = dZ^T X.
+enum Dir { FWD = 0, INPUT = 1, WEIGHT = 2 };
+
+// A call.  in: X (FWD, WEIGHT) or dZ (INPUT); in2: dZ (WEIGHT); w: the dense weight; out: Z, dX or dW.
+struct Call {
+  const void* in;
+  const void* in2;
+  const void* w;
+  void* out;
+  i64 ld_in, ld_in2, ld_out;
+  const int32_t* offsets;
+  i64 rows;
+  int m, n, groups;
+  int accumulate;
+};
+
+// First row and end of group g, inside the tensor whatever the offsets say.
+struct Range {
+  int r0, r1;
+};
+__device__ __forceinline__ Range group_range(const int32_t* offsets, int g, i64 rows) {
+  const int last = (int)rows;
+  const int a = offsets[g], b = offsets[g + 1];
+  const int r0 = a < 0 ? 0 : a > last ? last : a;
+  const int r1 = b < r0 ? r0 : b > last ? last : b;
+  return Range{r0, r1};
+}
+
+// Sum over a wave of the values of lower lanes and this one.
+__device__ __forceinline__ int wave_scan(int v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) {
+    const int o = __shfl_up(v, s);
+    if (lane >= s) v += o;
+  }
+  return v;
+}
+
+// Tiles of `height` rows of all groups; a group's last tile may be short.
+__device__ inline int count_row_tiles(const int32_t* offsets, int groups, i64 rows, int height) {
+  const int lane = threadIdx.x & 63;
+  int total = 0;
+  for (int base = 0; base < groups; base += 64) {
+    int t = 0;
+    if (base + lane < groups) {
+      const Range r = group_range(offsets, base + lane, rows);
+      t = (r.r1 - r.r0 + height - 1) / height;
+    }
+    total += __builtin_amdgcn_readlane(wave_scan(t), 63);
+  }
+  return total;
+}
+// Tile u of them (u below their number): its group, its first row and the group's end.
+struct RowTile {
+  int g, r0, r1;
+};
+__device__ inline RowTile find_row_tile(const int32_t* offsets, int groups, i64 rows, int height, int u) {
+  const int lane = threadIdx.x & 63;
+  for (int base = 0; base < groups; base += 64) {
+    int t = 0;
+    Range r{0, 0};
+    if (base + lane < groups) {
+      r = group_range(offsets, base + lane, rows);
+      t = (r.r1 - r.r0 + height - 1) / height;
+    }
+    const int sum = wave_scan(t), all = __builtin_amdgcn_readlane(sum, 63);
+    if (u < all) {
+      const int l = __builtin_ctzll(__ballot(sum > u));      // all > u: some lane has it
+      const int before = __builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(t, l);
+      return RowTile{base + l, __builtin_amdgcn_readlane(r.r0, l) + (u - before) * height, __builtin_amdgcn_readlane(r.r1, l)};
+    }
+    u -= all;
+  }
+  return RowTile{0, 0, 0};
+}
+
+// Row tiles that any offsets of so many groups and rows can have.
+inline i64 most_row_tiles(i64 rows, int groups, int height) { return rows / height + (rows < groups ? rows : groups); }
+
+// Workgroup bx of `total` that work: consecutive ones go to the 8 XCDs in turn, so that XCD's take contiguous runs of the work.
+__device__ __forceinline__ int xcd_run(int bx, int total) {
+  const int xcd = bx & 7, per = total >> 3, extra = total & 7;
+  return xcd * per + (xcd < extra ? xcd : extra) + (bx >> 3);
+}
+
+// ---- launchers -----------------------------------------------------------------------------------
+void edge_launch(int dtype, Dir dir, const Call& c, hipStream_t st);      // any shape (grouped_edge.hip)
+
+}  // namespace grouped
+}  // namespace poetx

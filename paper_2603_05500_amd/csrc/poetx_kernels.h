@@ -172,4 +172,12 @@ bool skew_tiled_supported(int b, i64 d);
 void skew_materialize_tiled_launch(const float* theta, int b, i64 nb, float* Qf, uint16_t* Qb, uint16_t* Tb, hipStream_t st);
 void skew_project_tiled_launch(const float* M, int b, i64 nb, float* dtheta, int accumulate, hipStream_t st);
 
+// ---- 4-bit buffers (mx4.hip; layout: mx4.h) -----------------------------------------------------
+void mx4_quantize_launch(int dtype, const void* X, i64 rows, int cols, i64 ld, void* Q, hipStream_t st);
+void mx4_dequantize_launch(const void* Q, i64 rows, int cols, int dtype, void* out, i64 ld, hipStream_t st);
+
+// ---- rows in the order of their groups (group_order.hip) ---------------------------------------
+size_t group_order_workspace_bytes(i64 n, int groups);
+void group_order_launch(const int32_t* ids, i64 n, int groups, int32_t* offsets, int32_t* order, void* ws, hipStream_t st);
+
 }  // namespace poetx

@@ -1,0 +1,379 @@
+"""4-bit buffers, grouped products and the order of groups against plain float64 forms written here.
+
+Bounds.  A product of two bf16 (or of two 4-bit values) is exact in fp32, so a result differs from the exact sum by the
+roundings of K fp32 additions, at most K 2^-24 of the sum of magnitudes (fp32 inputs: one rounding more per product), and by
+one rounding to its own type: 2^-8 of itself in bf16 (8 significant bits, half a unit of the last), 2^-24 in fp32.  Conversions to and from four bits are exact."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2603_05500_amd as px
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+CODE = {"f32": px.F32, "bf16": px.BF16}
+GRID = np.array([0, .5, 1, 1.5, 2, 3, 4, 6])
+
+
+def dev(a, dtype):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(dtype).cuda()
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def strided(rows, cols, pad, dtype, shift=0, fill=float("nan")):
+    """A rows x cols matrix with `pad` columns between its rows and `shift` elements in front, all of them `fill`."""
+    flat = torch.full((rows * (cols + pad) + shift + 8,), fill, dtype=dtype, device="cuda")
+    return flat[shift: shift + rows * (cols + pad)].view(rows, cols + pad)[:, :cols], flat
+
+
+# ------------------------------------------------------------------------------------ four bits
+def oracle_codes(x):
+    """float64 [rows][cols] -> codes [rows][mp], scale bytes [rows][mp / 32], by the definition."""
+    rows, cols = x.shape
+    mp = -(-cols // 128) * 128
+    code, scale = np.zeros((rows, mp), np.int64), np.zeros((rows, mp // 32), np.int64)
+    p = np.zeros((rows, mp))
+    p[:, :cols] = x
+    for b in range(mp // 32):
+        blk = p[:, 32 * b: 32 * b + 32]
+        for r in range(rows):
+            v = blk[r]
+            if not np.isfinite(v).all():
+                scale[r, b] = 255
+                continue
+            top = np.abs(v).max()
+            if top == 0:
+                code[r, 32 * b: 32 * b + 32] = 8 * np.signbit(v)
+                continue
+            s = min(max(int(np.floor(np.log2(top))) - 2 + 127, 0), 254)
+            scale[r, b] = s
+            a = np.abs(v) * 2.0 ** (127 - s)
+            dist = np.abs(a[:, None] - GRID[None])
+            c = dist.argmin(1)                      # the lower of two equally near ...
+            tie = (c < 7) & (dist[np.arange(32), c] == dist[np.arange(32), np.minimum(c + 1, 7)])
+            c = np.where(tie & (c % 2 == 1), c + 1, c)     # ... unless the upper one is even
+            code[r, 32 * b: 32 * b + 32] = c + 8 * np.signbit(v)
+    return code, scale
+
+
+def oracle_values(code, scale, cols):
+    v = GRID[code & 7] * np.where(code & 8, -1.0, 1.0)
+    s = np.where(scale == 255, np.nan, 2.0 ** (scale - 127.0))
+    return (v * np.repeat(s, 32, axis=1))[:, :cols]
+
+
+def split_buffer(Q, rows, cols):
+    q = Q.cpu().numpy()
+    mp = -(-cols // 128) * 128
+    off = -(-rows * mp // 2 // 256) * 256
+    b = q[: rows * mp // 2].reshape(rows, -1).astype(np.int64)
+    code = np.stack([b & 15, b >> 4], -1).reshape(rows, mp)
+    return code, q[off: off + rows * mp // 32].reshape(rows, -1).astype(np.int64)
+
+
+def quantised(W, fill=255):
+    """W (rows x cols on the device) -> its 4-bit buffer, which held `fill` before."""
+    Q = torch.full((px.poetx_mx4_bytes(*W.shape),), fill, dtype=torch.uint8, device="cuda")
+    px.poetx_mx4_quantize(W, Q)
+    return Q
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols,pad,shift", [(1, 1, 0, 0), (3, 31, 0, 0), (5, 32, 0, 0), (2, 33, 7, 1), (4, 127, 1, 3), (7, 128, 8, 0), (17, 160, 0, 0),
+                                                 (33, 257, 3, 1), (9, 1376, 0, 0), (1, 4096, 0, 0)])
+def test_mx4_round_trip(lib, rows, cols, pad, shift, dtype):
+    rng = np.random.default_rng(rows * 1000 + cols)
+    x = rng.standard_normal((rows, cols)) * np.exp2(rng.integers(-30, 30, (rows, 1)).astype(float))
+    X, _ = strided(rows, cols, pad, DT[dtype], shift)
+    X.copy_(dev(x, DT[dtype]))
+    code, scale = oracle_codes(host(X))
+    Q = quantised(X)
+    got_c, got_s = split_buffer(Q, rows, cols)
+    assert np.array_equal(got_s, scale) and np.array_equal(got_c, code)
+    want = oracle_values(code, scale, cols)
+    for out_type in ("bf16", "f32"):
+        out, flat = strided(rows, cols, pad, DT[out_type], shift, fill=7.0)
+        px.poetx_mx4_dequantize(Q, out)
+        assert np.array_equal(host(out), want)
+        left = flat.clone()
+        left[shift: shift + rows * (cols + pad)].view(rows, cols + pad)[:, :cols] = 7.0
+        assert bool((left == 7.0).all()), "written outside the matrix"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_mx4_ties_and_extremes(lib, dtype):
+    """Every tie and its neighbours, zeros, the smallest and largest numbers, infinities and NaN."""
+    tie = np.array([.25, .75, 1.25, 1.75, 2.5, 3.5, 5, 7.5])
+    rows = [np.concatenate([[4.0], tie[:7], -tie[:7], np.zeros(17)]), np.concatenate([[7.5, -7.5], tie, -tie, np.zeros(14)]),
+            np.concatenate([[4.0], tie[:7] * (1 + 2.0 ** -7), tie[:7] * (1 - 2.0 ** -7), np.full(17, -0.0)]),
+            np.zeros(32), np.full(32, -0.0), np.full(32, 2.0 ** -126), np.full(32, 2.0 ** -130), np.full(32, 3.0e38), np.arange(32) * 2.0 ** -133,
+            np.r_[np.inf, np.ones(31)], np.r_[np.ones(31), -np.inf], np.r_[np.ones(7), np.nan, np.zeros(24)], np.r_[1e30, np.full(31, 1e-30)]]
+    X = dev(np.array(rows), DT[dtype])
+    code, scale = oracle_codes(host(X))
+    Q = quantised(X)
+    got_c, got_s = split_buffer(Q, *X.shape)
+    assert np.array_equal(got_s, scale) and np.array_equal(got_c, code)
+    out = torch.empty_like(X)
+    px.poetx_mx4_dequantize(Q, out)
+    assert np.array_equal(host(out), oracle_values(code, scale, 32), equal_nan=True)
+
+
+def test_mx4_all_codes_and_scales(lib):
+    """A buffer a caller built: every code under every scale byte, 2^-127 and NaN among them; what bf16 or fp32 cannot hold is infinite."""
+    rows = 256
+    code = np.tile(np.r_[np.arange(16), np.arange(16)[::-1]], (rows, 4))
+    scale = np.tile(np.arange(256)[:, None], (1, 4))
+    Q = torch.from_numpy(np.concatenate([(code[:, 0::2] + 16 * code[:, 1::2]).astype(np.uint8).ravel(), scale.astype(np.uint8).ravel()])).cuda()
+    want = torch.from_numpy(oracle_values(code, scale, 128))
+    for dtype in DT.values():
+        out = torch.empty((rows, 128), dtype=dtype, device="cuda")
+        px.poetx_mx4_dequantize(Q, out)
+        assert np.array_equal(host(out), want.to(dtype).double().numpy(), equal_nan=True)
+
+
+# ------------------------------------------------------------------------------------ grouped products
+def offsets_of(counts):
+    return torch.tensor(np.r_[0, np.cumsum(counts)], dtype=torch.int32, device="cuda")
+
+
+def bound(mag, ref, K, dtype):
+    return (K + 4) * 2.0 ** -24 * mag + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -23) * np.abs(ref) + 1e-37
+
+
+def check(got, ref, mag, K, dtype, what):
+    assert np.isfinite(got).all(), what
+    err, lim = np.abs(got - ref), bound(mag, ref, K, dtype)
+    assert (err <= lim).all(), (what, float(err.max()), float((err / lim).max()))
+
+
+def run_grouped(counts, m, n, dtype, weight="dense", act="same", pads=(0, 0), shift=0, extra=0, kinds=("fwd", "input", "weight"), seed=0):
+    """All the calls on groups of `counts` rows, with `extra` rows behind them that no group has, against float64."""
+    rng = np.random.default_rng(seed + m + 7 * n + 31 * len(counts))
+    G, rows, dt = len(counts), int(sum(counts)) + extra, DT[dtype]
+    off = offsets_of(counts)
+    ends = off.cpu().numpy()
+    X, _ = strided(rows, m, pads[0], dt, shift)
+    dZ, _ = strided(rows, n, pads[1], dt, shift)
+    live = int(sum(counts))
+    X[:live].copy_(dev(rng.standard_normal((live, m)), dt))       # the rows of no group stay NaN, as does what lies between rows
+    dZ[:live].copy_(dev(rng.standard_normal((live, n)) * 0.1, dt))
+    W = dev(rng.standard_normal((G, n, m)) * 0.02, dt)
+    flags = 0
+    Wx, Wh, Xh, dZh = W, host(W), host(X), host(dZ)
+    if weight == "mx4":
+        Wx, flags = quantised(W.view(G * n, m)), px.GROUPED_W_MX4
+        Wh = oracle_values(*split_buffer(Wx, G * n, m), m).reshape(G, n, m)
+    if act == "mx4":
+        flags |= px.GROUPED_X_MX4
+        q = quantised(X[:live].contiguous()) if live else None
+        Xq = oracle_values(*split_buffer(q, live, m), m) if live else Xh
+    desc = px.make_grouped_desc(m, n, G, rows, CODE[dtype], flags)
+    need = px.poetx_grouped_workspace_bytes(desc)
+    ws = torch.full((need // 4 + 64,), float("nan"), device="cuda").view(torch.uint8) if need else None
+    res = {}
+    if "fwd" in kinds:
+        Z, flat = strided(rows, n, pads[1], dt, shift, fill=3.0)
+        px.poetx_grouped_fwd(desc, X, Wx, off, Z, ws)
+        ref, mag = np.full((rows, n), 3.0), np.zeros((rows, n))
+        xs = Xq if act == "mx4" else Xh
+        for g in range(G):
+            a, b = ends[g], ends[g + 1]
+            ref[a:b], mag[a:b] = xs[a:b] @ Wh[g].T, np.abs(xs[a:b]) @ np.abs(Wh[g]).T
+        check(host(Z), ref, mag, m, dtype, "Z")
+        Z.fill_(3.0)
+        assert bool((flat == 3.0).all()), "Z: written outside the matrix"
+        res["Z"] = Z
+    if "input" in kinds:
+        dX, flat = strided(rows, m, pads[0], dt, shift, fill=3.0)
+        px.poetx_grouped_bwd_input(desc, dZ, Wx, off, dX, ws)
+        ref, mag = np.full((rows, m), 3.0), np.zeros((rows, m))
+        for g in range(G):
+            a, b = ends[g], ends[g + 1]
+            ref[a:b], mag[a:b] = dZh[a:b] @ Wh[g], np.abs(dZh[a:b]) @ np.abs(Wh[g])
+        check(host(dX), ref, mag, n, dtype, "dX")
+        dX.fill_(3.0)
+        assert bool((flat == 3.0).all()), "dX: written outside the matrix"
+    if "weight" in kinds and weight == "dense":
+        dW = torch.full((G, n, m), float("nan"), device="cuda")
+        px.poetx_grouped_bwd_weight(desc, X, dZ, off, dW, False, ws)
+        first = dW.clone()
+        px.poetx_grouped_bwd_weight(desc, X, dZ, off, dW, True, ws)
+        for g in range(G):
+            a, b = ends[g], ends[g + 1]
+            ref, mag = dZh[a:b].T @ Xh[a:b], np.abs(dZh[a:b]).T @ np.abs(Xh[a:b])
+            check(host(first[g]), ref, mag, b - a, "f32", "dW")
+            check(host(dW[g]), 2 * ref, 2 * mag, b - a, "f32", "dW added to")
+    return res
+
+
+SHAPES = [
+    # counts, m, n
+    ([1], 1, 1), ([0], 8, 8), ([3], 7, 5), ([1, 0, 2], 33, 17), ([5, 1, 0, 130, 64], 64, 96), ([31, 33, 32], 100, 60),
+    ([0, 0, 7], 256, 128), ([257], 130, 258), ([128, 129, 127], 128, 256), ([300, 0, 1, 211], 256, 320), ([64] * 5, 96, 1376),
+    ([1] * 70, 64, 64), ([2, 0] * 70, 40, 72), ([600, 5], 512, 264),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("counts,m,n", SHAPES)
+def test_grouped(lib, counts, m, n, dtype):
+    run_grouped(counts, m, n, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pads,shift,extra", [((8, 16), 0, 0), ((3, 5), 0, 9), ((0, 0), 1, 0), ((8, 8), 8, 130), ((1, 0), 3, 1)])
+def test_grouped_strides(lib, pads, shift, extra, dtype):
+    run_grouped([17, 0, 150, 3], 136, 200, dtype, pads=pads, shift=shift, extra=extra)
+
+
+@pytest.mark.parametrize("act", ["same", "mx4"])
+@pytest.mark.parametrize("counts,m,n", SHAPES + [([1], 4096, 512), ([1, 1, 0, 1], 1024, 1376), ([16], 640, 256), ([17, 40], 2048, 264), ([513], 1408, 512)])
+def test_grouped_mx4(lib, counts, m, n, act):
+    run_grouped(counts, m, n, "bf16", weight="mx4", act=act)
+
+
+@pytest.mark.parametrize("act", ["same", "mx4"])
+@pytest.mark.parametrize("pads,shift,extra", [((8, 16), 0, 0), ((3, 5), 0, 9), ((0, 0), 1, 0), ((8, 8), 8, 130)])
+def test_grouped_mx4_strides(lib, pads, shift, extra, act):
+    run_grouped([17, 0, 150, 3], 136, 200, "bf16", weight="mx4", act=act, pads=pads, shift=shift, extra=extra)
+
+
+@pytest.mark.parametrize("weight", ["dense", "mx4"])
+def test_grouped_not_finite(lib, weight):
+    """An infinity or NaN in one row or one group's weight stays in what reads it."""
+    m, n, counts = 256, 256, [130, 70, 0, 300]
+    G, rows = len(counts), sum(counts)
+    off = offsets_of(counts)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    X, dZ = (torch.randn((rows, d), device="cuda", generator=g).bfloat16() for d in (m, n))
+    W = (torch.randn((G, n, m), device="cuda", generator=g) * 0.02).bfloat16()
+    X[129, 255], X[200, 0], dZ[130, 3], dZ[199, 255] = float("nan"), float("inf"), float("nan"), float("-inf")
+    W[2] = float("nan")                       # the weight of a group without rows
+    W[3, 5, 7] = float("nan")
+    Wx, flags = (quantised(W.view(G * n, m)), px.GROUPED_W_MX4) if weight == "mx4" else (W, 0)
+    desc = px.make_grouped_desc(m, n, G, rows, px.BF16, flags)
+    ws = torch.empty(max(256, px.poetx_grouped_workspace_bytes(desc)), dtype=torch.uint8, device="cuda")
+    Z, dX = torch.empty((rows, n), dtype=torch.bfloat16, device="cuda"), torch.empty((rows, m), dtype=torch.bfloat16, device="cuda")
+    px.poetx_grouped_fwd(desc, X, Wx, off, Z, ws)
+    px.poetx_grouped_bwd_input(desc, dZ, Wx, off, dX, ws)
+    bad = ~torch.isfinite(Z)
+    want = torch.zeros_like(bad)
+    want[129] = want[200] = True
+    want[200:, 5] = True
+    assert torch.equal(bad, want)
+    bad = ~torch.isfinite(dX)
+    want = torch.zeros_like(bad)
+    want[130] = want[199] = True
+    cols = slice(0, 32) if weight == "mx4" else slice(7, 8)      # a block of four-bit values shares its NaN
+    want[200:, cols] = True
+    assert torch.equal(bad, want)
+    if weight == "dense":
+        dW = torch.empty((G, n, m), device="cuda")
+        px.poetx_grouped_bwd_weight(desc, X, dZ, off, dW, False, ws)
+        bad = ~torch.isfinite(dW)
+        want = torch.zeros_like(bad)
+        want[0, :, 255] = want[1, 3] = want[1, 255] = want[3, :, 0] = True
+        assert torch.equal(bad, want)
+
+
+def test_grouped_offsets_out_of_range(lib):
+    """Offsets past the rows, below zero or decreasing touch nothing outside the tensors; groups that are in order get their rows."""
+    m = n = 128
+    rows = 100
+    X = torch.randn((rows, m), device="cuda").bfloat16()
+    W = torch.randn((4, n, m), device="cuda").bfloat16()
+    desc = px.make_grouped_desc(m, n, 4, rows, px.BF16)
+    off = torch.tensor([-5, 40, 30, 70, 1000], dtype=torch.int32, device="cuda")
+    flat = torch.full((rows + 64, n), 3.0, dtype=torch.bfloat16, device="cuda")
+    Z = flat[:rows]
+    px.poetx_grouped_fwd(desc, X, W, off, Z)
+    ref = torch.empty((rows, n), dtype=torch.float64)
+    for a, b, g in ((0, 30, 0), (40, 70, 2), (70, 100, 3)):      # rows 30 .. 39 are claimed twice
+        ref[a:b] = X[a:b].double().cpu() @ W[g].double().cpu().t()
+        assert float((Z[a:b].double().cpu() - ref[a:b]).abs().max()) <= 2.0 ** -8 * float(ref[a:b].abs().max())
+    assert bool((flat[rows:] == 3.0).all())
+
+
+def test_gradients_against_differences(lib):
+    """dX and dW are the derivatives of L = <dZ, Z(X, W)>: Z is linear in either, so differences of any size are exact."""
+    counts, m, n = [5, 0, 9], 24, 40
+    G, rows = len(counts), sum(counts)
+    off = offsets_of(counts)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    X, dZ = (torch.randn((rows, d), device="cuda", generator=g) for d in (m, n))
+    W = torch.randn((G, n, m), device="cuda", generator=g)
+    desc = px.make_grouped_desc(m, n, G, rows, px.F32)
+    dX, dW = torch.empty_like(X), torch.empty_like(W)
+    px.poetx_grouped_bwd_input(desc, dZ, W, off, dX)
+    px.poetx_grouped_bwd_weight(desc, X, dZ, off, dW, False)
+
+    def loss(x, w):
+        Z = torch.zeros((rows, n), device="cuda")
+        px.poetx_grouped_fwd(desc, x, w, off, Z)
+        return float((Z.double() * dZ.double()).sum())
+
+    for i in range(6):
+        vx, vw = torch.randn(X.shape, device="cuda", generator=g), torch.randn(W.shape, device="cuda", generator=g)
+        size = float(vx.abs().sum() + vw.abs().sum())      # every product of the sums is of order one
+        assert abs((loss(X + vx, W) - loss(X - vx, W)) / 2 - float((dX.double() * vx.double()).sum())) < 1e-6 * size * n
+        assert abs((loss(X, W + vw) - loss(X, W - vw)) / 2 - float((dW.double() * vw.double()).sum())) < 1e-6 * size * n
+
+
+def test_results_do_not_depend_on_the_other_groups(lib):
+    """A group's rows and weight give the same bits again on a second call."""
+    for dtype in ("bf16", "f32"):
+        a = run_grouped([300, 0, 77, 140], 256, 512, dtype, kinds=("fwd",))["Z"]
+        X = torch.randn((517, 256), device="cuda").to(DT[dtype])
+        dZ = torch.randn((517, 512), device="cuda").to(DT[dtype])
+        desc = px.make_grouped_desc(256, 512, 4, 517, CODE[dtype])
+        off = offsets_of([300, 0, 77, 140])
+        dW = [torch.empty((4, 512, 256), device="cuda") for _ in range(2)]
+        for w in dW:
+            px.poetx_grouped_bwd_weight(desc, X, dZ, off, w, False)
+        assert torch.equal(dW[0], dW[1]) and a.shape == (517, 512)
+
+
+def test_grouped_on_another_stream(lib):
+    """The calls run on the current stream, behind what it holds."""
+    X = torch.zeros((512, 256), dtype=torch.bfloat16, device="cuda")
+    W = torch.randn((2, 256, 256), device="cuda").bfloat16()
+    Z = torch.empty((512, 256), dtype=torch.bfloat16, device="cuda")
+    off = offsets_of([200, 312])
+    desc = px.make_grouped_desc(256, 256, 2, 512, px.BF16)
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        X.copy_(torch.randn((512, 256), device="cuda"))
+        px.poetx_grouped_fwd(desc, X, W, off, Z)
+        got = Z.clone()
+    st.synchronize()
+    px.poetx_grouped_fwd(desc, X, W, off, Z)
+    assert torch.equal(got, Z) and float(Z.abs().max()) > 0
+
+
+# ------------------------------------------------------------------------------------ order
+@pytest.mark.parametrize("n,groups", [(0, 3), (1, 1), (1, 512), (8, 64), (63, 5), (64, 2), (1000, 7), (8192, 128), (8193, 128), (10000, 512), (131072, 100), (300001, 3)])
+@pytest.mark.parametrize("dropped", [0.0, 0.3, 1.0])
+def test_group_order(lib, n, groups, dropped):
+    rng = np.random.default_rng(n + groups)
+    ids = rng.integers(0, groups, n)
+    if groups > 4:
+        ids[ids == 3] = 2                          # a group without rows
+    gone = rng.random(n) < dropped
+    ids[gone] = rng.choice([-1, groups, groups + 5, -2 ** 31, 2 ** 31 - 1], n)[gone]
+    keep = (ids >= 0) & (ids < groups)
+    want_off = np.r_[0, np.cumsum(np.bincount(ids[keep], minlength=groups))]
+    want = np.full(n, -1)
+    kept = np.flatnonzero(keep)
+    want[: len(kept)] = kept[np.argsort(ids[keep], kind="stable")]
+    off = torch.full((groups + 1,), -7, dtype=torch.int32, device="cuda")
+    order = torch.full((n,), -7, dtype=torch.int32, device="cuda")
+    ws = torch.full((max(256, px.poetx_group_order_workspace_bytes(n, groups)),), 255, dtype=torch.uint8, device="cuda")
+    px.poetx_group_order(torch.from_numpy(ids.astype(np.int32)).cuda(), off, order, ws)
+    assert np.array_equal(off.cpu().numpy(), want_off) and np.array_equal(order.cpu().numpy(), want)
