@@ -94,6 +94,12 @@ __device__ __forceinline__ int xcd_run(int bx, int total) {
 
 // ---- launchers -----------------------------------------------------------------------------------
 void edge_launch(int dtype, Dir dir, const Call& c, hipStream_t st);      // any shape (grouped_edge.hip)
+// bf16 in whole 16-byte vectors (grouped_stream.hip)
+bool stream_supported(Dir dir, const Call& c);
+void stream_launch(Dir dir, const Call& c, hipStream_t st);
+// Z = X W^T on 4-bit buffers of both
+bool codes_supported(const poetx_grouped_desc* d, const void* Z, i64 ldz);
+void codes_launch(const poetx_grouped_desc* d, const void* Xq, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, hipStream_t st);
 
 }  // namespace grouped
 }  // namespace poetx

@@ -61,7 +61,8 @@ const void* dense_weight(const poetx_grouped_desc* d, const void* W, void* ws, h
 
 void product(int dtype, grouped::Dir dir, const grouped::Call& c, hipStream_t st) {
   StageTimer tm(POETX_STAGE_DENSE, st);
-  grouped::edge_launch(dtype, dir, c, st);
+  if (dtype == POETX_BF16 && grouped::stream_supported(dir, c)) grouped::stream_launch(dir, c, st);
+  else grouped::edge_launch(dtype, dir, c, st);
 }
 
 // Forward and input gradient: in is rows x d_i, out rows x d_o.
@@ -114,6 +115,15 @@ int poetx_grouped_fwd(const poetx_grouped_desc* d, const void* X, int64_t ldx, c
   const int rc = check_rows_call(d, X, ldx, d ? d->d_in : 0, W, offsets, Z, ldz, d ? d->d_out : 0, ws, ws_bytes);
   if (rc != POETX_OK || d->rows == 0) return rc;
   hipStream_t st = (hipStream_t)stream;
+  if ((d->flags & POETX_GROUPED_X_MX4) && grouped::codes_supported(d, Z, ldz)) {
+    {
+      StageTimer tm(POETX_STAGE_DEQUANT, st);
+      mx4_quantize_launch(POETX_BF16, X, d->rows, d->d_in, ldx, ws, st);
+    }
+    StageTimer tm(POETX_STAGE_DENSE, st);
+    grouped::codes_launch(d, ws, W, offsets, Z, ldz, st);
+    return launch_status();
+  }
   const void* w = dense_weight(d, W, ws, st);
   if (d->flags & POETX_GROUPED_X_MX4) {
     char* values = (char*)ws + dequantised_bytes(d);

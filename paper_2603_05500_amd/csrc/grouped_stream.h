@@ -1,0 +1,450 @@
+// Grouped bf16 products on the matrix cores, and those of 4-bit operands: the kernel.
+//   FWD     Z  (rows x n) = X  (rows x m) W_g^T      both operands contracted along their rows
+//   INPUT   dX (rows x m) = dZ (rows x n) W_g        W_g over its strided index
+//   WEIGHT  dW_g (n x m)  = dZ^T X over g's rows     both over their strided index; fp32 out
+//
+// The same persistent stream as the dense product's: one workgroup per CU, 4 waves (2 x 2), the operand stages of all the tiles a
+// workgroup computes in one ring of LDS stages filled by direct-to-LDS loads well ahead of the multiplication and across tiles, fragments of the next stage read
+// under the products of this one.  What differs:
+//  - Which rows a tile has is only known on the device.  Each wave holds the groups' row ranges in registers (four groups per lane) and
+//    finds a tile's group by ballots, once per tile on the loading side and once on the storing side.
+//  - Groups end inside tiles, and contractions inside stages.  The loads go through buffer descriptors that end where the operand
+//    does: what lies behind reads as zeros, on both operands, so that nothing of another group takes part.  Only the last stage of rows whose length is
+//    no multiple of a stage needs a mask, the same 64 lanes for every load of it.  Past the last tile the descriptors are
+//    empty: the number of loads in flight never changes and the last ones cost no traffic.
+//  - FP4: a stage is 64 bytes of a row either way, 32 bf16 or 128 codes with a word of four scales, and an MFMA of 16 x 16 x 128 codes takes as long
+//    as one of 16 x 16 x 32 bf16: the same stream carries four times the products.
+#pragma once
+#include "grouped.h"
+#include "mfma_dense_kernel.h"
+#include "mx4.h"
+
+namespace poetx {
+namespace grouped {
+
+using dense::floatx4;
+using mm::bf16x8;
+using mx4::u32x4;
+
+
+
+template <int BM_, int BN_, int NS_, bool FP4_>
+struct StreamTile {
+  static constexpr int BM = BM_, BN = BN_, NS = NS_, NW = 4;
+  static constexpr bool FP4 = FP4_;
+  static constexpr int SETS = FP4 ? 2 : 4, GROUPS = 64 * SETS;      // groups per lane (codes leave fewer registers), in all
+  static constexpr int A_BYTES = BM * 64, B_BYTES = BN * 64, S_BYTES = FP4 ? (BM + BN) * 4 : 0, STAGE_BYTES = A_BYTES + B_BYTES + S_BYTES;
+  static constexpr int TM = BM / 32, TN = BN / 32, MF = TM * TN;
+  static constexpr int RS = MF / (TM + TN) < 3 ? MF / (TM + TN) : 3;
+  static constexpr int OUT_BYTES = TN / 4 * 2048;
+  static constexpr int LDS_BYTES = NS * STAGE_BYTES + NW * OUT_BYTES;
+  static constexpr int IPWA = A_BYTES / 1024 / NW, IPWB = B_BYTES / 1024 / NW, IPWS = FP4 ? (BM + BN) / 256 : 0;
+  static constexpr int LPT = IPWA + IPWB + IPWS;
+  static constexpr int DS = MF / LPT;
+  static_assert(!FP4 || (BM == BN && (BM + BN) % 256 == 0), "scale loads: as many for every wave, each of one operand");
+  static_assert(NS * LPT < 64 && DS >= 1 && RS >= 1 && (TM + TN) * RS <= MF && TN % 4 == 0 && LDS_BYTES <= 160 * 1024, "stream tile");
+};
+
+struct StreamArgs {
+  const char* A;          // FWD, INPUT: rows of X or dZ; WEIGHT: dZ.  FP4: codes
+  const char* B;          // W, or X (WEIGHT).  FP4: codes
+  const uint8_t* SA;      // FP4: scales
+  const uint8_t* SB;
+  void* C;
+  i64 lda, ldb, ldc;      // row strides: bytes of A and B, elements of C
+  const int32_t* offsets;
+  i64 rows;
+  int groups;
+  int K;                  // FWD, INPUT: contraction, in elements (FP4: of whole units)
+  int M, N;               // WEIGHT: rows of C (n); columns of C
+  int tiles_n;            // column tiles
+  int accumulate;
+};
+
+// 16 (4) bytes per lane from base + voff straight into LDS at lds + 16 (4) * lane; zeros from the descriptor's end on.
+__device__ __forceinline__ void dma16b(const u32x4& rsrc, uint32_t voff, uint32_t lds) {
+  asm volatile("buffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "{m0}"(lds) : "memory");
+}
+__device__ __forceinline__ void dma4b(const u32x4& rsrc, uint32_t voff, uint32_t lds) {
+  asm volatile("buffer_load_dword %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "{m0}"(lds) : "memory");
+}
+
+// One operand of the tile in issue: where its next stage starts and how many bytes there are from there on.
+struct Feed {
+  uint64_t at;
+  i64 left;
+  __device__ __forceinline__ u32x4 rsrc(bool on) const {      // empty if !on
+    const i64 most = 0x7ffffff0;      // a stage or a tile spans less
+    const int n = left <= 0 || !on ? 0 : (int)(left < most ? left : most);
+    return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)at), (uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) & 0xffffu,
+                 (uint32_t)__builtin_amdgcn_readfirstlane(n), 0x00020000u};
+  }
+  __device__ __forceinline__ void step(i64 bytes) {
+    at += bytes;
+    left -= bytes;
+  }
+};
+
+constexpr int kNowhere = 0x7ffffff0;      // an offset behind every descriptor
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(void* p, i64 bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(p, (short)0, bytes <= 0 ? 0 : (int)(bytes < kNowhere ? bytes : kNowhere), 0x00020000);
+}
+
+__device__ __forceinline__ void mfma_fp4(floatx4& c, const u32x4& a, const u32x4& b, uint32_t sa, uint32_t sb) {
+  asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] cbsz:4 blgp:4" : "+a"(c) : "v"(a), "v"(b), "v"(sa), "v"(sb));
+}
+
+template <Dir DIR, class C>
+__global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
+  constexpr bool FP4 = C::FP4, A_K = DIR != WEIGHT, B_K = DIR == FWD;
+  static_assert(!FP4 || DIR == FWD, "codes are contracted along their rows");
+  constexpr int BM = C::BM, BN = C::BN, NS = C::NS, STAGE_BYTES = C::STAGE_BYTES, A_BYTES = C::A_BYTES;
+  constexpr int IPWA = C::IPWA, IPWB = C::IPWB, IPWS = C::IPWS, LPT = C::LPT, TM = C::TM, TN = C::TN, MF = C::MF, RS = C::RS, DS = C::DS;
+  constexpr int GROUP = dense::GROUP;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+
+  // ---- the groups: lane l of set q has group 64 q + l
+  constexpr int kTableSets = C::SETS;
+  int tr0[kTableSets], tr1[kTableSets], tsum[kTableSets];
+  int row_tiles = 0;
+#pragma unroll
+  for (int q = 0; q < kTableSets; ++q) {
+    const int gr = 64 * q + lane;
+    Range r{0, 0};
+    if (gr < g.groups) r = group_range(g.offsets, gr, g.rows);
+    tr0[q] = r.r0;
+    tr1[q] = r.r1;
+    tsum[q] = 0;
+    if (DIR != WEIGHT && 64 * q < g.groups) {
+      tsum[q] = row_tiles + wave_scan((r.r1 - r.r0 + BM - 1) / BM);
+      row_tiles = __builtin_amdgcn_readlane(tsum[q], 63);
+    }
+  }
+  const int tiles_m = DIR == WEIGHT ? (g.M + BM - 1) / BM : row_tiles;      // WEIGHT: of one group
+  const int per_weight = tiles_m * g.tiles_n;
+  const int T = DIR == WEIGHT ? per_weight * g.groups : per_weight;
+  const int G = gridDim.x;
+  int wq = blockIdx.x;
+  if ((G & 7) == 0) wq = (wq & 7) * (G >> 3) + (wq >> 3);
+  const int n_my = wq < T ? (T - 1 - wq) / G + 1 : 0;
+  if (n_my == 0) return;
+
+  struct Where {
+    int gr, r0, r1;      // group; FWD, INPUT: first row of the tile; WEIGHT: of the group; end of the group
+    int i0, j0;          // WEIGHT: first row of C; first column
+    int stages;          // an even number
+  };
+  auto locate = [&](int ti) __attribute__((always_inline)) {
+    Where w;
+    int u = ti * G + wq;
+    w.gr = 0;
+    if (DIR == WEIGHT) {
+      w.gr = u / per_weight;
+      u -= w.gr * per_weight;
+    }
+    const int per_group = GROUP * g.tiles_n;
+    const int first_m = (u / per_group) * GROUP;
+    const int gsz = (tiles_m - first_m) < GROUP ? (tiles_m - first_m) : GROUP;
+    const int rt = first_m + (u % per_group) % gsz;
+    w.j0 = ((u % per_group) / gsz) * BN;
+    w.i0 = rt * BM;
+    w.r0 = w.r1 = 0;
+    if (DIR == WEIGHT) {
+#pragma unroll
+      for (int q = 0; q < kTableSets; ++q)
+        if (w.gr >> 6 == q) {
+          w.r0 = __builtin_amdgcn_readlane(tr0[q], w.gr & 63);
+          w.r1 = __builtin_amdgcn_readlane(tr1[q], w.gr & 63);
+        }
+      w.stages = (w.r1 - w.r0 + 63) / 64 * 2;
+    } else {
+      bool found = false;
+#pragma unroll
+      for (int q = 0; q < kTableSets; ++q) {
+        const uint64_t after = __ballot(tsum[q] > rt);      // the sums of lanes without a group repeat the last one's
+        if (!found && 64 * q < g.groups && after) {
+          found = true;
+          const int l = __builtin_ctzll(after);
+          w.gr = 64 * q + l;
+          w.r0 = __builtin_amdgcn_readlane(tr0[q], l);
+          w.r1 = __builtin_amdgcn_readlane(tr1[q], l);
+          const int end = __builtin_amdgcn_readlane(tsum[q], l), mine = (w.r1 - w.r0 + BM - 1) / BM;
+          w.r0 += (rt - (end - mine)) * BM;
+        }
+      }
+      w.stages = (g.K + (FP4 ? 255 : 63)) / (FP4 ? 256 : 64) * 2;
+    }
+    return w;
+  };
+
+  // ---- per-lane byte offsets of the loads, the same for every stage and tile
+  uint32_t voffA[IPWA], voffB[FP4 ? 1 : IPWB], voffS[IPWS ? IPWS : 1];      // FP4: both operands' rows are as long, and the tile square
+  auto slot_offset = [&](int slot, bool kmajor, int width, i64 ld) __attribute__((always_inline)) {
+    if (kmajor) {
+      const int r = slot >> 2, c = dense::xk16_chunk(slot & 3, r);
+      return (uint32_t)(r * ld + c * 16);
+    }
+    const int k = slot / (width / 8), c = dense::kx16_chunk(slot % (width / 8), k);
+    return (uint32_t)(k * ld + c * 16);
+  };
+#pragma unroll
+  for (int s = 0; s < IPWA; ++s) voffA[s] = slot_offset((wave * IPWA + s) * 64 + lane, A_K, BM, g.lda);
+#pragma unroll
+  for (int s = 0; s < (FP4 ? 0 : IPWB); ++s) voffB[s] = slot_offset((wave * IPWB + s) * 64 + lane, B_K, BN, g.ldb);
+  // scales: loads 0 .. BM / 64 - 1 are A's, the others B's
+  auto scale_of_a = [&](int s) __attribute__((always_inline)) { return (wave * IPWS + s) * 64 < BM; };
+#pragma unroll
+  for (int s = 0; s < IPWS; ++s) {
+    const int r = (wave * IPWS + s) * 64 + lane;
+    voffS[s] = (uint32_t)((r < BM ? r : r - BM) * ((r < BM ? g.lda : g.ldb) / 16));
+  }
+  // lanes whose 16 bytes lie past the end of a row in its last, short stage: the chunk a lane fetches is the same in each of its loads
+  const int short_stage = !FP4 && DIR != WEIGHT && g.K % 32 ? g.K / 32 : -1;
+  const uint64_t past_end = __ballot(8 * dense::xk16_chunk(lane & 3, lane >> 2) >= g.K % 32);
+
+  // ---- issue side
+  Feed fa, fb;
+  int iti = -1, ikt = 0, iKT = 0, islot = 0;
+  const i64 stepA = A_K ? 64 : 32 * g.lda, stepB = B_K ? 64 : 32 * g.ldb;
+  auto next_tile = [&]() __attribute__((always_inline)) {
+    Where w;
+    do {
+      ++iti;
+      if (iti >= n_my) break;
+      w = locate(iti);
+    } while (DIR == WEIGHT && w.stages == 0);
+    ikt = 0;
+    if (iti >= n_my) {      // nothing more: empty descriptors
+      fa.left = fb.left = 0;
+      iKT = 0x7fffffff;
+      return;
+    }
+    iKT = w.stages;
+    const int hb = DIR == FWD ? g.N - w.j0 < BN ? g.N - w.j0 : BN : 0;      // rows of W in the tile
+    if (DIR == WEIGHT) {
+      const i64 len = w.r1 - w.r0;
+      fa.at = (uint64_t)(g.A + (i64)w.r0 * g.lda + 2 * w.i0);
+      fa.left = (len - 1) * g.lda + 2 * (i64)(g.M - w.i0);
+      fb.at = (uint64_t)(g.B + (i64)w.r0 * g.ldb + 2 * w.j0);
+      fb.left = (len - 1) * g.ldb + 2 * (i64)(g.N - w.j0);
+    } else {
+      const int ha = w.r1 - w.r0 < BM ? w.r1 - w.r0 : BM;
+      const i64 row = FP4 ? g.K / 2 : 2 * (i64)g.K;      // bytes of a row
+      fa.at = (uint64_t)(g.A + (i64)w.r0 * g.lda);
+      fa.left = (ha - 1) * g.lda + row;
+      if (DIR == FWD) {
+        const i64 first = (i64)w.gr * g.N + w.j0;
+        fb.at = (uint64_t)(g.B + first * g.ldb);
+        fb.left = (hb - 1) * g.ldb + row;
+      } else {
+        fb.at = (uint64_t)(g.B + (i64)w.gr * g.K * g.ldb + 2 * w.j0);
+        fb.left = (i64)(g.K - 1) * g.ldb + 2 * (i64)(g.N - w.j0);
+      }
+    }
+  };
+  const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  u32x4 ra, rb, rsa, rsb;
+  uint64_t masked = 0;
+  auto stage_rsrc = [&]() __attribute__((always_inline)) {
+    const bool on = ikt * (FP4 ? 128 : 32) < g.K;      // not a stage that only evens their number (WEIGHT: has no rows)
+    ra = fa.rsrc(!A_K || on);
+    rb = fb.rsrc(!B_K || on);
+    if (FP4) {
+      // a byte of scales per 16 bytes of codes, in rows as many times shorter
+      rsa = Feed{(uint64_t)g.SA + ((fa.at - (uint64_t)g.A) >> 4), fa.left >> 4}.rsrc(on);
+      rsb = Feed{(uint64_t)g.SB + ((fb.at - (uint64_t)g.B) >> 4), fb.left >> 4}.rsrc(on);
+    } else {
+      masked = ikt == short_stage ? past_end : 0;
+    }
+  };
+  auto masked_off = [&](uint32_t v) __attribute__((always_inline)) {
+    uint32_t o;
+    asm("v_cndmask_b32 %0, %1, %2, %3" : "=v"(o) : "v"(v), "v"(0xfffffff0u), "s"(masked));
+    return o;
+  };
+  auto issue = [&](int i) __attribute__((always_inline)) {      // load i of the stage (a constant wherever this is called)
+    const uint32_t stage = lds_base + islot * STAGE_BYTES;
+    if (i < IPWA) dma16b(ra, !FP4 && A_K ? masked_off(voffA[i]) : voffA[i], stage + (wave * IPWA + i) * 1024);
+    else if (i < IPWA + IPWB) dma16b(rb, FP4 ? voffA[i - IPWA] : B_K ? masked_off(voffB[i - IPWA]) : voffB[i - IPWA], stage + A_BYTES + (wave * IPWB + i - IPWA) * 1024);
+    else {
+      const int s = i - IPWA - IPWB;
+      dma4b(scale_of_a(s) ? rsa : rsb, voffS[s], stage + A_BYTES + C::B_BYTES + (wave * IPWS + s) * 256);
+    }
+  };
+  auto issue_advance = [&]() __attribute__((always_inline)) {
+    islot = islot + 1 == NS ? 0 : islot + 1;
+    ++ikt;
+    fa.step(stepA);
+    fb.step(stepB);
+    stage_rsrc();
+  };
+  // after every second stage: tiles have even numbers of them, and so has the ring
+  static_assert(NS % 2 == 0, "a tile's first stage is issued first of a pair");
+  auto tile_advance = [&]() __attribute__((always_inline)) {
+    if (ikt == iKT) {
+      next_tile();
+      stage_rsrc();
+    }
+  };
+
+  // ---- fragments
+  // K major: the 16-row pieces lie 1024 bytes apart, as their swizzle is the same
+  int fragA[A_K ? 1 : TM], fragB[B_K ? 1 : TN];
+  const int q4 = lane >> 4, li = lane & 15;
+  {
+    const int k = 8 * q4 + (li >> 2);
+    auto frag = [&](int x0, bool kmajor, int width) {
+      if (kmajor) return (x0 + li) * 64 + 16 * dense::xk16_chunk(q4, li);
+      return k * (width * 2) + 16 * dense::kx16_chunk((x0 >> 3) + ((li & 3) >> 1), k) + 8 * (li & 1);
+    };
+#pragma unroll
+    for (int a = 0; a < (A_K ? 1 : TM); ++a) fragA[a] = frag(wm * (BM / 2) + a * 16, A_K, BM);
+#pragma unroll
+    for (int c = 0; c < (B_K ? 1 : TN); ++c) fragB[c] = A_BYTES + frag(wn * (BN / 2) + c * 16, B_K, BN);
+  }
+  const int scaleA = A_BYTES + C::B_BYTES + (wm * (BM / 2) + li) * 4 + q4, scaleB = A_BYTES + C::B_BYTES + (BM + wn * (BN / 2) + li) * 4 + q4;
+  auto load_frag = [&](const char* p, bool kmajor, int row_bytes) -> u32x4 {
+    if (kmajor) return *reinterpret_cast<const u32x4*>(p);
+    const mm::short4v lo = mm::lds_read_tr(p), hi = mm::lds_read_tr(p + 4 * row_bytes);
+    const mm::short8v v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    return __builtin_bit_cast(u32x4, v);
+  };
+  struct Frags {
+    u32x4 a[TM], b[TN];
+    uint32_t sa[FP4 ? TM : 1], sb[FP4 ? TN : 1];
+  };
+  // piece p, in the order the MFMAs first need them: A0 B0 A1 .. A(TM-1) B1 .. B(TN-1)
+  auto load_piece = [&](Frags& f, int slot, int p) __attribute__((always_inline)) {
+    const char* st = lds + slot * STAGE_BYTES;
+    if (p != 1 && p <= TM) {
+      const int a = p ? p - 1 : 0;
+      f.a[a] = load_frag(st + fragA[A_K ? 0 : a] + (A_K ? a * 1024 : 0), A_K, BM * 2);
+      if (FP4) f.sa[FP4 ? a : 0] = *reinterpret_cast<const uint8_t*>(st + scaleA + a * 64);
+    } else {
+      const int b = p == 1 ? 0 : p - TM;
+      f.b[b] = load_frag(st + fragB[B_K ? 0 : b] + (B_K ? b * 1024 : 0), B_K, BN * 2);
+      if (FP4) f.sb[FP4 ? b : 0] = *reinterpret_cast<const uint8_t*>(st + scaleB + b * 64);
+    }
+  };
+
+  floatx4 acc[TM][TN];
+#pragma unroll
+  for (int a = 0; a < TM; ++a)
+#pragma unroll
+    for (int c = 0; c < TN; ++c) acc[a][c] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+  next_tile();
+  stage_rsrc();
+#pragma unroll 1
+  for (int t = 0; t < NS; t += 2) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int i = 0; i < LPT; ++i) issue(i);
+      issue_advance();
+    }
+    tile_advance();
+  }
+  mm::wait_vmcnt_and_barrier<(NS - 1) * LPT>();
+  Frags F, Gf;
+  int cslot = 0;
+#pragma unroll
+  for (int p = 0; p < TM + TN; ++p) load_piece(F, 0, p);
+
+  // once per wave: wave W issues its loads W quarters of the way from one to the next
+  auto run = [&](auto WC) __attribute__((always_inline)) {
+    constexpr int W = decltype(WC)::value;
+    auto multiply = [&](const Frags& X, Frags& Y) __attribute__((always_inline)) {
+      mm::wait_all_reads_and_barrier<(NS - 2) * LPT>();
+      const int nslot = cslot + 1 == NS ? 0 : cslot + 1;
+#pragma unroll
+      for (int i = 0; i < MF; ++i) {
+        if constexpr (FP4) mfma_fp4(acc[i % TM][i / TM], X.b[i / TM], X.a[i % TM], X.sb[i / TM], X.sa[i % TM]);
+        else dense::mfma16(acc[i % TM][i / TM], __builtin_bit_cast(bf16x8, X.b[i / TM]), __builtin_bit_cast(bf16x8, X.a[i % TM]));
+        if (i % RS == 0 && i / RS < TM + TN) load_piece(Y, nslot, i / RS);
+        if (i % DS == W * DS / 4 && i / DS < LPT) issue(i / DS);
+        if (i == MF - 1) issue_advance();
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      cslot = nslot;
+    };
+    for (int ti = 0; ti < n_my; ++ti) {
+      const int KT = locate(ti).stages;
+      for (int kt = 0; kt < KT; kt += 2) {
+        multiply(F, Gf);
+        multiply(Gf, F);
+        tile_advance();
+      }
+      dense::settle(acc);
+      const Where w = locate(ti);
+      // Stores go through a descriptor as well: rows past the group's end (of dW) lie behind it, and a lane whose columns do not exist gets an offset that does.
+      if constexpr (DIR == WEIGHT) {
+        // a lane's four columns of a row
+        const int row = wm * (BM / 2) + li, col = wn * (BN / 2) + 4 * q4;
+        const auto rc = make_rsrc((float*)g.C + (i64)w.gr * g.M * g.N + (i64)w.i0 * g.N + w.j0, ((i64)(g.M - w.i0 - 1) * g.N + g.N - w.j0) * 4);
+        auto store = [&](auto ADD) __attribute__((always_inline)) {
+#pragma unroll
+          for (int a = 0; a < TM; ++a) {
+            const int at = ((row + a * 16) * g.N + col) * 4;
+#pragma unroll
+            for (int c = 0; c < TN; ++c) {
+              const int v = col + c * 16 < g.N - w.j0 ? at + c * 64 : kNowhere;
+              floatx4 x = acc[a][c];
+              acc[a][c] = floatx4{0.f, 0.f, 0.f, 0.f};
+              if constexpr (decltype(ADD)::value) x += __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(rc, v, 0, 0));
+              __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), rc, v, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        };
+        if (g.accumulate) store(std::true_type{});
+        else store(std::false_type{});
+      } else {
+        // through LDS, 16 rows x 64 columns at a time, so that every instruction writes whole 128-byte lines
+        char* stg = lds + NS * STAGE_BYTES + wave * C::OUT_BYTES;
+        const int rows = w.r1 - w.r0, cols = g.N - w.j0;
+        const auto rc = make_rsrc((uint16_t*)g.C + (i64)w.r0 * g.ldc + w.j0, ((i64)(rows - 1) * g.ldc + cols) * 2);
+        const int row = wm * (BM / 2) + (lane >> 3), col = wn * (BN / 2) + (lane & 7) * 8, step = (int)g.ldc * 16;      // 8 rows further down
+        int at[TN / 4];
+#pragma unroll
+        for (int cp = 0; cp < TN / 4; ++cp) at[cp] = (row * (int)g.ldc + col + cp * 64) * 2;
+#pragma unroll
+        for (int a = 0; a < TM; ++a) {
+#pragma unroll
+          for (int c = 0; c < TN; c += 2) {
+            uint32_t o[4];
+            dense::pack_pair(acc[a][c], acc[a][c + 1], o);
+            acc[a][c] = floatx4{0.f, 0.f, 0.f, 0.f};
+            acc[a][c + 1] = floatx4{0.f, 0.f, 0.f, 0.f};
+            const int ch = ((c & 3) + (q4 & 1)) * 2 + (q4 >> 1);
+            *reinterpret_cast<u32x4*>(stg + (c >> 2) * 2048 + li * 128 + 16 * (ch ^ ((li >> 1) & 7))) = u32x4{o[0], o[1], o[2], o[3]};
+          }
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // this wave's own writes; the area is private to it
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int cp = 0; cp < TN / 4; ++cp) {
+              const int r = (lane >> 3) + 8 * i, ch = lane & 7;
+              const u32x4 o = *reinterpret_cast<const u32x4*>(stg + cp * 2048 + r * 128 + 16 * (ch ^ ((r >> 1) & 7)));
+              __builtin_amdgcn_raw_buffer_store_b128(o, rc, col + cp * 64 < cols ? at[cp] : kNowhere, 0, 0);
+              at[cp] += step;
+            }
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // read back before the area is rewritten
+        }
+      }
+    }
+  };
+  switch (wave) {
+    case 0: run(std::integral_constant<int, 0>{}); break;
+    case 1: run(std::integral_constant<int, 1>{}); break;
+    case 2: run(std::integral_constant<int, 2>{}); break;
+    default: run(std::integral_constant<int, 3>{}); break;
+  }
+  mm::wait_vmcnt_and_barrier<0>();      // the last loads land before the LDS is released
+}
+
+}  // namespace grouped
+}  // namespace poetx
