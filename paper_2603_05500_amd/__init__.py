@@ -158,9 +158,15 @@ def _check(status: int, where: str):
         raise PoetxError(status, where)
 
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def _ptr(t):
@@ -170,18 +176,32 @@ def _ptr(t):
     return c_void_p(t.data_ptr())
 
 
-def _rows_ptr(t):
-    """A matrix whose rows may be further apart than they are long."""
-    assert t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1 or t.shape[0] == 0), "device-resident matrices with contiguous rows only"
-    return c_void_p(t.data_ptr())
+def _matrix(t, dtype, shape):
+    """Pointer and leading dimension of a matrix whose rows may be further apart than they are long."""
+    assert t.is_cuda and t.dtype is dtype and t.shape == shape, "a device-resident matrix of another type or shape"
+    ld, step = t.stride()
+    assert step == 1 or shape[1] == 1 or shape[0] == 0, "the elements of a row have to be contiguous"
+    return t.data_ptr(), ld if shape[0] > 1 else max(ld, shape[1])
 
 
-def _ld(t):
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+def _buffer(t, nbytes):
+    assert t.is_cuda and t.is_contiguous() and t.numel() * t.element_size() >= nbytes, "a device-resident buffer, large enough"
+    return t.data_ptr()
+
+
+def _vector(t, n):
+    assert t.is_cuda and t.is_contiguous() and t.dtype is _torch().int32 and t.numel() == n, "device-resident int32, as many as the call takes"
+    return t.data_ptr()
+
+
+def _scratch(ws):
+    return (None, 0) if ws is None else (_ptr(ws), _ws_bytes(ws))
 
 
 def _stream():
-    return c_void_p(_torch().cuda.current_stream().cuda_stream)
+    """The current HIP stream's handle (torch.cuda.current_stream().cuda_stream without building a Stream object: 3 us of a call)."""
+    C = _torch()._C
+    return C._cuda_getCurrentRawStream(C._cuda_getDevice())
 
 
 def dtype_code(t) -> int:
@@ -362,16 +382,17 @@ def poetx_mx4_bytes(rows: int, cols: int) -> int:
 
 def poetx_mx4_quantize(X, Q):
     """X: rows x cols (f32 or bf16, rows may be strided) -> Q: uint8 buffer of poetx_mx4_bytes(rows, cols) bytes."""
-    rows, cols = X.shape
-    assert _ws_bytes(Q) >= poetx_mx4_bytes(rows, cols), "4-bit buffer too small"
-    _check(load_library().poetx_mx4_quantize(_rows_ptr(X), dtype_code(X), rows, cols, _ld(X), _ptr(Q), _stream()), "poetx_mx4_quantize")
+    lib, shape = load_library(), X.shape
+    rows, cols = shape
+    x, ld = _matrix(X, X.dtype, shape)
+    _check(lib.poetx_mx4_quantize(x, dtype_code(X), rows, cols, ld, _buffer(Q, lib.poetx_mx4_bytes(rows, cols)), _stream()), "poetx_mx4_quantize")
 
 
 def poetx_mx4_dequantize(Q, out):
-    rows, cols = out.shape
-    assert _ws_bytes(Q) >= poetx_mx4_bytes(rows, cols), "4-bit buffer too small"
-    _check(load_library().poetx_mx4_dequantize(_ptr(Q), rows, cols, dtype_code(out), _rows_ptr(out), _ld(out), _stream()),
-           "poetx_mx4_dequantize")
+    lib, shape = load_library(), out.shape
+    rows, cols = shape
+    o, ld = _matrix(out, out.dtype, shape)
+    _check(lib.poetx_mx4_dequantize(_buffer(Q, lib.poetx_mx4_bytes(rows, cols)), rows, cols, dtype_code(out), o, ld, _stream()), "poetx_mx4_dequantize")
 
 
 def make_grouped_desc(d_in, d_out, groups, rows, dtype, flags=0) -> GroupedDesc:
@@ -382,43 +403,41 @@ def poetx_grouped_workspace_bytes(desc: GroupedDesc) -> int:
     return load_library().poetx_grouped_workspace_bytes(ctypes.byref(desc))
 
 
-def _grouped_check(desc, W, offsets, *tensors):
-    """The tensors are those the descriptor speaks of: the library sees pointers only."""
-    torch = _torch()
-    dt = torch.float32 if desc.dtype == F32 else torch.bfloat16
-    for t, d in tensors:
-        assert t.dtype == dt and t.dim() == 2 and t.shape[0] == desc.rows and t.shape[1] == d, "a tensor is not the descriptor's"
-    assert offsets.dtype == torch.int32 and offsets.numel() == desc.groups + 1, "offsets: groups + 1 int32"
-    if W is None:
-        return
+def _grouped_type(desc):
+    return _torch().float32 if desc.dtype == F32 else _torch().bfloat16
+
+
+def _grouped_weight(lib, desc, W):
     if desc.flags & GROUPED_W_MX4:
-        assert _ws_bytes(W) >= poetx_mx4_bytes(desc.groups * desc.d_out, desc.d_in), "4-bit weight buffer too small"
-    else:
-        assert W.dtype == dt and W.numel() == desc.groups * desc.d_out * desc.d_in, "W: groups x d_out x d_in"
+        return _buffer(W, lib.poetx_mx4_bytes(desc.groups * desc.d_out, desc.d_in))
+    assert W.dtype is _grouped_type(desc) and W.is_contiguous() and W.is_cuda and W.numel() == desc.groups * desc.d_out * desc.d_in, "W: groups x d_out x d_in"
+    return W.data_ptr()
+
+
+def _grouped_rows(name, desc, A, d_a, W, offsets, C, d_c, ws):
+    lib, rows, dt = load_library(), desc.rows, _grouped_type(desc)
+    a, lda = _matrix(A, dt, (rows, d_a))
+    c, ldc = _matrix(C, dt, (rows, d_c))
+    _check(getattr(lib, name)(ctypes.byref(desc), a, lda, _grouped_weight(lib, desc, W), _vector(offsets, desc.groups + 1), c, ldc, *_scratch(ws), _stream()), name)
 
 
 def poetx_grouped_fwd(desc, X, W, offsets, Z, ws=None):
     """Z: rows x d_out = each row of X (rows x d_in) times its group's weight, transposed.  Rows of X and Z may be strided."""
-    _grouped_check(desc, W, offsets, (X, desc.d_in), (Z, desc.d_out))
-    _check(load_library().poetx_grouped_fwd(ctypes.byref(desc), _rows_ptr(X), _ld(X), _ptr(W), _ptr(offsets), _rows_ptr(Z), _ld(Z), _ptr(ws),
-                                            _ws_bytes(ws) if ws is not None else 0, _stream()),
-           "poetx_grouped_fwd")
+    _grouped_rows("poetx_grouped_fwd", desc, X, desc.d_in, W, offsets, Z, desc.d_out, ws)
 
 
 def poetx_grouped_bwd_input(desc, dZ, W, offsets, dX, ws=None):
-    _grouped_check(desc, W, offsets, (dZ, desc.d_out), (dX, desc.d_in))
-    _check(load_library().poetx_grouped_bwd_input(ctypes.byref(desc), _rows_ptr(dZ), _ld(dZ), _ptr(W), _ptr(offsets), _rows_ptr(dX), _ld(dX),
-                                                  _ptr(ws), _ws_bytes(ws) if ws is not None else 0, _stream()),
-           "poetx_grouped_bwd_input")
+    _grouped_rows("poetx_grouped_bwd_input", desc, dZ, desc.d_out, W, offsets, dX, desc.d_in, ws)
 
 
 def poetx_grouped_bwd_weight(desc, X, dZ, offsets, dW, accumulate, ws=None):
     """dW: groups x d_out x d_in float32."""
-    _grouped_check(desc, None, offsets, (X, desc.d_in), (dZ, desc.d_out))
-    assert dW.dtype == _torch().float32 and dW.numel() == desc.groups * desc.d_out * desc.d_in, "dW: groups x d_out x d_in float32"
-    _check(load_library().poetx_grouped_bwd_weight(ctypes.byref(desc), _rows_ptr(X), _ld(X), _rows_ptr(dZ), _ld(dZ), _ptr(offsets), _ptr(dW),
-                                                   int(bool(accumulate)), _ptr(ws), _ws_bytes(ws) if ws is not None else 0, _stream()),
-           "poetx_grouped_bwd_weight")
+    lib, dt = load_library(), _grouped_type(desc)
+    x, ldx = _matrix(X, dt, (desc.rows, desc.d_in))
+    dz, lddz = _matrix(dZ, dt, (desc.rows, desc.d_out))
+    assert dW.dtype is _torch().float32 and dW.numel() == desc.groups * desc.d_out * desc.d_in, "dW: groups x d_out x d_in float32"
+    _check(lib.poetx_grouped_bwd_weight(ctypes.byref(desc), x, ldx, dz, lddz, _vector(offsets, desc.groups + 1), _ptr(dW), int(bool(accumulate)),
+                                        *_scratch(ws), _stream()), "poetx_grouped_bwd_weight")
 
 
 def poetx_group_order_workspace_bytes(n: int, groups: int) -> int:
@@ -427,8 +446,6 @@ def poetx_group_order_workspace_bytes(n: int, groups: int) -> int:
 
 def poetx_group_order(ids, offsets, order, ws=None):
     """ids: n int32 group numbers -> offsets: groups + 1 int32, order: n int32 (rows group by group, -1 past the last)."""
-    torch = _torch()
-    assert ids.dtype == offsets.dtype == order.dtype == torch.int32 and order.numel() == ids.numel(), "int32 ids, offsets and order"
-    _check(load_library().poetx_group_order(_ptr(ids), ids.numel(), offsets.numel() - 1, _ptr(offsets), _ptr(order), _ptr(ws),
-                                            _ws_bytes(ws) if ws is not None else 0, _stream()),
-           "poetx_group_order")
+    n = ids.numel()
+    _check(load_library().poetx_group_order(_vector(ids, n), n, offsets.numel() - 1, _vector(offsets, offsets.numel()), _vector(order, n),
+                                            *_scratch(ws), _stream()), "poetx_group_order")

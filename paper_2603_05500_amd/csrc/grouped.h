@@ -92,14 +92,26 @@ __device__ __forceinline__ int xcd_run(int bx, int total) {
   return xcd * per + (xcd < extra ? xcd : extra) + (bx >> 3);
 }
 
+// ---- which kernel ------------------------------------------------------------------------------------
+enum Kernel { EDGE_32, EDGE_32_DEEP, EDGE_64, EDGE_128, STREAM_256, STREAM_256x128, STREAM_128, KERNELS };
+// What a kernel takes for a call, in us, from what one stage of its tile's contraction takes alone and how many tiles the chip works on at a time.
+Kernel plan(int dtype, Dir dir, const Call& c, bool streams);
+
 // ---- launchers -----------------------------------------------------------------------------------
-void edge_launch(int dtype, Dir dir, const Call& c, hipStream_t st);      // any shape (grouped_edge.hip)
+void edge_launch(int dtype, Dir dir, Kernel k, const Call& c, hipStream_t st);      // any shape (grouped_edge.hip)
 // bf16 in whole 16-byte vectors (grouped_stream.hip)
 bool stream_supported(Dir dir, const Call& c);
-void stream_launch(Dir dir, const Call& c, hipStream_t st);
+void stream_launch(Dir dir, Kernel k, const Call& c, hipStream_t st);
 // Z = X W^T on 4-bit buffers of both
 bool codes_supported(const poetx_grouped_desc* d, const void* Z, i64 ldz);
 void codes_launch(const poetx_grouped_desc* d, const void* Xq, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, hipStream_t st);
+
+// the forward of a handful of rows per group, bf16 (grouped_few.hip): any sizes, strides and alignments
+enum Weight { DENSE_BF16, VALUES_MX4, CODES_MX4 };      // CODES: of X as well
+bool few_supported(int dtype, Dir dir, i64 rows, int groups, Weight w);
+void few_dense(const Call& c, hipStream_t st);
+void few_values(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, hipStream_t st);      // 4-bit weight
+void few_codes(const poetx_grouped_desc* d, const void* Xq, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, hipStream_t st);               // 4-bit rows too
 
 }  // namespace grouped
 }  // namespace poetx

@@ -61,8 +61,9 @@ const void* dense_weight(const poetx_grouped_desc* d, const void* W, void* ws, h
 
 void product(int dtype, grouped::Dir dir, const grouped::Call& c, hipStream_t st) {
   StageTimer tm(POETX_STAGE_DENSE, st);
-  if (dtype == POETX_BF16 && grouped::stream_supported(dir, c)) grouped::stream_launch(dir, c, st);
-  else grouped::edge_launch(dtype, dir, c, st);
+  if (grouped::few_supported(dtype, dir, c.rows, c.groups, grouped::DENSE_BF16)) return grouped::few_dense(c, st);
+  const grouped::Kernel k = grouped::plan(dtype, dir, c, dtype == POETX_BF16 && grouped::stream_supported(dir, c));
+  k >= grouped::STREAM_256 ? grouped::stream_launch(dir, k, c, st) : grouped::edge_launch(dtype, dir, k, c, st);
 }
 
 // Forward and input gradient: in is rows x d_i, out rows x d_o.
@@ -74,6 +75,7 @@ int check_rows_call(const poetx_grouped_desc* d, const void* in, i64 ld_in, int 
   if (ld_in < d_i || ld_out < d_o) return POETX_ERR_BAD_SHAPE;
   if (d->rows > 0 && (ld_in >= kMostElements / d->rows || ld_out >= kMostElements / d->rows)) return POETX_ERR_UNSUPPORTED;
   const size_t es = esize(d->dtype), ob = span(d->rows, d_o, ld_out, es);
+  if ((d->flags & POETX_GROUPED_W_MX4) && ((uintptr_t)W & 15)) return POETX_ERR_INVALID_ARG;
   if (overlap(out, ob, in, span(d->rows, d_i, ld_in, es)) || overlap(out, ob, W, weight_bytes(d)) || overlap(out, ob, offsets, 4 * ((size_t)d->groups + 1)))
     return POETX_ERR_INVALID_ARG;
   const size_t need = workspace_bytes(d);
@@ -115,13 +117,20 @@ int poetx_grouped_fwd(const poetx_grouped_desc* d, const void* X, int64_t ldx, c
   const int rc = check_rows_call(d, X, ldx, d ? d->d_in : 0, W, offsets, Z, ldz, d ? d->d_out : 0, ws, ws_bytes);
   if (rc != POETX_OK || d->rows == 0) return rc;
   hipStream_t st = (hipStream_t)stream;
-  if ((d->flags & POETX_GROUPED_X_MX4) && grouped::codes_supported(d, Z, ldz)) {
+  const bool mx4 = d->flags & POETX_GROUPED_W_MX4, both = d->flags & POETX_GROUPED_X_MX4;
+  const bool few = mx4 && grouped::few_supported(d->dtype, grouped::FWD, d->rows, d->groups, both ? grouped::CODES_MX4 : grouped::VALUES_MX4);
+  if (both && (few || grouped::codes_supported(d, Z, ldz))) {
     {
       StageTimer tm(POETX_STAGE_DEQUANT, st);
       mx4_quantize_launch(POETX_BF16, X, d->rows, d->d_in, ldx, ws, st);
     }
     StageTimer tm(POETX_STAGE_DENSE, st);
-    grouped::codes_launch(d, ws, W, offsets, Z, ldz, st);
+    few ? grouped::few_codes(d, ws, W, offsets, Z, ldz, st) : grouped::codes_launch(d, ws, W, offsets, Z, ldz, st);
+    return launch_status();
+  }
+  if (few) {
+    StageTimer tm(POETX_STAGE_DENSE, st);
+    grouped::few_values(d, X, ldx, W, offsets, Z, ldz, st);
     return launch_status();
   }
   const void* w = dense_weight(d, W, ws, st);

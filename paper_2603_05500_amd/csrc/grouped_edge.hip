@@ -74,26 +74,23 @@ void launch_tile(const Call& c, hipStream_t st) {
   });
 }
 
-// Tile: as many rows as an average group has, as long as the chip is full.
 template <class T, class O, Dir DIR, bool ADD>
-void launch_dir(const Call& c, hipStream_t st) {
+void launch_dir(Kernel k, const Call& c, hipStream_t st) {
   constexpr int D = 128 / (int)sizeof(T);
-  const i64 cols = DIR == FWD ? c.n : c.m;
-  const i64 height = DIR == WEIGHT ? c.n : c.rows / c.groups, all = DIR == WEIGHT ? (i64)c.groups * c.n : c.rows;
-  auto tiles = [&](int t) { return (all + t - 1) / t * ((cols + t - 1) / t); };
-  if (height > 64 && tiles(128) >= 256) launch_tile<T, O, 128, D, 2, 4, DIR, ADD>(c, st);
-  else if (height > 32 && tiles(64) >= 256) launch_tile<T, O, 64, D, 2, 4, DIR, ADD>(c, st);
-  else launch_tile<T, O, 32, 2 * D, 1, 4, DIR, ADD>(c, st);
+  if (k == EDGE_128) launch_tile<T, O, 128, D, 2, 4, DIR, ADD>(c, st);
+  else if (k == EDGE_64) launch_tile<T, O, 64, D, 2, 4, DIR, ADD>(c, st);
+  else if (k == EDGE_32) launch_tile<T, O, 32, 2 * D, 1, 4, DIR, ADD>(c, st);
+  else launch_tile<T, O, 32, 8 * D, 1, 16, DIR, ADD>(c, st);
 }
 
 }  // namespace
 
-void edge_launch(int dtype, Dir dir, const Call& c, hipStream_t st) {
+void edge_launch(int dtype, Dir dir, Kernel k, const Call& c, hipStream_t st) {
   const bool f = dtype == POETX_F32;
-  if (dir == FWD) f ? launch_dir<float, float, FWD, false>(c, st) : launch_dir<uint16_t, uint16_t, FWD, false>(c, st);
-  else if (dir == INPUT) f ? launch_dir<float, float, INPUT, false>(c, st) : launch_dir<uint16_t, uint16_t, INPUT, false>(c, st);
-  else if (c.accumulate) f ? launch_dir<float, float, WEIGHT, true>(c, st) : launch_dir<uint16_t, float, WEIGHT, true>(c, st);
-  else f ? launch_dir<float, float, WEIGHT, false>(c, st) : launch_dir<uint16_t, float, WEIGHT, false>(c, st);
+  if (dir == FWD) f ? launch_dir<float, float, FWD, false>(k, c, st) : launch_dir<uint16_t, uint16_t, FWD, false>(k, c, st);
+  else if (dir == INPUT) f ? launch_dir<float, float, INPUT, false>(k, c, st) : launch_dir<uint16_t, uint16_t, INPUT, false>(k, c, st);
+  else if (c.accumulate) f ? launch_dir<float, float, WEIGHT, true>(k, c, st) : launch_dir<uint16_t, float, WEIGHT, true>(k, c, st);
+  else f ? launch_dir<float, float, WEIGHT, false>(k, c, st) : launch_dir<uint16_t, float, WEIGHT, false>(k, c, st);
 }
 
 }  // namespace grouped

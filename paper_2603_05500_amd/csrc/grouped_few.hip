@@ -1,0 +1,230 @@
+// Forward products where groups have a handful of rows each (generation; a router's many experts): Z = X W_g^T as one read of the weights.
+//
+// What bounds it: the bytes of the weights.  A wave streams 16 RT rows of a weight straight into registers, all loads of a step in flight at once, as
+// the first operand of 16 x 16 MFMAs whose second one is up to 16 NT rows of X; the waves of a workgroup split the contraction and meet in LDS.
+// A lane's load is 16 bytes of one weight row, whatever they hold:
+//   DENSE   8 bf16, one MFMA of depth 32
+//   VALUES  32 codes with their scale, decoded in registers: four MFMAs of depth 32, in which the four groups of 16 lanes hold four different blocks of 32
+//           (the order of a contraction is free as long as both operands keep it)
+//   CODES   32 codes, and 32 of X: one scaled MFMA of depth 128
+#include "edge_gemm.h"
+#include "grouped.h"
+#include "mx4.h"
+
+namespace poetx {
+namespace grouped {
+namespace {
+
+using edge::load16;
+using edge::u32x4;
+using mm::bf16x8;
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef int intx8 __attribute__((ext_vector_type(8)));
+
+enum Kind { DENSE, VALUES, CODES };
+
+struct FewArgs {
+  const void* X;            // bf16 rows; CODES: codes
+  const uint8_t* xs;        // CODES: scales
+  const void* W;            // bf16 rows of m; else codes
+  const uint8_t* ws;
+  uint16_t* Z;
+  i64 ldx, ldz;             // elements; CODES: ldx is the bytes of a row of codes
+  const int32_t* offsets;
+  i64 rows;
+  int m, n, groups, units, tiles_n;
+};
+
+template <int RT, int NT, int NW, Kind KIND, int U>
+__global__ __launch_bounds__(64 * NW) void grouped_few_kernel(FewArgs a, int first) {
+  __shared__ float part[NW][RT * NT * 256];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int x = lane & 15, q = lane >> 4;
+  const int bx = first + (int)blockIdx.x;
+  const int rt_no = bx / a.tiles_n, n0 = bx % a.tiles_n * (16 * RT);
+  RowTile t;
+  if (a.groups == 1) {
+    const Range r = group_range(a.offsets, 0, a.rows);
+    t = RowTile{0, r.r0 + rt_no * (16 * NT), r.r1};
+  } else {
+    t = find_row_tile(a.offsets, a.groups, a.rows, 16 * NT, rt_no);
+  }
+  const int rows = t.r1 - t.r0;      // 0 where there are fewer tiles
+  if (rows <= 0) return;
+
+  const int s0 = a.units * wave / NW, s1 = a.units * (wave + 1) / NW;
+  // a row past the tile's end (of the weight) is some other one: what it gives goes nowhere
+  i64 wrow[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    const int row = n0 + 16 * r + x;
+    wrow[r] = (i64)t.g * a.n + (row < a.n ? row : a.n - 1);
+  }
+  i64 xrow[NT];
+#pragma unroll
+  for (int c = 0; c < NT; ++c) xrow[c] = t.r0 + (16 * c + x < rows ? 16 * c + x : 0);
+
+  floatx4 acc[RT][NT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int c = 0; c < NT; ++c) acc[r][c] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+  auto steps = [&](int s, auto N_, auto WHOLE_) __attribute__((always_inline)) {      // that many units of 128, their loads in flight together; WHOLE: inside the rows
+    constexpr int N = decltype(N_)::value;
+    constexpr bool WHOLE = decltype(WHOLE_)::value;
+    auto values = [&](const uint16_t* row, int k) __attribute__((always_inline)) { return WHOLE ? load16(row + k) : edge::load_branched(row, k, a.m, true); };
+    if constexpr (KIND == DENSE) {
+      u32x4 fw[N][4][RT], fx[N][4][NT];
+#pragma unroll
+      for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const int k = (s + u) * 128 + 32 * p + 8 * q;
+#pragma unroll
+          for (int r = 0; r < RT; ++r) fw[u][p][r] = values((const uint16_t*)a.W + wrow[r] * a.m, k);
+#pragma unroll
+          for (int c = 0; c < NT; ++c) fx[u][p][c] = values((const uint16_t*)a.X + xrow[c] * a.ldx, k);
+        }
+#pragma unroll
+      for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+#pragma unroll
+          for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int c = 0; c < NT; ++c)
+              acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fw[u][p][r]), __builtin_bit_cast(bf16x8, fx[u][p][c]), acc[r][c], 0, 0, 0);
+    } else {
+      u32x4 fw[N][RT];
+      uint32_t sw[N][RT];
+      // a row's scales of N units, of which a lane takes one byte each; four units' words are one load
+      auto scales = [&](const uint8_t* p, auto put) __attribute__((always_inline)) {
+        if constexpr (N == 4) {
+          const u32x4 v = load16((const float*)p);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) put(u, (v[u] >> (8 * q)) & 255);
+        } else {
+#pragma unroll
+          for (int u = 0; u < N; ++u) put(u, p[4 * u + q]);
+        }
+      };
+#pragma unroll
+      for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          fw[u][r] = *reinterpret_cast<const u32x4*>((const uint8_t*)a.W + ((wrow[r] * a.units + s + u) * 4 + q) * 16);
+        }
+#pragma unroll
+      for (int r = 0; r < RT; ++r) scales(a.ws + (wrow[r] * a.units + s) * 4, [&](int u, uint32_t b) { sw[u][r] = b; });
+      if constexpr (KIND == VALUES) {
+        u32x4 fx[N][4][NT];
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+#pragma unroll
+          for (int p = 0; p < 4; ++p)
+#pragma unroll
+            for (int c = 0; c < NT; ++c) fx[u][p][c] = values((const uint16_t*)a.X + xrow[c] * a.ldx, (s + u) * 128 + 32 * q + 8 * p);
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+#pragma unroll
+          for (int r = 0; r < RT; ++r) {
+            const float sc = mx4::scale_of(sw[u][r]);
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+              const bf16x8 w = __builtin_bit_cast(bf16x8, mx4::to_bf16(fw[u][r][p], sc));
+#pragma unroll
+              for (int c = 0; c < NT; ++c) acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf16x8, fx[u][p][c]), acc[r][c], 0, 0, 0);
+            }
+          }
+      } else {
+        u32x4 fx[N][NT];
+        uint32_t sx[N][NT];
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+#pragma unroll
+          for (int c = 0; c < NT; ++c) fx[u][c] = *reinterpret_cast<const u32x4*>((const uint8_t*)a.X + ((xrow[c] * a.units + s + u) * 4 + q) * 16);
+#pragma unroll
+        for (int c = 0; c < NT; ++c) scales(a.xs + (xrow[c] * a.units + s) * 4, [&](int u, uint32_t b) { sx[u][c] = b; });
+        auto wide = [](const u32x4& v) { return intx8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0}; };
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+#pragma unroll
+          for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int c = 0; c < NT; ++c)
+              acc[r][c] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(fw[u][r]), wide(fx[u][c]), acc[r][c], 4, 4, 0, (int)sw[u][r], 0, (int)sx[u][c]);
+      }
+    }
+  };
+  const int whole = KIND == CODES ? a.units : a.m / 128;
+  int s = s0;
+  for (; s + U <= s1 && s + U <= whole; s += U) steps(s, std::integral_constant<int, U>{}, std::true_type{});
+  for (; s < s1 && s < whole; ++s) steps(s, std::integral_constant<int, 1>{}, std::true_type{});
+  if constexpr (KIND != CODES) {
+    if (s < s1) steps(s, std::integral_constant<int, 1>{}, std::false_type{});      // the last, short unit
+  }
+
+  // lane (row x of the tile, q), register e: weight row 4 q + e
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int c = 0; c < NT; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) part[wave][((16 * c + x) * RT + r) * 16 + 4 * q + e] = acc[r][c][e];
+  __syncthreads();
+  for (int i = tid; i < RT * NT * 256; i += 64 * NW) {
+    const int row = i / (16 * RT), col = n0 + i % (16 * RT);
+    float y = 0.f;
+#pragma unroll
+    for (int z = 0; z < NW; ++z) y += part[z][i];
+    if (row < rows && col < a.n) a.Z[(t.r0 + row) * a.ldz + col] = (uint16_t)mm::pack2_bf16(y, 0.f);
+  }
+}
+
+template <int RT, int NT, int NW, Kind KIND, int U>
+void go(FewArgs a, hipStream_t st) {
+  a.tiles_n = ceil_div(a.n, 16 * RT);
+  const i64 total = (a.groups == 1 ? (a.rows + 16 * NT - 1) / (16 * NT) : most_row_tiles(a.rows, a.groups, 16 * NT)) * a.tiles_n;
+  launch_in_rows(total, [&](int first, unsigned count) {
+    hipLaunchKernelGGL((grouped_few_kernel<RT, NT, NW, KIND, U>), dim3(count), dim3(64 * NW), 0, st, a, first);
+  });
+}
+
+// Rows of X per tile: as many as an average group has; weight rows per wave: more where there are workgroups enough, as each reads its rows of X anew.
+// us, by (weight rows, rows of X, waves, units in flight), weights from memory:
+//   4 bits:  4096 x 4096, 1 row (16,16,4,4) 4.1  (32,16,4,4) 6.0; 16 rows 6.8, 8.2; 14336 x 4096, 1 row (16,16,4,4) 11.2  (32,16,4,4) 9.9  (64,16,8,4) 11.0; 16 rows 21.6, 14.6, 12.5;
+//            eight of 64 experts of 1376 x 2048 a row each 5.8, 6.1, 7.4; all of them with 8 each 45.6, 32.6, 35.8; 14336 x 4096, 32 rows (64,32,4,1) 18.6  (64,64,4,1) 22.7
+//   bf16:    14336 x 4096, 1 row (16,16,4,4) 23.2  (64,16,4,2) 24.9; 16 rows 35.3, 27.2; the experts 10.2, 11.4; with 8 rows each 81.0, 75.6
+template <Kind KIND>
+void pick(const FewArgs& a, hipStream_t st) {
+  const i64 live = a.rows < a.groups ? a.rows : a.groups, mean = (a.rows + live - 1) / live, tiles = live * ((a.n + 15) / 16);
+  if (mean > 32) go<4, 4, 4, KIND, 1>(a, st);
+  else if (mean > 16) go<4, 2, 4, KIND, 1>(a, st);
+  else if (KIND == DENSE) tiles <= 1024 && mean <= 8 ? go<1, 1, 4, KIND, 4>(a, st) : go<4, 1, 4, KIND, 2>(a, st);
+  else if (tiles <= 768) go<1, 1, 4, KIND, 4>(a, st);
+  else if (mean <= 8) go<2, 1, 4, KIND, 4>(a, st);
+  else go<4, 1, 8, KIND, 4>(a, st);
+}
+
+}  // namespace
+
+bool few_supported(int dtype, Dir dir, i64 rows, int groups, Weight w) {
+  i64 most = w == VALUES_MX4 ? 128 : 16;
+  return dtype == POETX_BF16 && dir == FWD && rows <= most * groups;
+}
+void few_dense(const Call& c, hipStream_t st) {
+  pick<DENSE>(FewArgs{c.in, nullptr, c.w, nullptr, (uint16_t*)c.out, c.ld_in, c.ld_out, c.offsets, c.rows, c.m, c.n, c.groups, (c.m + 127) / 128, 0}, st);
+}
+void few_values(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, hipStream_t st) {
+  const mx4::View w = mx4::view(Wq, (i64)d->groups * d->d_out, d->d_in);
+  pick<VALUES>(FewArgs{X, nullptr, w.codes, w.scales, (uint16_t*)Z, ldx, ldz, offsets, d->rows, d->d_in, d->d_out, d->groups, mx4::units(d->d_in), 0}, st);
+}
+void few_codes(const poetx_grouped_desc* d, const void* Xq, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, hipStream_t st) {
+  const mx4::View w = mx4::view(Wq, (i64)d->groups * d->d_out, d->d_in), x = mx4::view(Xq, d->rows, d->d_in);
+  pick<CODES>(FewArgs{x.codes, x.scales, w.codes, w.scales, (uint16_t*)Z, 0, ldz, offsets, d->rows, d->d_in, d->d_out, d->groups, mx4::units(d->d_in), 0}, st);
+}
+
+}  // namespace grouped
+}  // namespace poetx
