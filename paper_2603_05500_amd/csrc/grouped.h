@@ -102,9 +102,10 @@ void edge_launch(int dtype, Dir dir, Kernel k, const Call& c, hipStream_t st);  
 // bf16 in whole 16-byte vectors (grouped_stream.hip)
 bool stream_supported(Dir dir, const Call& c);
 void stream_launch(Dir dir, Kernel k, const Call& c, hipStream_t st);
-// Z = X W^T on 4-bit buffers of both
+// Z = X W^T with X rounded to four bits on the way, W a 4-bit buffer
 bool codes_supported(const poetx_grouped_desc* d, const void* Z, i64 ldz);
-void codes_launch(const poetx_grouped_desc* d, const void* Xq, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, hipStream_t st);
+size_t codes_workspace_bytes(const poetx_grouped_desc* d);
+void codes_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, void* ws, hipStream_t st);
 
 // the forward of a handful of rows per group, bf16 (grouped_few.hip): any sizes, strides and alignments
 enum Weight { DENSE_BF16, VALUES_MX4, CODES_MX4 };      // CODES: of X as well

@@ -48,7 +48,9 @@ size_t rounded_bytes(const poetx_grouped_desc* d) { return align256((size_t)d->r
 
 size_t workspace_bytes(const poetx_grouped_desc* d) {
   if (!(d->flags & POETX_GROUPED_W_MX4) || d->rows == 0) return 0;
-  return dequantised_bytes(d) + (d->flags & POETX_GROUPED_X_MX4 ? rounded_bytes(d) : 0);
+  if (!(d->flags & POETX_GROUPED_X_MX4)) return dequantised_bytes(d);
+  const size_t codes = grouped::codes_workspace_bytes(d), values = dequantised_bytes(d) + rounded_bytes(d);
+  return codes > values ? codes : values;
 }
 
 // The products of a 4-bit weight run on its values, made in the workspace.
@@ -119,13 +121,17 @@ int poetx_grouped_fwd(const poetx_grouped_desc* d, const void* X, int64_t ldx, c
   hipStream_t st = (hipStream_t)stream;
   const bool mx4 = d->flags & POETX_GROUPED_W_MX4, both = d->flags & POETX_GROUPED_X_MX4;
   const bool few = mx4 && grouped::few_supported(d->dtype, grouped::FWD, d->rows, d->groups, both ? grouped::CODES_MX4 : grouped::VALUES_MX4);
-  if (both && (few || grouped::codes_supported(d, Z, ldz))) {
+  if (both && few) {
     {
       StageTimer tm(POETX_STAGE_DEQUANT, st);
       mx4_quantize_launch(POETX_BF16, X, d->rows, d->d_in, ldx, ws, st);
     }
     StageTimer tm(POETX_STAGE_DENSE, st);
-    few ? grouped::few_codes(d, ws, W, offsets, Z, ldz, st) : grouped::codes_launch(d, ws, W, offsets, Z, ldz, st);
+    grouped::few_codes(d, ws, W, offsets, Z, ldz, st);
+    return launch_status();
+  }
+  if (both && grouped::codes_supported(d, Z, ldz)) {
+    grouped::codes_launch(d, X, ldx, W, offsets, Z, ldz, ws, st);
     return launch_status();
   }
   if (few) {

@@ -15,6 +15,8 @@
 //  - FP4: a stage is 64 bytes of a row either way, 32 bf16 or 128 codes with a word of four scales, and an MFMA of 16 x 16 x 128 codes takes as long
 //    as one of 16 x 16 x 32 bf16: the same stream carries four times the products.
 #pragma once
+#include <utility>
+
 #include "grouped.h"
 #include "mfma_dense_kernel.h"
 #include "mx4.h"
@@ -32,7 +34,7 @@ template <int BM_, int BN_, int NS_, bool FP4_>
 struct StreamTile {
   static constexpr int BM = BM_, BN = BN_, NS = NS_, NW = 4;
   static constexpr bool FP4 = FP4_;
-  static constexpr int SETS = FP4 ? 2 : 4, GROUPS = 64 * SETS;      // groups per lane (codes leave fewer registers), in all
+  static constexpr int SETS = 4, GROUPS = 64 * SETS;      // groups per lane, in all
   static constexpr int A_BYTES = BM * 64, B_BYTES = BN * 64, S_BYTES = FP4 ? (BM + BN) * 4 : 0, STAGE_BYTES = A_BYTES + B_BYTES + S_BYTES;
   static constexpr int TM = BM / 32, TN = BN / 32, MF = TM * TN;
   static constexpr int RS = MF / (TM + TN) < 3 ? MF / (TM + TN) : 3;
@@ -48,13 +50,13 @@ struct StreamTile {
 struct StreamArgs {
   const char* A;          // FWD, INPUT: rows of X or dZ; WEIGHT: dZ.  FP4: codes
   const char* B;          // W, or X (WEIGHT).  FP4: codes
-  const uint8_t* SA;      // FP4: scales
-  const uint8_t* SB;
+  const uint32_t* SA;     // FP4: scales, ordered as in mx4.h
+  const uint32_t* SB;
+  int sa_step, sb_step;   // bytes from unit to unit
   void* C;
-  i64 lda, ldb, ldc;      // row strides: bytes of A and B, elements of C
+  int lda, ldb, ldc;      // row strides: bytes of A and B, elements of C
   const int32_t* offsets;
-  i64 rows;
-  int groups;
+  int rows, groups;
   int K;                  // FWD, INPUT: contraction, in elements (FP4: of whole units)
   int M, N;               // WEIGHT: rows of C (n); columns of C
   int tiles_n;            // column tiles
@@ -69,17 +71,24 @@ __device__ __forceinline__ void dma4b(const u32x4& rsrc, uint32_t voff, uint32_t
   asm volatile("buffer_load_dword %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "{m0}"(lds) : "memory");
 }
 
-// One operand of the tile in issue: where its next stage starts and how many bytes there are from there on.
+// The same value in every lane, in scalar registers.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ i64 uniform(i64 v) { return (i64)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v)); }
+__device__ __forceinline__ uint64_t uniform(uint64_t v) { return (uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v); }
+
+// One operand of the tile in issue: where its next stage starts and how many bytes there are from there on (of rows along the contraction: of a tile's
+// height of them, which is less than 2^31).
+template <class Left>
 struct Feed {
   uint64_t at;
-  i64 left;
+  Left left;
   __device__ __forceinline__ u32x4 rsrc(bool on) const {      // empty if !on
-    const i64 most = 0x7ffffff0;      // a stage or a tile spans less
-    const int n = left <= 0 || !on ? 0 : (int)(left < most ? left : most);
-    return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)at), (uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) & 0xffffu,
-                 (uint32_t)__builtin_amdgcn_readfirstlane(n), 0x00020000u};
+    const int high = sizeof(Left) == 8 ? (int)((i64)left >> 32) : left < 0 ? -1 : 0;      // compared in halves: there is no scalar comparison of 64 bits
+    const uint32_t low = (uint32_t)left, most = 0x7ffffff0u;                                // a stage or a tile spans less
+    const uint32_t n = high < 0 || !on ? 0u : high > 0 || low > most ? most : low;
+    return u32x4{(uint32_t)uniform((int)at), (uint32_t)uniform((int)(at >> 32)) & 0xffffu, (uint32_t)uniform((int)n), 0x00020000u};
   }
-  __device__ __forceinline__ void step(i64 bytes) {
+  __device__ __forceinline__ void step(Left bytes) {
     at += bytes;
     left -= bytes;
   }
@@ -90,8 +99,17 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(void* p, i64 bytes) 
   return __builtin_amdgcn_make_buffer_rsrc(p, (short)0, bytes <= 0 ? 0 : (int)(bytes < kNowhere ? bytes : kNowhere), 0x00020000);
 }
 
+// c += a b on 16 x 16 x 128 codes; SA, SB: which byte of a lane's words scales its 32 codes
+template <int SA, int SB>
 __device__ __forceinline__ void mfma_fp4(floatx4& c, const u32x4& a, const u32x4& b, uint32_t sa, uint32_t sb) {
-  asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] cbsz:4 blgp:4" : "+a"(c) : "v"(a), "v"(b), "v"(sa), "v"(sb));
+  asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%5,%6,0] op_sel_hi:[%7,%8,0] cbsz:4 blgp:4"
+               : "+a"(c)
+               : "v"(a), "v"(b), "v"(sa), "v"(sb), "n"(SA & 1), "n"(SB & 1), "n"(SA >> 1), "n"(SB >> 1));
+}
+// f(0), f(1), .. as constants
+template <int... I, class F>
+__device__ __forceinline__ void in_turn(std::integer_sequence<int, I...>, const F& f) {
+  (f(std::integral_constant<int, I>{}), ...);
 }
 
 template <Dir DIR, class C>
@@ -133,7 +151,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   if (n_my == 0) return;
 
   struct Where {
-    int gr, r0, r1;      // group; FWD, INPUT: first row of the tile; WEIGHT: of the group; end of the group
+    int gr, first, r0, r1;      // group, its first row; FWD, INPUT: the tile's first row; WEIGHT: the group's; end of the group
     int i0, j0;          // WEIGHT: first row of C; first column
     int stages;          // an even number
   };
@@ -151,7 +169,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
     const int rt = first_m + (u % per_group) % gsz;
     w.j0 = ((u % per_group) / gsz) * BN;
     w.i0 = rt * BM;
-    w.r0 = w.r1 = 0;
+    w.first = w.r0 = w.r1 = 0;
     if (DIR == WEIGHT) {
 #pragma unroll
       for (int q = 0; q < kTableSets; ++q)
@@ -171,6 +189,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
           w.gr = 64 * q + l;
           w.r0 = __builtin_amdgcn_readlane(tr0[q], l);
           w.r1 = __builtin_amdgcn_readlane(tr1[q], l);
+          w.first = w.r0;
           const int end = __builtin_amdgcn_readlane(tsum[q], l), mine = (w.r1 - w.r0 + BM - 1) / BM;
           w.r0 += (rt - (end - mine)) * BM;
         }
@@ -182,7 +201,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
 
   // ---- per-lane byte offsets of the loads, the same for every stage and tile
   uint32_t voffA[IPWA], voffB[FP4 ? 1 : IPWB], voffS[IPWS ? IPWS : 1];      // FP4: both operands' rows are as long, and the tile square
-  auto slot_offset = [&](int slot, bool kmajor, int width, i64 ld) __attribute__((always_inline)) {
+  auto slot_offset = [&](int slot, bool kmajor, int width, int ld) __attribute__((always_inline)) {
     if (kmajor) {
       const int r = slot >> 2, c = dense::xk16_chunk(slot & 3, r);
       return (uint32_t)(r * ld + c * 16);
@@ -199,16 +218,22 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
 #pragma unroll
   for (int s = 0; s < IPWS; ++s) {
     const int r = (wave * IPWS + s) * 64 + lane;
-    voffS[s] = (uint32_t)((r < BM ? r : r - BM) * ((r < BM ? g.lda : g.ldb) / 16));
+    voffS[s] = (uint32_t)((r < BM ? r : r - BM) * 4);
   }
   // lanes whose 16 bytes lie past the end of a row in its last, short stage: the chunk a lane fetches is the same in each of its loads
   const int short_stage = !FP4 && DIR != WEIGHT && g.K % 32 ? g.K / 32 : -1;
   const uint64_t past_end = __ballot(8 * dense::xk16_chunk(lane & 3, lane >> 2) >= g.K % 32);
 
   // ---- issue side
-  Feed fa, fb;
+  typedef typename std::conditional<A_K, int, i64>::type LeftA;
+  typedef typename std::conditional<B_K, int, i64>::type LeftB;
+  Feed<LeftA> fa;
+  Feed<LeftB> fb;
+  uint64_t fsa = 0, fsb = 0;      // FP4: scales of the tile's rows in this stage, and their bytes
+  int fha = 0, fhb = 0;
   int iti = -1, ikt = 0, iKT = 0, islot = 0;
-  const i64 stepA = A_K ? 64 : 32 * g.lda, stepB = B_K ? 64 : 32 * g.ldb;
+  const LeftA stepA = A_K ? 64 : 32 * (LeftA)g.lda;
+  const LeftB stepB = B_K ? 64 : 32 * (LeftB)g.ldb;
   auto next_tile = [&]() __attribute__((always_inline)) {
     Where w;
     do {
@@ -217,32 +242,44 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
       w = locate(iti);
     } while (DIR == WEIGHT && w.stages == 0);
     ikt = 0;
-    if (iti >= n_my) {      // nothing more: empty descriptors
-      fa.left = fb.left = 0;
-      iKT = 0x7fffffff;
-      return;
-    }
-    iKT = w.stages;
-    const int hb = DIR == FWD ? g.N - w.j0 < BN ? g.N - w.j0 : BN : 0;      // rows of W in the tile
+    Feed<LeftA> na{0, 0};      // nothing more: empty descriptors
+    Feed<LeftB> nb{0, 0};
+    int stages = 0x7fffffff, ha = 0, hb = 0;
+    uint64_t nsa = 0, nsb = 0;
+    if (iti < n_my) {
+    stages = w.stages;
+    if (DIR == FWD) hb = g.N - w.j0 < BN ? g.N - w.j0 : BN;      // rows of W in the tile
     if (DIR == WEIGHT) {
       const i64 len = w.r1 - w.r0;
-      fa.at = (uint64_t)(g.A + (i64)w.r0 * g.lda + 2 * w.i0);
-      fa.left = (len - 1) * g.lda + 2 * (i64)(g.M - w.i0);
-      fb.at = (uint64_t)(g.B + (i64)w.r0 * g.ldb + 2 * w.j0);
-      fb.left = (len - 1) * g.ldb + 2 * (i64)(g.N - w.j0);
+      na.at = (uint64_t)(g.A + (i64)w.r0 * g.lda + 2 * w.i0);
+      na.left = (len - 1) * (i64)g.lda + 2 * (i64)(g.M - w.i0);
+      nb.at = (uint64_t)(g.B + (i64)w.r0 * g.ldb + 2 * w.j0);
+      nb.left = (len - 1) * (i64)g.ldb + 2 * (i64)(g.N - w.j0);
     } else {
-      const int ha = w.r1 - w.r0 < BM ? w.r1 - w.r0 : BM;
-      const i64 row = FP4 ? g.K / 2 : 2 * (i64)g.K;      // bytes of a row
-      fa.at = (uint64_t)(g.A + (i64)w.r0 * g.lda);
-      fa.left = (ha - 1) * g.lda + row;
+      ha = w.r1 - w.r0 < BM ? w.r1 - w.r0 : BM;
+      const int row = FP4 ? g.K / 2 : 2 * g.K;      // bytes of a row
+      na.at = (uint64_t)(g.A + (i64)w.r0 * g.lda);
+      na.left = (ha - 1) * (LeftA)g.lda + row;
       if (DIR == FWD) {
         const i64 first = (i64)w.gr * g.N + w.j0;
-        fb.at = (uint64_t)(g.B + first * g.ldb);
-        fb.left = (hb - 1) * g.ldb + row;
+        nb.at = (uint64_t)(g.B + first * g.ldb);
+        nb.left = (hb - 1) * (LeftB)g.ldb + row;
+        nsa = (uint64_t)(g.SA + mx4::position(w.first, w.gr) + (w.r0 - w.first));      // a word per row
+        nsb = (uint64_t)(g.SB + (i64)w.gr * ((g.N + 63) / 64 * 64) + w.j0);
       } else {
-        fb.at = (uint64_t)(g.B + (i64)w.gr * g.K * g.ldb + 2 * w.j0);
-        fb.left = (i64)(g.K - 1) * g.ldb + 2 * (i64)(g.N - w.j0);
+        nb.at = (uint64_t)(g.B + (i64)w.gr * g.K * g.ldb + 2 * w.j0);
+        nb.left = (i64)(g.K - 1) * g.ldb + 2 * (i64)(g.N - w.j0);
       }
+    }
+    }
+    iKT = uniform(stages);
+    fa = Feed<LeftA>{uniform(na.at), uniform(na.left)};
+    fb = Feed<LeftB>{uniform(nb.at), uniform(nb.left)};
+    if (FP4) {
+      fsa = uniform(nsa);
+      fsb = uniform(nsb);
+      fha = uniform((ha + 63) / 64 * 256);
+      fhb = uniform((hb + 63) / 64 * 256);
     }
   };
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
@@ -253,9 +290,8 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
     ra = fa.rsrc(!A_K || on);
     rb = fb.rsrc(!B_K || on);
     if (FP4) {
-      // a byte of scales per 16 bytes of codes, in rows as many times shorter
-      rsa = Feed{(uint64_t)g.SA + ((fa.at - (uint64_t)g.A) >> 4), fa.left >> 4}.rsrc(on);
-      rsb = Feed{(uint64_t)g.SB + ((fb.at - (uint64_t)g.B) >> 4), fb.left >> 4}.rsrc(on);
+      rsa = Feed<int>{fsa, fha}.rsrc(on);
+      rsb = Feed<int>{fsb, fhb}.rsrc(on);
     } else {
       masked = ikt == short_stage ? past_end : 0;
     }
@@ -279,6 +315,10 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
     ++ikt;
     fa.step(stepA);
     fb.step(stepB);
+    if (FP4) {
+      fsa += g.sa_step;
+      fsb += g.sb_step;
+    }
     stage_rsrc();
   };
   // after every second stage: tiles have even numbers of them, and so has the ring
@@ -305,7 +345,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
 #pragma unroll
     for (int c = 0; c < (B_K ? 1 : TN); ++c) fragB[c] = A_BYTES + frag(wn * (BN / 2) + c * 16, B_K, BN);
   }
-  const int scaleA = A_BYTES + C::B_BYTES + (wm * (BM / 2) + li) * 4 + q4, scaleB = A_BYTES + C::B_BYTES + (BM + wn * (BN / 2) + li) * 4 + q4;
+  const int scaleA = A_BYTES + C::B_BYTES + wm * (BM / 2) * 4 + lane * 4, scaleB = A_BYTES + C::B_BYTES + (BM + wn * (BN / 2)) * 4 + lane * 4;
   auto load_frag = [&](const char* p, bool kmajor, int row_bytes) -> u32x4 {
     if (kmajor) return *reinterpret_cast<const u32x4*>(p);
     const mm::short4v lo = mm::lds_read_tr(p), hi = mm::lds_read_tr(p + 4 * row_bytes);
@@ -314,7 +354,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   };
   struct Frags {
     u32x4 a[TM], b[TN];
-    uint32_t sa[FP4 ? TM : 1], sb[FP4 ? TN : 1];
+    uint32_t sa[TM / 4], sb[TN / 4];      // FP4: a byte per piece
   };
   // piece p, in the order the MFMAs first need them: A0 B0 A1 .. A(TM-1) B1 .. B(TN-1)
   auto load_piece = [&](Frags& f, int slot, int p) __attribute__((always_inline)) {
@@ -322,11 +362,11 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
     if (p != 1 && p <= TM) {
       const int a = p ? p - 1 : 0;
       f.a[a] = load_frag(st + fragA[A_K ? 0 : a] + (A_K ? a * 1024 : 0), A_K, BM * 2);
-      if (FP4) f.sa[FP4 ? a : 0] = *reinterpret_cast<const uint8_t*>(st + scaleA + a * 64);
+      if (FP4 && a % 4 == 0) f.sa[a / 4] = *reinterpret_cast<const uint32_t*>(st + scaleA + a * 64);
     } else {
       const int b = p == 1 ? 0 : p - TM;
       f.b[b] = load_frag(st + fragB[B_K ? 0 : b] + (B_K ? b * 1024 : 0), B_K, BN * 2);
-      if (FP4) f.sb[FP4 ? b : 0] = *reinterpret_cast<const uint8_t*>(st + scaleB + b * 64);
+      if (FP4 && b % 4 == 0) f.sb[b / 4] = *reinterpret_cast<const uint32_t*>(st + scaleB + b * 64);
     }
   };
 
@@ -360,15 +400,15 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
     auto multiply = [&](const Frags& X, Frags& Y) __attribute__((always_inline)) {
       mm::wait_all_reads_and_barrier<(NS - 2) * LPT>();
       const int nslot = cslot + 1 == NS ? 0 : cslot + 1;
-#pragma unroll
-      for (int i = 0; i < MF; ++i) {
-        if constexpr (FP4) mfma_fp4(acc[i % TM][i / TM], X.b[i / TM], X.a[i % TM], X.sb[i / TM], X.sa[i % TM]);
-        else dense::mfma16(acc[i % TM][i / TM], __builtin_bit_cast(bf16x8, X.b[i / TM]), __builtin_bit_cast(bf16x8, X.a[i % TM]));
-        if (i % RS == 0 && i / RS < TM + TN) load_piece(Y, nslot, i / RS);
-        if (i % DS == W * DS / 4 && i / DS < LPT) issue(i / DS);
-        if (i == MF - 1) issue_advance();
+      in_turn(std::make_integer_sequence<int, MF>{}, [&](auto I) __attribute__((always_inline)) {
+        constexpr int i = decltype(I)::value, a = i % TM, b = i / TM;
+        if constexpr (FP4) mfma_fp4<b % 4, a % 4>(acc[a][b], X.b[b], X.a[a], X.sb[b / 4], X.sa[a / 4]);
+        else dense::mfma16(acc[a][b], __builtin_bit_cast(bf16x8, X.b[b]), __builtin_bit_cast(bf16x8, X.a[a]));
+        if constexpr (i % RS == 0 && i / RS < TM + TN) load_piece(Y, nslot, i / RS);
+        if constexpr (i % DS == W * DS / 4 && i / DS < LPT) issue(i / DS);
+        if constexpr (i == MF - 1) issue_advance();
         __builtin_amdgcn_sched_barrier(0);
-      }
+      });
       cslot = nslot;
     };
     for (int ti = 0; ti < n_my; ++ti) {

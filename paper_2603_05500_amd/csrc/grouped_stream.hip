@@ -87,24 +87,24 @@ Kernel plan(int dtype, Dir dir, const Call& c, bool streams) {
 void stream_launch(Dir dir, Kernel k, const Call& c, hipStream_t st) {
   StreamArgs a = {};
   a.offsets = c.offsets;
-  a.rows = c.rows;
+  a.rows = (int)c.rows;
   a.groups = c.groups;
   a.C = c.out;
-  a.ldc = c.ld_out;
+  a.ldc = (int)c.ld_out;
   a.accumulate = c.accumulate;
   if (dir == WEIGHT) {
     a.A = (const char*)c.in2;
-    a.lda = 2 * c.ld_in2;
+    a.lda = (int)(2 * c.ld_in2);
     a.B = (const char*)c.in;
-    a.ldb = 2 * c.ld_in;
+    a.ldb = (int)(2 * c.ld_in);
     a.M = c.n;
     a.N = c.m;
     return pick<WEIGHT>(k, a, st);
   }
   a.A = (const char*)c.in;
-  a.lda = 2 * c.ld_in;
+  a.lda = (int)(2 * c.ld_in);
   a.B = (const char*)c.w;
-  a.ldb = 2 * (i64)c.m;
+  a.ldb = 2 * c.m;
   a.K = dir == FWD ? c.m : c.n;
   a.N = dir == FWD ? c.n : c.m;
   dir == FWD ? pick<FWD>(k, a, st) : pick<INPUT>(k, a, st);
@@ -112,21 +112,35 @@ void stream_launch(Dir dir, Kernel k, const Call& c, hipStream_t st) {
 
 // ---- both operands in four bits ---------------------------------------------------------------------
 bool codes_supported(const poetx_grouped_desc* d, const void* Z, i64 ldz) {
-  return d->groups <= Codes256::GROUPS && d->d_out % 8 == 0 && ldz % 8 == 0 && ldz * 512 < (1ll << 31) && aligned16(Z) && (i64)mx4::units(d->d_in) * 64 * 256 < (1ll << 31);
+  return d->groups <= Codes256::GROUPS && d->d_out % 8 == 0 && ldz % 8 == 0 && ldz * 512 < (1ll << 31) && aligned16(Z) && (i64)mx4::units(d->d_in) * 64 * 256 < (1ll << 31) &&
+         d->rows < (1 << 28) && (i64)d->groups * (d->d_out + 64) < (1 << 28);
 }
-void codes_launch(const poetx_grouped_desc* d, const void* Xq, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, hipStream_t st) {
-  const mx4::View x = mx4::view(Xq, d->rows, d->d_in), w = mx4::view(Wq, (i64)d->groups * d->d_out, d->d_in);
+size_t codes_workspace_bytes(const poetx_grouped_desc* d) {
+  const size_t units = mx4::units(d->d_in);
+  return align256(d->rows * units * 64) + align256(mx4::positions(d->rows, d->groups) * units * 4) + align256((size_t)d->groups * ((d->d_out + 63) / 64) * units * 256);
+}
+void codes_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, void* ws, hipStream_t st) {
+  const i64 wrows = (i64)d->groups * d->d_out;
   const int units = mx4::units(d->d_in);
+  char* xs = (char*)ws + align256((size_t)d->rows * units * 64);
+  char* wst = xs + align256(mx4::positions(d->rows, d->groups) * units * 4);
+  {
+    StageTimer tm(POETX_STAGE_DEQUANT, st);
+    mx4_operands_launch(X, d->rows, d->d_in, ldx, offsets, d->groups, d->d_out, Wq, ws, xs, wst, st);
+  }
+  StageTimer tm(POETX_STAGE_DENSE, st);
   StreamArgs a = {};
-  a.A = (const char*)x.codes;
-  a.B = (const char*)w.codes;
-  a.SA = x.scales;
-  a.SB = w.scales;
+  a.A = (const char*)ws;
+  a.B = (const char*)mx4::view(Wq, wrows, d->d_in).codes;
+  a.SA = (const uint32_t*)xs;
+  a.SB = (const uint32_t*)wst;
+  a.sa_step = (int)(4 * mx4::positions(d->rows, d->groups));
+  a.sb_step = d->groups * ((d->d_out + 63) / 64) * 256;
   a.C = Z;
-  a.lda = a.ldb = (i64)units * 64;
-  a.ldc = ldz;
+  a.lda = a.ldb = units * 64;
+  a.ldc = (int)ldz;
   a.offsets = offsets;
-  a.rows = d->rows;
+  a.rows = (int)d->rows;
   a.groups = d->groups;
   a.K = units * mx4::UNIT;
   a.N = d->d_out;

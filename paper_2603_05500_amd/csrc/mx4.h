@@ -18,6 +18,13 @@ struct View {
 };
 inline View view(const void* Q, i64 rows, int cols) { return View{(const uint8_t*)Q, (const uint8_t*)Q + scale_offset(rows, cols)}; }
 
+// ---- scales as the streaming product reads them -------------------------------------------------------
+// Unit by unit, 256 bytes per 64 rows: byte (16 q + i) 4 + s is that of row 16 s + i and the unit's block q, so that a lane's word holds its fragments of four 16-row
+// pieces.  A group starts a new 64: of the weight its rows are rounded up; the rows of X, whose groups start anywhere, have positions that leave room for it.
+__host__ __device__ inline i64 position(i64 r0, int g) { return (r0 + 63) / 64 * 64 + 64 * (i64)g; }      // of a group's first row: past the last row of those before
+inline __host__ __device__ i64 positions(i64 rows, int groups) { return position(rows, groups); }
+__device__ __forceinline__ int scale_place(int row, int q) { return (16 * q + (row & 15)) * 4 + (row >> 4); }
+
 // A scale byte as the fp32 power of two it stands for.  2^-127 has no exponent field of its own; 255 gives an infinity, whose field the conversions below take as NaN.
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte ? byte << 23 : 0x00400000u); }
 // Scale byte of a block whose largest magnitude has these fp32 bits: the exponent field less 2 (e2m1 reaches 2^2), where infinities and NaN, whose bits are

@@ -174,6 +174,9 @@ void skew_project_tiled_launch(const float* M, int b, i64 nb, float* dtheta, int
 
 // ---- 4-bit buffers (mx4.hip; layout: mx4.h) -----------------------------------------------------
 void mx4_quantize_launch(int dtype, const void* X, i64 rows, int cols, i64 ld, void* Q, hipStream_t st);
+// codes of X (rows x units x 64 bytes), and the scales of X and of the buffer Wq (groups * n rows) in the streaming product's order (mx4.h)
+void mx4_operands_launch(const void* X, i64 rows, int cols, i64 ld, const int32_t* offsets, int groups, int n, const void* Wq, void* codes, void* xs, void* wst,
+                         hipStream_t st);
 void mx4_dequantize_launch(const void* Q, i64 rows, int cols, int dtype, void* out, i64 ld, hipStream_t st);
 
 // ---- rows in the order of their groups (group_order.hip) ---------------------------------------
