@@ -107,10 +107,10 @@ bool codes_supported(const poetx_grouped_desc* d, const void* Z, i64 ldz);
 size_t codes_workspace_bytes(const poetx_grouped_desc* d);
 void codes_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, void* ws, hipStream_t st);
 
-// the forward of a handful of rows per group, bf16 (grouped_few.hip): any sizes, strides and alignments
-enum Weight { DENSE_BF16, VALUES_MX4, CODES_MX4 };      // CODES: of X as well
-bool few_supported(int dtype, Dir dir, i64 rows, int groups, Weight w);
-void few_dense(const Call& c, hipStream_t st);
+// the forward of a handful of rows per group (grouped_few.hip): any sizes, strides and alignments
+enum Weight { DENSE_WEIGHT, VALUES_MX4, CODES_MX4 };      // CODES: of X as well
+bool few_supported(int dtype, Dir dir, i64 rows, int m, int n, int groups, Weight w);
+void few_dense(int dtype, const Call& c, hipStream_t st);
 void few_values(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, hipStream_t st);      // 4-bit weight
 void few_codes(const poetx_grouped_desc* d, const void* Xq, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, hipStream_t st);               // 4-bit rows too
 

@@ -54,16 +54,16 @@ size_t workspace_bytes(const poetx_grouped_desc* d) {
 }
 
 // The products of a 4-bit weight run on its values, made in the workspace.
-const void* dense_weight(const poetx_grouped_desc* d, const void* W, void* ws, hipStream_t st) {
+const void* dense_weight(const poetx_grouped_desc* d, const void* W, const int32_t* offsets, void* ws, hipStream_t st) {
   if (!(d->flags & POETX_GROUPED_W_MX4)) return W;
   StageTimer tm(POETX_STAGE_DEQUANT, st);
-  mx4_dequantize_launch(W, (i64)d->groups * d->d_out, d->d_in, POETX_BF16, ws, d->d_in, st);
+  mx4_dequantize_groups_launch(W, d->groups, d->d_out, d->d_in, offsets, d->rows, ws, st);
   return ws;
 }
 
 void product(int dtype, grouped::Dir dir, const grouped::Call& c, hipStream_t st) {
   StageTimer tm(POETX_STAGE_DENSE, st);
-  if (grouped::few_supported(dtype, dir, c.rows, c.groups, grouped::DENSE_BF16)) return grouped::few_dense(c, st);
+  if (grouped::few_supported(dtype, dir, c.rows, c.m, c.n, c.groups, grouped::DENSE_WEIGHT)) return grouped::few_dense(dtype, c, st);
   const grouped::Kernel k = grouped::plan(dtype, dir, c, dtype == POETX_BF16 && grouped::stream_supported(dir, c));
   k >= grouped::STREAM_256 ? grouped::stream_launch(dir, k, c, st) : grouped::edge_launch(dtype, dir, k, c, st);
 }
@@ -120,7 +120,7 @@ int poetx_grouped_fwd(const poetx_grouped_desc* d, const void* X, int64_t ldx, c
   if (rc != POETX_OK || d->rows == 0) return rc;
   hipStream_t st = (hipStream_t)stream;
   const bool mx4 = d->flags & POETX_GROUPED_W_MX4, both = d->flags & POETX_GROUPED_X_MX4;
-  const bool few = mx4 && grouped::few_supported(d->dtype, grouped::FWD, d->rows, d->groups, both ? grouped::CODES_MX4 : grouped::VALUES_MX4);
+  const bool few = mx4 && grouped::few_supported(d->dtype, grouped::FWD, d->rows, d->d_in, d->d_out, d->groups, both ? grouped::CODES_MX4 : grouped::VALUES_MX4);
   if (both && few) {
     {
       StageTimer tm(POETX_STAGE_DEQUANT, st);
@@ -139,7 +139,7 @@ int poetx_grouped_fwd(const poetx_grouped_desc* d, const void* X, int64_t ldx, c
     grouped::few_values(d, X, ldx, W, offsets, Z, ldz, st);
     return launch_status();
   }
-  const void* w = dense_weight(d, W, ws, st);
+  const void* w = dense_weight(d, W, offsets, ws, st);
   if (d->flags & POETX_GROUPED_X_MX4) {
     char* values = (char*)ws + dequantised_bytes(d);
     char* codes = values + align256((size_t)d->rows * d->d_in * 2);
@@ -158,7 +158,7 @@ int poetx_grouped_bwd_input(const poetx_grouped_desc* d, const void* dZ, int64_t
   const int rc = check_rows_call(d, dZ, lddz, d ? d->d_out : 0, W, offsets, dX, lddx, d ? d->d_in : 0, ws, ws_bytes);
   if (rc != POETX_OK || d->rows == 0) return rc;
   hipStream_t st = (hipStream_t)stream;
-  const void* w = dense_weight(d, W, ws, st);
+  const void* w = dense_weight(d, W, offsets, ws, st);
   product(d->dtype, grouped::INPUT, grouped::Call{dZ, nullptr, w, dX, lddz, 0, lddx, offsets, d->rows, d->d_in, d->d_out, d->groups, 0}, st);
   return launch_status();
 }

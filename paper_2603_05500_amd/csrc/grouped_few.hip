@@ -4,6 +4,7 @@
 // the first operand of 16 x 16 MFMAs whose second one is up to 16 NT rows of X; the waves of a workgroup split the contraction and meet in LDS.
 // A lane's load is 16 bytes of one weight row, whatever they hold:
 //   DENSE   8 bf16, one MFMA of depth 32
+//   SINGLE  4 fp32, four MFMAs of depth 4, the groups of 16 lanes holding every fourth four
 //   VALUES  32 codes with their scale, decoded in registers: four MFMAs of depth 32, in which the four groups of 16 lanes hold four different blocks of 32
 //           (the order of a contraction is free as long as both operands keep it)
 //   CODES   32 codes, and 32 of X: one scaled MFMA of depth 128
@@ -21,14 +22,14 @@ using mm::bf16x8;
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef int intx8 __attribute__((ext_vector_type(8)));
 
-enum Kind { DENSE, VALUES, CODES };
+enum Kind { DENSE, VALUES, CODES, SINGLE };
 
 struct FewArgs {
-  const void* X;            // bf16 rows; CODES: codes
+  const void* X;            // rows; CODES: codes
   const uint8_t* xs;        // CODES: scales
-  const void* W;            // bf16 rows of m; else codes
+  const void* W;            // rows of m, or codes
   const uint8_t* ws;
-  uint16_t* Z;
+  void* Z;
   i64 ldx, ldz;             // elements; CODES: ldx is the bytes of a row of codes
   const int32_t* offsets;
   i64 rows;
@@ -74,7 +75,34 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(FewArgs a, int fir
   auto steps = [&](int s, auto N_, auto WHOLE_) __attribute__((always_inline)) {      // that many units of 128, their loads in flight together; WHOLE: inside the rows
     constexpr int N = decltype(N_)::value;
     constexpr bool WHOLE = decltype(WHOLE_)::value;
-    auto values = [&](const uint16_t* row, int k) __attribute__((always_inline)) { return WHOLE ? load16(row + k) : edge::load_branched(row, k, a.m, true); };
+    auto values = [&](const auto* row, int k) __attribute__((always_inline)) { return WHOLE ? load16(row + k) : edge::load_branched(row, k, a.m, true); };
+    if constexpr (KIND == SINGLE) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {      // 64 of depth at a time
+        u32x4 fw[N][4][RT], fx[N][4][NT];
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+#pragma unroll
+          for (int p = 0; p < 4; ++p) {
+            const int k = (s + u) * 128 + 64 * h + 16 * p + 4 * q;
+#pragma unroll
+            for (int r = 0; r < RT; ++r) fw[u][p][r] = values((const float*)a.W + wrow[r] * a.m, k);
+#pragma unroll
+            for (int c = 0; c < NT; ++c) fx[u][p][c] = values((const float*)a.X + xrow[c] * a.ldx, k);
+          }
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+#pragma unroll
+          for (int p = 0; p < 4; ++p)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int c = 0; c < NT; ++c)
+                  acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, (uint32_t)fw[u][p][r][e]), __builtin_bit_cast(float, (uint32_t)fx[u][p][c][e]), acc[r][c], 0, 0, 0);
+      }
+    } else
     if constexpr (KIND == DENSE) {
       u32x4 fw[N][4][RT], fx[N][4][NT];
 #pragma unroll
@@ -179,7 +207,11 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(FewArgs a, int fir
     float y = 0.f;
 #pragma unroll
     for (int z = 0; z < NW; ++z) y += part[z][i];
-    if (row < rows && col < a.n) a.Z[(t.r0 + row) * a.ldz + col] = (uint16_t)mm::pack2_bf16(y, 0.f);
+    if (row < rows && col < a.n) {
+      const i64 at = (t.r0 + row) * a.ldz + col;
+      if constexpr (KIND == SINGLE) ((float*)a.Z)[at] = y;
+      else ((uint16_t*)a.Z)[at] = (uint16_t)mm::pack2_bf16(y, 0.f);
+    }
   }
 }
 
@@ -192,38 +224,53 @@ void go(FewArgs a, hipStream_t st) {
   });
 }
 
-// Rows of X per tile: as many as an average group has; weight rows per wave: more where there are workgroups enough, as each reads its rows of X anew.
-// us, by (weight rows, rows of X, waves, units in flight), weights from memory:
+// 16 x 16 tiles that groups of average size give
+i64 small_tiles(i64 rows, int groups, int n) {
+  const i64 live = rows < groups ? rows : groups, tiles = groups == 1 ? (rows + 15) / 16 : rows / 16 + live / 2;
+  return (tiles > live ? tiles : live) * ((n + 15) / 16);
+}
+
+// Tiles of 16 x 16 where there are few in all, whatever the rows; otherwise as many rows of X as an average group has, and more weight rows per wave, as each wave reads its rows of X
+// anew.  us, by (weight rows, rows of X, waves, units in flight), weights from memory:
 //   4 bits:  4096 x 4096, 1 row (16,16,4,4) 4.1  (32,16,4,4) 6.0; 16 rows 6.8, 8.2; 14336 x 4096, 1 row (16,16,4,4) 11.2  (32,16,4,4) 9.9  (64,16,8,4) 11.0; 16 rows 21.6, 14.6, 12.5;
-//            eight of 64 experts of 1376 x 2048 a row each 5.8, 6.1, 7.4; all of them with 8 each 45.6, 32.6, 35.8; 14336 x 4096, 32 rows (64,32,4,1) 18.6  (64,64,4,1) 22.7
+//            eight of 64 experts of 1376 x 2048 a row each 5.8, 6.1, 7.4; all of them with 8 each 45.6, 32.6, 35.8; 14336 x 4096, 32 rows (64,32,4,1) 18.6  (64,64,4,1) 22.7;
+//            1024 x 4096, 64 rows (16,16,4,4) 6.8  (64,64,4,1) 25.8; 4096 x 4096, 128 rows (16,16,4,4) 39  (64,32,4,1) 17.9  (64,64,4,1) 26.7; eight experts, 512 rows 32.9, 19.4, 23.6
 //   bf16:    14336 x 4096, 1 row (16,16,4,4) 23.2  (64,16,4,2) 24.9; 16 rows 35.3, 27.2; the experts 10.2, 11.4; with 8 rows each 81.0, 75.6
 template <Kind KIND>
 void pick(const FewArgs& a, hipStream_t st) {
-  const i64 live = a.rows < a.groups ? a.rows : a.groups, mean = (a.rows + live - 1) / live, tiles = live * ((a.n + 15) / 16);
-  if (mean > 32) go<4, 4, 4, KIND, 1>(a, st);
-  else if (mean > 16) go<4, 2, 4, KIND, 1>(a, st);
-  else if (KIND == DENSE) tiles <= 1024 && mean <= 8 ? go<1, 1, 4, KIND, 4>(a, st) : go<4, 1, 4, KIND, 2>(a, st);
-  else if (tiles <= 768) go<1, 1, 4, KIND, 4>(a, st);
+  const i64 live = a.rows < a.groups ? a.rows : a.groups, mean = (a.rows + live - 1) / live, tiles = small_tiles(a.rows, a.groups, a.n);
+  if (tiles <= (KIND == SINGLE ? 1024 : 768)) return go<1, 1, 4, KIND, KIND == SINGLE ? 1 : 4>(a, st);
+  if constexpr (KIND == SINGLE) return go<2, 2, 4, KIND, 1>(a, st);
+  else if constexpr (KIND == DENSE) tiles <= 1024 && mean <= 8 ? go<1, 1, 4, KIND, 4>(a, st) : go<4, 1, 4, KIND, 2>(a, st);
   else if (mean <= 8) go<2, 1, 4, KIND, 4>(a, st);
-  else go<4, 1, 8, KIND, 4>(a, st);
+  else if (mean <= 16) go<4, 1, 8, KIND, 4>(a, st);
+  else if (mean <= 32 || tiles < 512 * 16) go<4, 2, 4, KIND, 1>(a, st);
+  else go<4, 4, 4, KIND, 1>(a, st);
 }
 
 }  // namespace
 
-bool few_supported(int dtype, Dir dir, i64 rows, int groups, Weight w) {
-  i64 most = w == VALUES_MX4 ? 128 : 16;
-  return dtype == POETX_BF16 && dir == FWD && rows <= most * groups;
+// Where it pays: up to so many rows per group, or few tiles in all.  us, these / the streams and edge kernels: bf16 64 experts of 1376 x 2048 with 8 rows each 76 / 86, 32 each 101 / 91;
+// both in four bits, 14336 x 4096, 16 rows 11 / 24, 64 experts with 32 rows each 51 / 37, 256 x 8192, four with 30 in all 9 / 33;
+// a 4-bit weight against its values in the workspace: 14336 x 4096, 128 rows 49 / 66, 64 experts with 64 rows each 96 / 194.
+// few tiles: bf16 1024 x 4096, 64 rows 9.5 / 13.8, 128 rows 16.5 / 14.6, 1024 x 1024, 128 rows 5.6 / 7.0; fp32 128 x 1749, 179 rows 7.4 / 32, 1024 x 2048, 256 rows 19 / 38.
+bool few_supported(int dtype, Dir dir, i64 rows, int m, int n, int groups, Weight w) {
+  if (dir != FWD) return false;
+  const i64 most = dtype == POETX_F32 ? 4 : w == VALUES_MX4 ? 128 : 16;
+  const i64 few = dtype == POETX_F32 ? 1024 : w != DENSE_WEIGHT ? 768 : m <= 2048 ? 640 : 320;
+  return rows <= most * groups || small_tiles(rows, groups, n) <= few;
 }
-void few_dense(const Call& c, hipStream_t st) {
-  pick<DENSE>(FewArgs{c.in, nullptr, c.w, nullptr, (uint16_t*)c.out, c.ld_in, c.ld_out, c.offsets, c.rows, c.m, c.n, c.groups, (c.m + 127) / 128, 0}, st);
+void few_dense(int dtype, const Call& c, hipStream_t st) {
+  const FewArgs a{c.in, nullptr, c.w, nullptr, c.out, c.ld_in, c.ld_out, c.offsets, c.rows, c.m, c.n, c.groups, (c.m + 127) / 128, 0};
+  dtype == POETX_F32 ? pick<SINGLE>(a, st) : pick<DENSE>(a, st);
 }
 void few_values(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, hipStream_t st) {
   const mx4::View w = mx4::view(Wq, (i64)d->groups * d->d_out, d->d_in);
-  pick<VALUES>(FewArgs{X, nullptr, w.codes, w.scales, (uint16_t*)Z, ldx, ldz, offsets, d->rows, d->d_in, d->d_out, d->groups, mx4::units(d->d_in), 0}, st);
+  pick<VALUES>(FewArgs{X, nullptr, w.codes, w.scales, Z, ldx, ldz, offsets, d->rows, d->d_in, d->d_out, d->groups, mx4::units(d->d_in), 0}, st);
 }
 void few_codes(const poetx_grouped_desc* d, const void* Xq, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, hipStream_t st) {
   const mx4::View w = mx4::view(Wq, (i64)d->groups * d->d_out, d->d_in), x = mx4::view(Xq, d->rows, d->d_in);
-  pick<CODES>(FewArgs{x.codes, x.scales, w.codes, w.scales, (uint16_t*)Z, 0, ldz, offsets, d->rows, d->d_in, d->d_out, d->groups, mx4::units(d->d_in), 0}, st);
+  pick<CODES>(FewArgs{x.codes, x.scales, w.codes, w.scales, Z, 0, ldz, offsets, d->rows, d->d_in, d->d_out, d->groups, mx4::units(d->d_in), 0}, st);
 }
 
 }  // namespace grouped

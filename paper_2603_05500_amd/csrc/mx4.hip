@@ -76,23 +76,31 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const T* __restrict__
   }
 }
 
-template <class T>
+// One matrix, or (GROUPS) the weights of the groups that have rows: `total` units each.
+template <class T, bool GROUPS>
 __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint32_t* __restrict__ codes, const uint8_t* __restrict__ scales, int cols, int upr, i64 total,
-                                                             T* __restrict__ out, i64 ld, int block0) {
+                                                             T* __restrict__ out, i64 ld, int block0, const int32_t* offsets, i64 rows, int per_group) {
   const int lane = threadIdx.x & 15;
-  const i64 first = (i64)(block0 + blockIdx.x) * (16 * UPL) + (threadIdx.x >> 4);
+  i64 block = block0 + (i64)blockIdx.x, base = 0;
+  if constexpr (GROUPS) {
+    const int g = (int)(block / per_group);
+    const grouped::Range r = grouped::group_range(offsets, g, rows);
+    if (r.r0 == r.r1) return;
+    block -= (i64)g * per_group;
+    base = g * total;
+  }
+  const i64 first = block * (16 * UPL) + (threadIdx.x >> 4);
   uint32_t c[UPL], sb[UPL];
 #pragma unroll
   for (int p = 0; p < UPL; ++p) {
-    const i64 u = first + 16 * p < total ? first + 16 * p : total - 1;
+    const i64 u = base + (first + 16 * p < total ? first + 16 * p : total - 1);
     c[p] = codes[u * 16 + lane];
     sb[p] = scales[u * 4 + (lane >> 2)];
   }
 #pragma unroll
   for (int p = 0; p < UPL; ++p) {
-    const i64 u = first + 16 * p;
-    if (u >= total) continue;
-    const i64 row = u / upr;
+    if (first + 16 * p >= total) continue;
+    const i64 u = base + first + 16 * p, row = u / upr;
     const int k = (int)(u - row * upr) * mx4::UNIT + 8 * lane;
     if (k >= cols) continue;
     float v[8];
@@ -211,11 +219,21 @@ void mx4_dequantize_launch(const void* Q, i64 rows, int cols, int dtype, void* o
   const mx4::View q = mx4::view(Q, rows, cols);
   auto go = [&](auto kern, auto* o) {
     launch_in_rows((total + 16 * UPL - 1) / (16 * UPL), [&](int block0, unsigned count) {
-      hipLaunchKernelGGL(kern, dim3(count), dim3(256), 0, st, (const uint32_t*)q.codes, q.scales, cols, upr, total, o, ld, block0);
+      hipLaunchKernelGGL(kern, dim3(count), dim3(256), 0, st, (const uint32_t*)q.codes, q.scales, cols, upr, total, o, ld, block0, nullptr, 0, 0);
     });
   };
-  if (dtype == POETX_F32) go(mx4_dequantize_kernel<float>, (float*)out);
-  else go(mx4_dequantize_kernel<uint16_t>, (uint16_t*)out);
+  if (dtype == POETX_F32) go(mx4_dequantize_kernel<float, false>, (float*)out);
+  else go(mx4_dequantize_kernel<uint16_t, false>, (uint16_t*)out);
+}
+
+void mx4_dequantize_groups_launch(const void* Q, int groups, int n, int cols, const int32_t* offsets, i64 rows, void* out, hipStream_t st) {
+  const int upr = mx4::units(cols);
+  const i64 total = (i64)n * upr, per_group = (total + 16 * UPL - 1) / (16 * UPL);
+  const mx4::View q = mx4::view(Q, (i64)groups * n, cols);
+  launch_in_rows(per_group * groups, [&](int block0, unsigned count) {
+    hipLaunchKernelGGL((mx4_dequantize_kernel<uint16_t, true>), dim3(count), dim3(256), 0, st, (const uint32_t*)q.codes, q.scales, cols, upr, total, (uint16_t*)out, (i64)cols,
+                       block0, offsets, rows, (int)per_group);
+  });
 }
 
 }  // namespace poetx

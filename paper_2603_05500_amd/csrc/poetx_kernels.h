@@ -178,6 +178,8 @@ void mx4_quantize_launch(int dtype, const void* X, i64 rows, int cols, i64 ld, v
 void mx4_operands_launch(const void* X, i64 rows, int cols, i64 ld, const int32_t* offsets, int groups, int n, const void* Wq, void* codes, void* xs, void* wst,
                          hipStream_t st);
 void mx4_dequantize_launch(const void* Q, i64 rows, int cols, int dtype, void* out, i64 ld, hipStream_t st);
+// the bf16 values [groups][n][cols] of the groups that have rows
+void mx4_dequantize_groups_launch(const void* Q, int groups, int n, int cols, const int32_t* offsets, i64 rows, void* out, hipStream_t st);
 
 // ---- rows in the order of their groups (group_order.hip) ---------------------------------------
 size_t group_order_workspace_bytes(i64 n, int groups);
