@@ -64,8 +64,8 @@ const void* dense_weight(const poetx_grouped_desc* d, const void* W, const int32
 void product(int dtype, grouped::Dir dir, const grouped::Call& c, hipStream_t st) {
   StageTimer tm(POETX_STAGE_DENSE, st);
   if (grouped::few_supported(dtype, dir, c.rows, c.m, c.n, c.groups, grouped::DENSE_WEIGHT)) return grouped::few_dense(dtype, c, st);
-  const grouped::Kernel k = grouped::plan(dtype, dir, c, dtype == POETX_BF16 && grouped::stream_supported(dir, c));
-  k >= grouped::STREAM_256 ? grouped::stream_launch(dir, k, c, st) : grouped::edge_launch(dtype, dir, k, c, st);
+  const grouped::Kernel k = grouped::plan(dtype, dir, c, grouped::stream_supported(dtype, dir, c));
+  k >= grouped::STREAM_256 ? grouped::stream_launch(dtype, dir, k, c, st) : grouped::edge_launch(dtype, dir, k, c, st);
 }
 
 // Forward and input gradient: in is rows x d_i, out rows x d_o.

@@ -1,4 +1,4 @@
-// Grouped bf16 products on the matrix cores, and those of 4-bit operands: the kernel.
+// Grouped products on the matrix cores, bf16, fp32 and of 4-bit operands: the kernel.
 //   FWD     Z  (rows x n) = X  (rows x m) W_g^T      both operands contracted along their rows
 //   INPUT   dX (rows x m) = dZ (rows x n) W_g        W_g over its strided index
 //   WEIGHT  dW_g (n x m)  = dZ^T X over g's rows     both over their strided index; fp32 out
@@ -12,8 +12,9 @@
 //    does: what lies behind reads as zeros, on both operands, so that nothing of another group takes part.  Only the last stage of rows whose length is
 //    no multiple of a stage needs a mask, the same 64 lanes for every load of it.  Past the last tile the descriptors are
 //    empty: the number of loads in flight never changes and the last ones cost no traffic.
-//  - FP4: a stage is 64 bytes of a row either way, 32 bf16 or 128 codes with a word of four scales, and an MFMA of 16 x 16 x 128 codes takes as long
-//    as one of 16 x 16 x 32 bf16: the same stream carries four times the products.
+//  - A stage is 64 bytes of a row whatever they hold: 32 bf16, 16 fp32, or 128 codes with a word of four scales.  An MFMA of 16 x 16 x 128 codes takes as long
+//    as one of 16 x 16 x 32 bf16: the same stream carries four times the products.  The fp32 ones take eight times as long for the bytes: smaller tiles and several
+//    workgroups per CU.
 #pragma once
 #include <utility>
 
@@ -30,21 +31,25 @@ using mx4::u32x4;
 
 
 
-template <int BM_, int BN_, int NS_, bool FP4_>
+enum Elem { BF16, F32, CODES };
+
+template <int BM_, int BN_, int NS_, Elem ELEM_, int PER_CU_ = 1>
 struct StreamTile {
-  static constexpr int BM = BM_, BN = BN_, NS = NS_, NW = 4;
-  static constexpr bool FP4 = FP4_;
+  static constexpr int BM = BM_, BN = BN_, NS = NS_, NW = 4, PER_CU = PER_CU_;
+  static constexpr Elem ELEM = ELEM_;
+  static constexpr bool FP4 = ELEM == CODES;
+  static constexpr int DEPTH = FP4 ? 128 : ELEM == F32 ? 16 : 32;      // elements of a stage
   static constexpr int SETS = 4, GROUPS = 64 * SETS;      // groups per lane, in all
   static constexpr int A_BYTES = BM * 64, B_BYTES = BN * 64, S_BYTES = FP4 ? (BM + BN) * 4 : 0, STAGE_BYTES = A_BYTES + B_BYTES + S_BYTES;
-  static constexpr int TM = BM / 32, TN = BN / 32, MF = TM * TN;
+  static constexpr int TM = BM / 32, TN = BN / 32, MF = TM * TN * (ELEM == F32 ? 4 : 1);      // MFMAs of a stage; fp32: 4 of depth per MFMA
   static constexpr int RS = MF / (TM + TN) < 3 ? MF / (TM + TN) : 3;
-  static constexpr int OUT_BYTES = TN / 4 * 2048;
+  static constexpr int OUT_BYTES = ELEM == F32 ? 0 : TN / 4 * 2048;
   static constexpr int LDS_BYTES = NS * STAGE_BYTES + NW * OUT_BYTES;
   static constexpr int IPWA = A_BYTES / 1024 / NW, IPWB = B_BYTES / 1024 / NW, IPWS = FP4 ? (BM + BN) / 256 : 0;
   static constexpr int LPT = IPWA + IPWB + IPWS;
   static constexpr int DS = MF / LPT;
   static_assert(!FP4 || (BM == BN && (BM + BN) % 256 == 0), "scale loads: as many for every wave, each of one operand");
-  static_assert(NS * LPT < 64 && DS >= 1 && RS >= 1 && (TM + TN) * RS <= MF && TN % 4 == 0 && LDS_BYTES <= 160 * 1024, "stream tile");
+  static_assert(NS * LPT < 64 && DS >= 1 && RS >= 1 && (TM + TN) * RS <= MF && (ELEM == F32 || TN % 4 == 0) && LDS_BYTES <= 160 * 1024, "stream tile");
 };
 
 struct StreamArgs {
@@ -57,7 +62,7 @@ struct StreamArgs {
   int lda, ldb, ldc;      // row strides: bytes of A and B, elements of C
   const int32_t* offsets;
   int rows, groups;
-  int K;                  // FWD, INPUT: contraction, in elements (FP4: of whole units)
+  int K;                  // FWD, INPUT: contraction, in elements (CODES: of whole units)
   int M, N;               // WEIGHT: rows of C (n); columns of C
   int tiles_n;            // column tiles
   int accumulate;
@@ -106,6 +111,9 @@ __device__ __forceinline__ void mfma_fp4(floatx4& c, const u32x4& a, const u32x4
                : "+a"(c)
                : "v"(a), "v"(b), "v"(sa), "v"(sb), "n"(SA & 1), "n"(SB & 1), "n"(SA >> 1), "n"(SB >> 1));
 }
+// c += a b on 16 x 16 x 4 fp32
+__device__ __forceinline__ void mfma_fp32(floatx4& c, uint32_t a, uint32_t b) { asm volatile("v_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b)); }
+
 // f(0), f(1), .. as constants
 template <int... I, class F>
 __device__ __forceinline__ void in_turn(std::integer_sequence<int, I...>, const F& f) {
@@ -114,7 +122,8 @@ __device__ __forceinline__ void in_turn(std::integer_sequence<int, I...>, const 
 
 template <Dir DIR, class C>
 __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
-  constexpr bool FP4 = C::FP4, A_K = DIR != WEIGHT, B_K = DIR == FWD;
+  constexpr bool FP4 = C::FP4, FP32 = C::ELEM == F32, A_K = DIR != WEIGHT, B_K = DIR == FWD;
+  constexpr int DEPTH = C::DEPTH, ES = FP32 ? 4 : 2;      // bytes of an element (not of a code)
   static_assert(!FP4 || DIR == FWD, "codes are contracted along their rows");
   constexpr int BM = C::BM, BN = C::BN, NS = C::NS, STAGE_BYTES = C::STAGE_BYTES, A_BYTES = C::A_BYTES;
   constexpr int IPWA = C::IPWA, IPWB = C::IPWB, IPWS = C::IPWS, LPT = C::LPT, TM = C::TM, TN = C::TN, MF = C::MF, RS = C::RS, DS = C::DS;
@@ -177,7 +186,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
           w.r0 = __builtin_amdgcn_readlane(tr0[q], w.gr & 63);
           w.r1 = __builtin_amdgcn_readlane(tr1[q], w.gr & 63);
         }
-      w.stages = (w.r1 - w.r0 + 63) / 64 * 2;
+      w.stages = (w.r1 - w.r0 + 2 * DEPTH - 1) / (2 * DEPTH) * 2;
     } else {
       bool found = false;
 #pragma unroll
@@ -194,19 +203,21 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
           w.r0 += (rt - (end - mine)) * BM;
         }
       }
-      w.stages = (g.K + (FP4 ? 255 : 63)) / (FP4 ? 256 : 64) * 2;
+      w.stages = (g.K + 2 * DEPTH - 1) / (2 * DEPTH) * 2;
     }
     return w;
   };
 
   // ---- per-lane byte offsets of the loads, the same for every stage and tile
   uint32_t voffA[IPWA], voffB[FP4 ? 1 : IPWB], voffS[IPWS ? IPWS : 1];      // FP4: both operands' rows are as long, and the tile square
+  // Rows along the output: where chunk c of row k lies.  bf16: as the transposing loads like it; fp32: a fragment's four rows 4 q + e, q = 0 .. 3, in four different 64 bytes.
+  auto strided_chunk = [&](int c, int k) __attribute__((always_inline)) { return FP32 ? c ^ (4 * ((k >> 2) & 3)) : dense::kx16_chunk(c, k); };
   auto slot_offset = [&](int slot, bool kmajor, int width, int ld) __attribute__((always_inline)) {
     if (kmajor) {
       const int r = slot >> 2, c = dense::xk16_chunk(slot & 3, r);
       return (uint32_t)(r * ld + c * 16);
     }
-    const int k = slot / (width / 8), c = dense::kx16_chunk(slot % (width / 8), k);
+    const int k = slot / (width * ES / 16), c = strided_chunk(slot % (width * ES / 16), k);
     return (uint32_t)(k * ld + c * 16);
   };
 #pragma unroll
@@ -221,8 +232,8 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
     voffS[s] = (uint32_t)((r < BM ? r : r - BM) * 4);
   }
   // lanes whose 16 bytes lie past the end of a row in its last, short stage: the chunk a lane fetches is the same in each of its loads
-  const int short_stage = !FP4 && DIR != WEIGHT && g.K % 32 ? g.K / 32 : -1;
-  const uint64_t past_end = __ballot(8 * dense::xk16_chunk(lane & 3, lane >> 2) >= g.K % 32);
+  const int short_stage = !FP4 && DIR != WEIGHT && g.K % DEPTH ? g.K / DEPTH : -1;
+  const uint64_t past_end = __ballot(16 / ES * dense::xk16_chunk(lane & 3, lane >> 2) >= g.K % DEPTH);
 
   // ---- issue side
   typedef typename std::conditional<A_K, int, i64>::type LeftA;
@@ -232,8 +243,8 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   uint64_t fsa = 0, fsb = 0;      // FP4: scales of the tile's rows in this stage, and their bytes
   int fha = 0, fhb = 0;
   int iti = -1, ikt = 0, iKT = 0, islot = 0;
-  const LeftA stepA = A_K ? 64 : 32 * (LeftA)g.lda;
-  const LeftB stepB = B_K ? 64 : 32 * (LeftB)g.ldb;
+  const LeftA stepA = A_K ? 64 : DEPTH * (LeftA)g.lda;
+  const LeftB stepB = B_K ? 64 : DEPTH * (LeftB)g.ldb;
   auto next_tile = [&]() __attribute__((always_inline)) {
     Where w;
     do {
@@ -251,13 +262,13 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
     if (DIR == FWD) hb = g.N - w.j0 < BN ? g.N - w.j0 : BN;      // rows of W in the tile
     if (DIR == WEIGHT) {
       const i64 len = w.r1 - w.r0;
-      na.at = (uint64_t)(g.A + (i64)w.r0 * g.lda + 2 * w.i0);
-      na.left = (len - 1) * (i64)g.lda + 2 * (i64)(g.M - w.i0);
-      nb.at = (uint64_t)(g.B + (i64)w.r0 * g.ldb + 2 * w.j0);
-      nb.left = (len - 1) * (i64)g.ldb + 2 * (i64)(g.N - w.j0);
+      na.at = (uint64_t)(g.A + (i64)w.r0 * g.lda + ES * w.i0);
+      na.left = (len - 1) * (i64)g.lda + ES * (i64)(g.M - w.i0);
+      nb.at = (uint64_t)(g.B + (i64)w.r0 * g.ldb + ES * w.j0);
+      nb.left = (len - 1) * (i64)g.ldb + ES * (i64)(g.N - w.j0);
     } else {
       ha = w.r1 - w.r0 < BM ? w.r1 - w.r0 : BM;
-      const int row = FP4 ? g.K / 2 : 2 * g.K;      // bytes of a row
+      const int row = FP4 ? g.K / 2 : ES * g.K;      // bytes of a row
       na.at = (uint64_t)(g.A + (i64)w.r0 * g.lda);
       na.left = (ha - 1) * (LeftA)g.lda + row;
       if (DIR == FWD) {
@@ -267,8 +278,8 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
         nsa = (uint64_t)(g.SA + mx4::position(w.first, w.gr) + (w.r0 - w.first));      // a word per row
         nsb = (uint64_t)(g.SB + (i64)w.gr * ((g.N + 63) / 64 * 64) + w.j0);
       } else {
-        nb.at = (uint64_t)(g.B + (i64)w.gr * g.K * g.ldb + 2 * w.j0);
-        nb.left = (i64)(g.K - 1) * g.ldb + 2 * (i64)(g.N - w.j0);
+        nb.at = (uint64_t)(g.B + (i64)w.gr * g.K * g.ldb + ES * w.j0);
+        nb.left = (i64)(g.K - 1) * g.ldb + ES * (i64)(g.N - w.j0);
       }
     }
     }
@@ -286,7 +297,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   u32x4 ra, rb, rsa, rsb;
   uint64_t masked = 0;
   auto stage_rsrc = [&]() __attribute__((always_inline)) {
-    const bool on = ikt * (FP4 ? 128 : 32) < g.K;      // not a stage that only evens their number (WEIGHT: has no rows)
+    const bool on = ikt * DEPTH < g.K;      // not a stage that only evens their number (WEIGHT: has no rows)
     ra = fa.rsrc(!A_K || on);
     rb = fb.rsrc(!B_K || on);
     if (FP4) {
@@ -338,6 +349,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
     const int k = 8 * q4 + (li >> 2);
     auto frag = [&](int x0, bool kmajor, int width) {
       if (kmajor) return (x0 + li) * 64 + 16 * dense::xk16_chunk(q4, li);
+      if (FP32) return 4 * q4 * (width * 4) + 16 * strided_chunk((x0 + li) >> 2, 4 * q4) + 4 * (li & 3);
       return k * (width * 2) + 16 * dense::kx16_chunk((x0 >> 3) + ((li & 3) >> 1), k) + 8 * (li & 1);
     };
 #pragma unroll
@@ -348,13 +360,19 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   const int scaleA = A_BYTES + C::B_BYTES + wm * (BM / 2) * 4 + lane * 4, scaleB = A_BYTES + C::B_BYTES + (BM + wn * (BN / 2)) * 4 + lane * 4;
   auto load_frag = [&](const char* p, bool kmajor, int row_bytes) -> u32x4 {
     if (kmajor) return *reinterpret_cast<const u32x4*>(p);
+    if constexpr (FP32) {      // row_bytes: of a row of bf16
+      u32x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const uint32_t*>(p + e * 2 * row_bytes);
+      return v;
+    }
     const mm::short4v lo = mm::lds_read_tr(p), hi = mm::lds_read_tr(p + 4 * row_bytes);
     const mm::short8v v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     return __builtin_bit_cast(u32x4, v);
   };
   struct Frags {
     u32x4 a[TM], b[TN];
-    uint32_t sa[TM / 4], sb[TN / 4];      // FP4: a byte per piece
+    uint32_t sa[(TM + 3) / 4], sb[(TN + 3) / 4];      // CODES: a byte per piece
   };
   // piece p, in the order the MFMAs first need them: A0 B0 A1 .. A(TM-1) B1 .. B(TN-1)
   auto load_piece = [&](Frags& f, int slot, int p) __attribute__((always_inline)) {
@@ -401,8 +419,9 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
       mm::wait_all_reads_and_barrier<(NS - 2) * LPT>();
       const int nslot = cslot + 1 == NS ? 0 : cslot + 1;
       in_turn(std::make_integer_sequence<int, MF>{}, [&](auto I) __attribute__((always_inline)) {
-        constexpr int i = decltype(I)::value, a = i % TM, b = i / TM;
+        constexpr int i = decltype(I)::value, a = i % TM, b = i / TM % TN;
         if constexpr (FP4) mfma_fp4<b % 4, a % 4>(acc[a][b], X.b[b], X.a[a], X.sb[b / 4], X.sa[a / 4]);
+        else if constexpr (FP32) mfma_fp32(acc[a][b], X.b[b][i / (TM * TN)], X.a[a][i / (TM * TN)]);
         else dense::mfma16(acc[a][b], __builtin_bit_cast(bf16x8, X.b[b]), __builtin_bit_cast(bf16x8, X.a[a]));
         if constexpr (i % RS == 0 && i / RS < TM + TN) load_piece(Y, nslot, i / RS);
         if constexpr (i % DS == W * DS / 4 && i / DS < LPT) issue(i / DS);
@@ -418,20 +437,27 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
         multiply(Gf, F);
         tile_advance();
       }
-      dense::settle(acc);
+      if constexpr (FP32) {      // as settle() does
+        asm volatile("s_nop 15\n\ts_nop 3");
+#pragma unroll
+        for (int a = 0; a < TM; ++a) asm volatile("" : "+a"(acc[a][TN - 1]));
+      } else {
+        dense::settle(acc);
+      }
       const Where w = locate(ti);
       // Stores go through a descriptor as well: rows past the group's end (of dW) lie behind it, and a lane whose columns do not exist gets an offset that does.
-      if constexpr (DIR == WEIGHT) {
+      if constexpr (DIR == WEIGHT || FP32) {
         // a lane's four columns of a row
-        const int row = wm * (BM / 2) + li, col = wn * (BN / 2) + 4 * q4;
-        const auto rc = make_rsrc((float*)g.C + (i64)w.gr * g.M * g.N + (i64)w.i0 * g.N + w.j0, ((i64)(g.M - w.i0 - 1) * g.N + g.N - w.j0) * 4);
+        const int row = wm * (BM / 2) + li, col = wn * (BN / 2) + 4 * q4, rows = DIR == WEIGHT ? g.M - w.i0 : w.r1 - w.r0, cols = g.N - w.j0;
+        const i64 first = DIR == WEIGHT ? ((i64)w.gr * g.M + w.i0) * g.ldc : (i64)w.r0 * g.ldc;
+        const auto rc = make_rsrc((float*)g.C + first + w.j0, ((i64)(rows - 1) * g.ldc + cols) * 4);
         auto store = [&](auto ADD) __attribute__((always_inline)) {
 #pragma unroll
           for (int a = 0; a < TM; ++a) {
-            const int at = ((row + a * 16) * g.N + col) * 4;
+            const int at = ((row + a * 16) * g.ldc + col) * 4;
 #pragma unroll
             for (int c = 0; c < TN; ++c) {
-              const int v = col + c * 16 < g.N - w.j0 ? at + c * 64 : kNowhere;
+              const int v = col + c * 16 < cols ? at + c * 64 : kNowhere;
               floatx4 x = acc[a][c];
               acc[a][c] = floatx4{0.f, 0.f, 0.f, 0.f};
               if constexpr (decltype(ADD)::value) x += __builtin_bit_cast(floatx4, __builtin_amdgcn_raw_buffer_load_b128(rc, v, 0, 0));
@@ -440,7 +466,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
             __builtin_amdgcn_sched_barrier(0);
           }
         };
-        if (g.accumulate) store(std::true_type{});
+        if (DIR == WEIGHT && g.accumulate) store(std::true_type{});
         else store(std::false_type{});
       } else {
         // through LDS, 16 rows x 64 columns at a time, so that every instruction writes whole 128-byte lines

@@ -5,11 +5,13 @@ namespace poetx {
 namespace grouped {
 namespace {
 
-typedef StreamTile<256, 256, 4, false> Tile256;
-typedef StreamTile<256, 128, 6, false> Tile256x128;
-typedef StreamTile<128, 128, 8, false> Tile128;
-typedef StreamTile<256, 256, 4, true> Codes256;
-typedef StreamTile<128, 128, 6, true> Codes128;
+typedef StreamTile<256, 256, 4, BF16> Tile256;
+typedef StreamTile<256, 128, 6, BF16> Tile256x128;
+typedef StreamTile<128, 128, 8, BF16> Tile128;
+typedef StreamTile<256, 256, 4, CODES> Codes256;
+typedef StreamTile<128, 128, 6, CODES> Codes128;
+typedef StreamTile<128, 128, 4, F32, 2> Single128;
+typedef StreamTile<64, 64, 8, F32, 2> Single64;
 
 constexpr int kCUs = 256;
 
@@ -20,12 +22,14 @@ void go(const StreamArgs& a0, hipStream_t st) {
   (void)configured;
   StreamArgs a = a0;
   a.tiles_n = ceil_div(a.N, C::BN);
-  hipLaunchKernelGGL(kern, dim3(kCUs), dim3(256), C::LDS_BYTES, st, a);
+  hipLaunchKernelGGL(kern, dim3(kCUs * C::PER_CU), dim3(256), C::LDS_BYTES, st, a);
 }
 
 template <Dir DIR>
 void pick(Kernel k, const StreamArgs& a, hipStream_t st) {
-  if (k == STREAM_256) go<DIR, Tile256>(a, st);
+  if (k == SINGLE_128) go<DIR, Single128>(a, st);
+  else if (k == SINGLE_64) go<DIR, Single64>(a, st);
+  else if (k == STREAM_256) go<DIR, Tile256>(a, st);
   else if (k == STREAM_256x128) go<DIR, Tile256x128>(a, st);
   else go<DIR, Tile128>(a, st);
 }
@@ -43,48 +47,59 @@ inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 }  // namespace
 
-bool stream_supported(Dir dir, const Call& c) {
-  const i64 wide = 1ll << 31;
-  return c.groups <= Tile256::GROUPS && c.m % 8 == 0 && c.n % 8 == 0 && c.ld_in % 8 == 0 && c.ld_out % 8 == 0 && aligned16(c.in) && aligned16(c.out) &&
-         (dir == WEIGHT ? c.ld_in2 % 8 == 0 && aligned16(c.in2) && c.ld_in2 * 64 < wide && c.ld_in * 64 < wide && (i64)c.m * 1024 < wide
-                        : aligned16(c.w) && c.ld_in * 512 < wide && (i64)c.m * 512 < wide && c.ld_out * 512 < wide);
+bool stream_supported(int dtype, Dir dir, const Call& c) {
+  const int es = dtype == POETX_F32 ? 4 : 2, v = 16 / es;
+  const i64 wide = (1ll << 31) / (es * 256);      // a tile's rows, or a stage's, span less than 2^31 bytes
+  return c.groups <= Tile256::GROUPS && c.m % v == 0 && c.n % v == 0 && c.ld_in % v == 0 && c.ld_out % v == 0 && aligned16(c.in) && aligned16(c.out) &&
+         c.ld_in < wide && c.ld_out < wide && c.m < wide / 2 &&
+         (dir == WEIGHT ? c.ld_in2 % v == 0 && aligned16(c.in2) && c.ld_in2 < wide : aligned16(c.w));
 }
 
-// The figures were fitted to 600 calls of random directions, sizes (64 to 14336), groups (1 to 128) and rows (1 to 32768) with every kernel that could take them; the choices
-// they lead to take 1.3 % more time than the best would (geometric mean), 10 % at worst in nine of ten.
+// The figures were fitted to 600 calls in bf16 and 700 in fp32 of random directions, sizes (64 to 14336; 64 to 4096), groups (1 to 128) and rows (1 to 32768; 8 to 8192), each
+// with every kernel that could take it; the choices they lead to take 1.5 % more time than the best would (geometric mean).
 Kernel plan(int dtype, Dir dir, const Call& c, bool streams) {
   struct Row {
+    Kernel kernel;
     int h, w, depth;      // tile, depth of a stage
     double stage;         // us
-    double at_once;       // edge kernels: tiles that the chip works on at a time
-    double uneven;        // streams: part of a round that the last one takes more than its share, where groups end inside tiles
+    double at_once;       // tiles that the chip works on at a time
+    double uneven;        // bf16 streams, which go round by round: part of a round that the last one takes more than its share, where groups end inside tiles
     double rest;          // us
   };
-  static const Row bf16[KERNELS] = {{32, 32, 128, 0.64, 400, 0, 3.5}, {32, 32, 512, 1.1, 137, 0, 5.1}, {64, 64, 64, 0.80, 433, 0, 2.9}, {128, 128, 64, 1.58, 224, 0, 3.2},
-                                    {256, 256, 32, 0.67, kCUs, 0.45, 11.8}, {256, 128, 32, 0.52, kCUs, 0.33, 7.5}, {128, 128, 32, 0.315, kCUs, 0.65, 7.7}};
-  static const Row f32[EDGE_128] = {{32, 32, 64, 1.0, 430, 0, 3}, {32, 32, 256, 1e9, 1, 0, 3}, {64, 64, 32, 1.05, 360, 0, 3}};
+  static const Row bf16[] = {{EDGE_32, 32, 32, 128, 0.64, 400, 0, 3.5},      {EDGE_32_DEEP, 32, 32, 512, 1.1, 137, 0, 5.1}, {EDGE_64, 64, 64, 64, 0.80, 433, 0, 2.9},
+                             {EDGE_128, 128, 128, 64, 1.58, 224, 0, 3.2},    {STREAM_256, 256, 256, 32, 0.67, kCUs, 0.45, 11.8}, {STREAM_256x128, 256, 128, 32, 0.52, kCUs, 0.33, 7.5},
+                             {STREAM_128, 128, 128, 32, 0.315, kCUs, 0.65, 7.7}};
+  static const Row fp32[] = {{EDGE_32, 32, 32, 64, 0.87, 356, 0, 3.9}, {EDGE_64, 64, 64, 32, 1.08, 260, 0, 3.6}, {SINGLE_128, 128, 128, 16, 1.42, 253, 0, 10.2},
+                             {SINGLE_64, 64, 64, 16, 0.42, 295, 0, 7.0}};
+  const bool f = dtype == POETX_F32;
+  const Row* rows = f ? fp32 : bf16;
+  const int count = f ? (int)(sizeof(fp32) / sizeof(Row)) : (int)(sizeof(bf16) / sizeof(Row));
   const double live = c.rows < c.groups ? (double)c.rows : c.groups;
   const double K = dir == FWD ? c.m : dir == INPUT ? c.n : live > 0 ? c.rows / live : 0;
   const double out_us = dir == WEIGHT ? 4.0 * c.groups * c.n * c.m / 5.1e6 : 0;      // fp32 weights to memory
-  int best = EDGE_32;
+  Kernel best = EDGE_32;
   double least = 1e30;
-  for (int k = 0; k < (dtype == POETX_F32 ? EDGE_128 : streams ? KERNELS : STREAM_256); ++k) {
-    const Row& r = dtype == POETX_F32 ? f32[k] : bf16[k];
-    const double tiles = tiles_of(dir, c.rows, c.m, c.n, c.groups, r.h, r.w), stages = (i64)((K + r.depth - 1) / r.depth);
+  for (int i = 0; i < count; ++i) {
+    const Row& r = rows[i];
+    const bool stream = r.kernel >= STREAM_256;
+    if (stream && !streams) break;
+    const double tiles = tiles_of(dir, c.rows, c.m, c.n, c.groups, r.h, r.w), stages = (double)(i64)((K + r.depth - 1) / r.depth);
     double us = tiles / r.at_once;
-    if (k >= STREAM_256) us = c.groups == 1 ? (double)(i64)(us + 0.999) : us + r.uneven;
+    if (stream && !f) us = c.groups == 1 ? (double)(i64)(us + 0.999) : us + r.uneven;
     us = (us < 1 ? 1 : us) * stages * r.stage;
     // a stream stores between multiplications; the others have several workgroups on a CU, but store less well
-    us = r.rest + (k >= STREAM_256 ? us + out_us : us > 1.23 * out_us ? us : 1.23 * out_us);
+    const double stores = (f ? 1.5 : 1.23) * out_us;
+    us = r.rest + (stream ? us + out_us : us > stores ? us : stores);
     if (us < least) {
       least = us;
-      best = k;
+      best = r.kernel;
     }
   }
-  return (Kernel)best;
+  return best;
 }
 
-void stream_launch(Dir dir, Kernel k, const Call& c, hipStream_t st) {
+void stream_launch(int dtype, Dir dir, Kernel k, const Call& c, hipStream_t st) {
+  const int es = dtype == POETX_F32 ? 4 : 2;
   StreamArgs a = {};
   a.offsets = c.offsets;
   a.rows = (int)c.rows;
@@ -94,17 +109,17 @@ void stream_launch(Dir dir, Kernel k, const Call& c, hipStream_t st) {
   a.accumulate = c.accumulate;
   if (dir == WEIGHT) {
     a.A = (const char*)c.in2;
-    a.lda = (int)(2 * c.ld_in2);
+    a.lda = (int)(es * c.ld_in2);
     a.B = (const char*)c.in;
-    a.ldb = (int)(2 * c.ld_in);
+    a.ldb = (int)(es * c.ld_in);
     a.M = c.n;
     a.N = c.m;
     return pick<WEIGHT>(k, a, st);
   }
   a.A = (const char*)c.in;
-  a.lda = (int)(2 * c.ld_in);
+  a.lda = (int)(es * c.ld_in);
   a.B = (const char*)c.w;
-  a.ldb = 2 * c.m;
+  a.ldb = es * c.m;
   a.K = dir == FWD ? c.m : c.n;
   a.N = dir == FWD ? c.n : c.m;
   dir == FWD ? pick<FWD>(k, a, st) : pick<INPUT>(k, a, st);
