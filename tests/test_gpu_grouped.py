@@ -377,3 +377,190 @@ def test_group_order(lib, n, groups, dropped):
     ws = torch.full((max(256, px.poetx_group_order_workspace_bytes(n, groups)),), 255, dtype=torch.uint8, device="cuda")
     px.poetx_group_order(torch.from_numpy(ids.astype(np.int32)).cuda(), off, order, ws)
     assert np.array_equal(off.cpu().numpy(), want_off) and np.array_equal(order.cpu().numpy(), want)
+
+
+# ------------------------------------------------------------------------------------ sizes at which every kernel runs
+def reference(kind, x, w, counts, dz=None):
+    """float64 results and sums of magnitudes, group by group, on the GPU."""
+    a, outs, mags = 0, [], []
+    for g, c in enumerate(counts):
+        if kind == "weight":
+            l, r = dz[a: a + c].double().t(), x[a: a + c].double()
+        else:
+            l, r = x[a: a + c].double(), w[g].double().t() if kind == "fwd" else w[g].double()
+        outs.append(l @ r)
+        mags.append(l.abs() @ r.abs())
+        a += c
+    return (torch.stack if kind == "weight" else torch.cat)(outs), (torch.stack if kind == "weight" else torch.cat)(mags)
+
+
+def within(got, ref, mag, K, dtype):
+    lim = (K + 4) * 2.0 ** -24 * mag + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -23) * ref.abs() + 1e-37
+    return bool((torch.isfinite(got) & ((got.double() - ref).abs() <= lim)).all())
+
+
+def spread(groups, rows, seed=0):
+    """Uneven group sizes, some of them zero, that add up to `rows`."""
+    rng = np.random.default_rng(seed)
+    p = np.exp(rng.standard_normal(groups)) * (rng.random(groups) > 0.1)
+    if p.sum() == 0:
+        p[:] = 1
+    return rng.multinomial(rows, p / p.sum()).tolist()
+
+
+LARGE = [
+    # groups, rows, d_in, d_out
+    (1, 4096, 1024, 4096), (1, 2000, 1416, 2056), (8, 5000, 1032, 3000), (64, 6000, 520, 1376), (3, 1300, 1824, 1760), (5, 9000, 264, 776), (200, 3000, 256, 512),
+    (300, 2000, 128, 136), (16, 8192, 512, 512), (2, 700, 2600, 96), (1, 333, 4000, 1000), (4, 12000, 40, 2048),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("groups,rows,m,n", LARGE)
+def test_grouped_large(lib, groups, rows, m, n, dtype):
+    counts, dt = spread(groups, rows), DT[dtype]
+    off = offsets_of(counts)
+    g = torch.Generator(device="cuda").manual_seed(groups + rows)
+    X, dZ = (torch.randn((rows, d), device="cuda", generator=g).to(dt) for d in (m, n))
+    W = (torch.randn((groups, n, m), device="cuda", generator=g) * 0.02).to(dt)
+    desc = px.make_grouped_desc(m, n, groups, rows, CODE[dtype])
+    ws = torch.empty(max(256, px.poetx_grouped_workspace_bytes(desc)), dtype=torch.uint8, device="cuda")
+    Z, dX, dW = torch.empty((rows, n), dtype=dt, device="cuda"), torch.empty((rows, m), dtype=dt, device="cuda"), torch.empty((groups, n, m), device="cuda")
+    px.poetx_grouped_fwd(desc, X, W, off, Z, ws)
+    px.poetx_grouped_bwd_input(desc, dZ, W, off, dX, ws)
+    px.poetx_grouped_bwd_weight(desc, X, dZ, off, dW, False, ws)
+    assert within(Z, *reference("fwd", X, W, counts), m, dtype)
+    assert within(dX, *reference("input", dZ, W, counts), n, dtype)
+    ref, mag = reference("weight", X, None, counts, dZ)
+    assert within(dW, ref, mag, rows, "f32")
+    px.poetx_grouped_bwd_weight(desc, X, dZ, off, dW, True, ws)
+    assert within(dW, 2 * ref, 2 * mag, rows, "f32")
+
+
+@pytest.mark.parametrize("act", ["same", "mx4"])
+@pytest.mark.parametrize("groups,rows,m,n", LARGE + [(1, 16, 2048, 8192), (1, 100, 1024, 4096), (1, 8, 512, 14336), (40, 1200, 384, 640), (1, 60, 4096, 6000), (64, 300, 256, 1376)])
+def test_grouped_mx4_large(lib, groups, rows, m, n, act):
+    counts = spread(groups, rows)
+    off = offsets_of(counts)
+    g = torch.Generator(device="cuda").manual_seed(groups + rows)
+    X, dZ = (torch.randn((rows, d), device="cuda", generator=g).bfloat16() for d in (m, n))
+    Q = quantised((torch.randn((groups * n, m), device="cuda", generator=g) * 0.02).bfloat16())
+    W, Xr = torch.empty((groups * n, m), dtype=torch.bfloat16, device="cuda"), X
+    px.poetx_mx4_dequantize(Q, W)
+    if act == "mx4":
+        Xr = torch.empty_like(X)
+        px.poetx_mx4_dequantize(quantised(X), Xr)
+    desc = px.make_grouped_desc(m, n, groups, rows, px.BF16, px.GROUPED_W_MX4 | (px.GROUPED_X_MX4 if act == "mx4" else 0))
+    ws = torch.full((px.poetx_grouped_workspace_bytes(desc),), 255, dtype=torch.uint8, device="cuda")
+    Z, dX = torch.empty((rows, n), dtype=torch.bfloat16, device="cuda"), torch.empty((rows, m), dtype=torch.bfloat16, device="cuda")
+    px.poetx_grouped_fwd(desc, X, Q, off, Z, ws)
+    px.poetx_grouped_bwd_input(desc, dZ, Q, off, dX, ws)
+    W = W.view(groups, n, m)
+    assert within(Z, *reference("fwd", Xr, W, counts), m, "bf16")
+    assert within(dX, *reference("input", dZ, W, counts), n, "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_grouped_offsets_past_32_bits(lib, dtype):
+    """Rows further apart than 2^31 elements (and 2^32 bytes) from the first one."""
+    ld, rows, m, n = 1 << 15, 70000, 64, 128
+    flat = torch.empty(rows * ld, dtype=DT[dtype], device="cuda")
+    X = flat.view(rows, ld)[:, :m]
+    tail = 300
+    X[-tail:] = torch.randn((tail, m), device="cuda").to(DT[dtype])
+    W = torch.randn((3, n, m), device="cuda").to(DT[dtype])
+    off = torch.tensor([rows - tail, rows - 200, rows - 200, rows], dtype=torch.int32, device="cuda")
+    Z = flat.view(rows, ld)[:, 1024: 1024 + n]      # the span of the output overlaps the input's: refused
+    desc = px.make_grouped_desc(m, n, 3, rows, CODE[dtype])
+    with pytest.raises(px.PoetxError):
+        px.poetx_grouped_fwd(desc, X, W, off, Z)
+    Z = torch.zeros((rows, n), dtype=DT[dtype], device="cuda")
+    px.poetx_grouped_fwd(desc, X, W, off, Z)
+    counts = [100, 0, 200]
+    assert within(Z[-tail:], *reference("fwd", X[-tail:], W, counts), m, dtype) and not bool(Z[:-tail].any())
+    dW = torch.empty((3, n, m), device="cuda")
+    px.poetx_grouped_bwd_weight(desc, X, Z, off, dW, False)
+    assert within(dW, *reference("weight", X[-tail:], None, counts, Z[-tail:]), tail, "f32")
+    dX = flat.view(rows, ld)[:, 2048: 2048 + m]
+    px.poetx_grouped_bwd_input(desc, Z, W, off, dX)
+    assert within(dX[-tail:], *reference("input", Z[-tail:], W, counts), n, dtype)
+    if dtype == "bf16":
+        Q = quantised(X[-tail:])
+        rows_q = (1 << 32) // 4096 + 3                  # more than 2^32 codes
+        big = torch.zeros((rows_q, 4096), dtype=torch.bfloat16, device="cuda")
+        big[-tail:, :m] = X[-tail:]
+        Qb = quantised(big)
+        del big
+        back = torch.empty((rows_q, 4096), dtype=torch.bfloat16, device="cuda")
+        px.poetx_mx4_dequantize(Qb, back)
+        want = torch.empty((tail, m), dtype=torch.bfloat16, device="cuda")
+        px.poetx_mx4_dequantize(Q, want)
+        assert torch.equal(back[-tail:, :m], want) and not bool(back[-1, m:].any())
+
+
+@pytest.mark.parametrize("weight", ["dense", "mx4", "both"])
+def test_grouped_in_a_graph(lib, weight):
+    """Captured once, replayed with other rows, offsets and ids in the same buffers."""
+    m, n, groups, tokens, k = 256, 384, 6, 500, 2
+    rows = tokens * k
+    g = torch.Generator(device="cuda").manual_seed(2)
+    W = (torch.randn((groups, n, m), device="cuda", generator=g) * 0.05).bfloat16()
+    Wx = W if weight == "dense" else quantised(W.view(groups * n, m))
+    desc = px.make_grouped_desc(m, n, groups, rows, px.BF16, {"dense": 0, "mx4": px.GROUPED_W_MX4, "both": px.GROUPED_W_MX4 | px.GROUPED_X_MX4}[weight])
+    ws = torch.empty(max(256, px.poetx_grouped_workspace_bytes(desc)), dtype=torch.uint8, device="cuda")
+    ows = torch.empty(max(256, px.poetx_group_order_workspace_bytes(rows, groups)), dtype=torch.uint8, device="cuda")
+    ids, x = torch.zeros(rows, dtype=torch.int32, device="cuda"), torch.zeros((rows, m), dtype=torch.bfloat16, device="cuda")
+    off, order = torch.zeros(groups + 1, dtype=torch.int32, device="cuda"), torch.zeros(rows, dtype=torch.int32, device="cuda")
+    Z, dX = torch.zeros((rows, n), dtype=torch.bfloat16, device="cuda"), torch.zeros((rows, m), dtype=torch.bfloat16, device="cuda")
+
+    def calls():
+        px.poetx_group_order(ids, off, order, ows)
+        px.poetx_grouped_fwd(desc, x, Wx, off, Z, ws)
+        px.poetx_grouped_bwd_input(desc, Z, Wx, off, dX, ws)
+
+    calls()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for i in range(4):
+        ids.copy_(torch.randint(0, groups, (rows,), device="cuda", generator=g).int())
+        x.copy_(torch.randn((rows, m), device="cuda", generator=g))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (off, order, Z, dX)]
+        for t in (off, order, Z, dX):
+            t.zero_()
+        calls()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, (off, order, Z, dX))) and float(dX.abs().max()) > 0
+
+
+def test_experts_example(lib):
+    """The example layer in fp32 against torch autograd in float64, and its 4-bit forms' command line."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "experts.py")
+    spec = importlib.util.spec_from_file_location("experts_example", path)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    tokens, d, f, E, k = 50, 64, 96, 5, 2
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    W1, W2 = (torch.stack([ex.merged(torch.randn(s, device="cuda", generator=gen) * 0.1, 16, 3, 0.02, gen) for _ in range(E)]) for s in ((f, d), (d, f)))
+    x, dout = (torch.randn((tokens, d), device="cuda", generator=gen) for _ in range(2))
+    ids = torch.randint(-1, E, (tokens, k), device="cuda", generator=gen)
+    gates = torch.rand((tokens, k), device="cuda", generator=gen)
+    layer = ex.Experts(W1, W2, tokens, k)
+    out = layer.forward(x, ids, gates)
+    dx, dgate, (dW1, dW2) = layer.backward(dout, weights=True)
+    leaves = [t.double().requires_grad_() for t in (x, gates, W1, W2)]
+    xr, gr, W1r, W2r = leaves
+    e = ids.clamp(min=0)
+    h = torch.einsum("tkfd,td->tkf", W1r[e], xr).clamp(min=0) ** 2
+    ref = (torch.einsum("tkdf,tkf->tkd", W2r[e], h) * (gr * (ids >= 0)).unsqueeze(2)).sum(1)
+    ref.backward(dout.double())
+    for got, want in ((out, ref), (dx, xr.grad), (dgate, gr.grad), (dW1, W1r.grad), (dW2, W2r.grad)):
+        assert float((got.double() - want.detach()).abs().max()) <= 1e-5 * float(want.detach().abs().max())
+    small = ["--tokens", "70", "--experts", "4", "--d", "256", "--hidden", "192", "--block", "64", "--steps", "1"]
+    for more in ([], ["--activations", "mx4"], ["--weights", "dense"]):
+        assert ex.main(small + more) == 0
