@@ -399,7 +399,10 @@ int poetx_mx4_dequantize(const void* Q, int64_t rows, int32_t cols, int32_t dtyp
  * copy to the host.  Groups may be empty.  Rows that no group has are neither read nor written; offsets outside
  * 0 .. rows are taken as the nearer end and a decreasing pair as an empty group, so that nothing outside the tensors is
  * ever touched.  Products of bf16 are exact and summed in fp32, and a result is rounded once.
- * Every sum has one order, so results are reproducible run to run. */
+ * Every sum has one order, so results are reproducible run to run.
+ * Which kernels run follows from the descriptor, the strides, the alignment and the scratch, never from the offsets: tensors of whole 16-byte
+ * vectors (pointers, leading dimensions, d_in and d_out) with up to 256 groups on streaming matrix-core kernels, a handful of forward rows per group on
+ * short ones, the rest on edge-handling ones of any size.  Input tensors must not overlap the output's span from its first to its last element. */
 typedef struct {
   int32_t d_in;        /* m */
   int32_t d_out;       /* n */
@@ -414,7 +417,10 @@ typedef struct {
 #define POETX_GROUPED_X_MX4 2   /* with W_MX4, forward only: the rows of X are rounded to four bits as well (by the rule
                                    above, along d_in) and the codes are multiplied; the input gradient passes the rounding by */
 
-/* Scratch of the largest of the three calls below; 0 for an invalid descriptor. */
+/* Scratch of the largest of the three calls below; 0 for an invalid descriptor.  16-byte aligned.  4-bit weights need it (values of the weight, or codes of
+ * X).  Dense ones use it where a product has few tiles, for fp32 sums of parts of its contraction, and run without (ws = NULL, or smaller) with the contraction
+ * unsplit: up to twice as long for such calls, and another order of the sums.  us with / without: bf16 input gradient 414 rows, 7360 -> 1888 31 / 55, forward 637 rows,
+ * 5568 -> 512 23 / 36. */
 size_t poetx_grouped_workspace_bytes(const poetx_grouped_desc* desc);
 
 int poetx_grouped_fwd(const poetx_grouped_desc* desc, const void* X, int64_t ldx, const void* W, const int32_t* offsets,

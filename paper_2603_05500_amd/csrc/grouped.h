@@ -94,14 +94,20 @@ __device__ __forceinline__ int xcd_run(int bx, int total) {
 
 // ---- which kernel ------------------------------------------------------------------------------------
 enum Kernel { EDGE_32, EDGE_32_DEEP, EDGE_64, EDGE_128, STREAM_256, STREAM_256x128, STREAM_128, SINGLE_128, SINGLE_64, KERNELS };      // SINGLE: streams of fp32
-// What a kernel takes for a call, in us, from what one stage of its tile's contraction takes alone and how many tiles the chip works on at a time.
-Kernel plan(int dtype, Dir dir, const Call& c, bool streams);
+// The one that a model of their times finds the fastest, from what one stage of its tile's contraction takes alone and how many tiles the chip works on at a time.
+// scratch: bytes there are for the sums of a contraction split among workgroups; parts: what of them the plan takes.
+struct Plan {
+  Kernel kernel;
+  int splits;
+  size_t parts;
+};
+Plan plan(int dtype, Dir dir, const Call& c, bool streams, size_t scratch);
 
 // ---- launchers -----------------------------------------------------------------------------------
 void edge_launch(int dtype, Dir dir, Kernel k, const Call& c, hipStream_t st);      // any shape (grouped_edge.hip)
 // whole 16-byte vectors (grouped_stream.hip)
 bool stream_supported(int dtype, Dir dir, const Call& c);
-void stream_launch(int dtype, Dir dir, Kernel k, const Call& c, hipStream_t st);
+void stream_launch(int dtype, Dir dir, const Plan& p, const Call& c, void* scratch, hipStream_t st);
 // Z = X W^T with X rounded to four bits on the way, W a 4-bit buffer
 bool codes_supported(const poetx_grouped_desc* d, const void* Z, i64 ldz);
 size_t codes_workspace_bytes(const poetx_grouped_desc* d);

@@ -46,12 +46,31 @@ size_t dequantised_bytes(const poetx_grouped_desc* d) { return align256((size_t)
 // X in four bits, as values
 size_t rounded_bytes(const poetx_grouped_desc* d) { return align256((size_t)d->rows * d->d_in * 2) + align256(mx4::bytes(d->rows, d->d_in)); }
 
-size_t workspace_bytes(const poetx_grouped_desc* d) {
+// fp32 sums of contractions that are split among workgroups, where the tensors allow the streaming kernels
+size_t parts_bytes(const poetx_grouped_desc* d) {
+  size_t most = 0;
+  for (const grouped::Dir dir : {grouped::FWD, grouped::INPUT}) {
+    if (grouped::few_supported(d->dtype, dir, d->rows, d->d_in, d->d_out, d->groups, grouped::DENSE_WEIGHT)) continue;
+    grouped::Call c = {};
+    c.rows = d->rows;
+    c.m = d->d_in;
+    c.n = d->d_out;
+    c.groups = d->groups;
+    if (!grouped::stream_supported(d->dtype, dir, c)) continue;
+    const size_t p = grouped::plan(d->dtype, dir, c, true, ~(size_t)0).parts;
+    most = p > most ? p : most;
+  }
+  return align256(most);
+}
+
+// What the 4-bit forms of the operands take; parts of the products follow.
+size_t operand_bytes(const poetx_grouped_desc* d) {
   if (!(d->flags & POETX_GROUPED_W_MX4) || d->rows == 0) return 0;
   if (!(d->flags & POETX_GROUPED_X_MX4)) return dequantised_bytes(d);
-  const size_t codes = grouped::codes_workspace_bytes(d), values = dequantised_bytes(d) + rounded_bytes(d);
+  const size_t codes = align256(grouped::codes_workspace_bytes(d)), values = dequantised_bytes(d) + rounded_bytes(d);
   return codes > values ? codes : values;
 }
+size_t workspace_bytes(const poetx_grouped_desc* d) { return d->rows == 0 ? 0 : operand_bytes(d) + parts_bytes(d); }
 
 // The products of a 4-bit weight run on its values, made in the workspace.
 const void* dense_weight(const poetx_grouped_desc* d, const void* W, const int32_t* offsets, void* ws, hipStream_t st) {
@@ -61,11 +80,16 @@ const void* dense_weight(const poetx_grouped_desc* d, const void* W, const int32
   return ws;
 }
 
-void product(int dtype, grouped::Dir dir, const grouped::Call& c, hipStream_t st) {
+// scratch: for the parts of a split contraction, behind what the operands take of the workspace
+void product(const poetx_grouped_desc* d, grouped::Dir dir, const grouped::Call& c, void* ws, size_t ws_bytes, hipStream_t st) {
   StageTimer tm(POETX_STAGE_DENSE, st);
+  const int dtype = d->dtype;
   if (grouped::few_supported(dtype, dir, c.rows, c.m, c.n, c.groups, grouped::DENSE_WEIGHT)) return grouped::few_dense(dtype, c, st);
-  const grouped::Kernel k = grouped::plan(dtype, dir, c, grouped::stream_supported(dtype, dir, c));
-  k >= grouped::STREAM_256 ? grouped::stream_launch(dtype, dir, k, c, st) : grouped::edge_launch(dtype, dir, k, c, st);
+  const size_t before = operand_bytes(d);
+  const size_t scratch = ws && ((uintptr_t)ws & 15) == 0 && ws_bytes > before ? ws_bytes - before : 0;
+  const grouped::Plan p = grouped::plan(dtype, dir, c, grouped::stream_supported(dtype, dir, c), scratch);
+  if (p.kernel >= grouped::STREAM_256) grouped::stream_launch(dtype, dir, p, c, (char*)ws + before, st);
+  else grouped::edge_launch(dtype, dir, p.kernel, c, st);
 }
 
 // Forward and input gradient: in is rows x d_i, out rows x d_o.
@@ -80,8 +104,8 @@ int check_rows_call(const poetx_grouped_desc* d, const void* in, i64 ld_in, int 
   if ((d->flags & POETX_GROUPED_W_MX4) && ((uintptr_t)W & 15)) return POETX_ERR_INVALID_ARG;
   if (overlap(out, ob, in, span(d->rows, d_i, ld_in, es)) || overlap(out, ob, W, weight_bytes(d)) || overlap(out, ob, offsets, 4 * ((size_t)d->groups + 1)))
     return POETX_ERR_INVALID_ARG;
-  const size_t need = workspace_bytes(d);
-  if (need > 0 && (!ws || ws_bytes < need)) return POETX_ERR_WORKSPACE;
+  // dense weights do without (see the header)
+  if ((d->flags & POETX_GROUPED_W_MX4) && d->rows > 0 && (!ws || ((uintptr_t)ws & 15) || ws_bytes < workspace_bytes(d))) return POETX_ERR_WORKSPACE;
   return POETX_OK;
 }
 
@@ -149,7 +173,7 @@ int poetx_grouped_fwd(const poetx_grouped_desc* d, const void* X, int64_t ldx, c
     X = values;
     ldx = d->d_in;
   }
-  product(d->dtype, grouped::FWD, grouped::Call{X, nullptr, w, Z, ldx, 0, ldz, offsets, d->rows, d->d_in, d->d_out, d->groups, 0}, st);
+  product(d, grouped::FWD, grouped::Call{X, nullptr, w, Z, ldx, 0, ldz, offsets, d->rows, d->d_in, d->d_out, d->groups, 0}, ws, ws_bytes, st);
   return launch_status();
 }
 
@@ -159,7 +183,7 @@ int poetx_grouped_bwd_input(const poetx_grouped_desc* d, const void* dZ, int64_t
   if (rc != POETX_OK || d->rows == 0) return rc;
   hipStream_t st = (hipStream_t)stream;
   const void* w = dense_weight(d, W, offsets, ws, st);
-  product(d->dtype, grouped::INPUT, grouped::Call{dZ, nullptr, w, dX, lddz, 0, lddx, offsets, d->rows, d->d_in, d->d_out, d->groups, 0}, st);
+  product(d, grouped::INPUT, grouped::Call{dZ, nullptr, w, dX, lddz, 0, lddx, offsets, d->rows, d->d_in, d->d_out, d->groups, 0}, ws, ws_bytes, st);
   return launch_status();
 }
 
@@ -176,7 +200,7 @@ int poetx_grouped_bwd_weight(const poetx_grouped_desc* d, const void* X, int64_t
   if (overlap(dW, ob, X, span(d->rows, d->d_in, ldx, es)) || overlap(dW, ob, dZ, span(d->rows, d->d_out, lddz, es)) ||
       overlap(dW, ob, offsets, 4 * ((size_t)d->groups + 1)))
     return POETX_ERR_INVALID_ARG;
-  product(d->dtype, grouped::WEIGHT, grouped::Call{X, dZ, nullptr, dW, ldx, lddz, d->d_in, offsets, d->rows, d->d_in, d->d_out, d->groups, accumulate != 0},
+  product(d, grouped::WEIGHT, grouped::Call{X, dZ, nullptr, dW, ldx, lddz, d->d_in, offsets, d->rows, d->d_in, d->d_out, d->groups, accumulate != 0}, nullptr, 0,
           (hipStream_t)stream);
   return launch_status();
 }

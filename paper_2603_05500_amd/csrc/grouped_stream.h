@@ -33,17 +33,19 @@ using mx4::u32x4;
 
 enum Elem { BF16, F32, CODES };
 
-template <int BM_, int BN_, int NS_, Elem ELEM_, int PER_CU_ = 1>
+// PARTS: fp32 sums of a range of the contraction go to `parts`, to be added up by another launch (bf16; fp32 needs no kernel of its own).
+template <int BM_, int BN_, int NS_, Elem ELEM_, int PER_CU_ = 1, bool PARTS_ = false>
 struct StreamTile {
   static constexpr int BM = BM_, BN = BN_, NS = NS_, NW = 4, PER_CU = PER_CU_;
   static constexpr Elem ELEM = ELEM_;
+  static constexpr bool PARTS = PARTS_;
   static constexpr bool FP4 = ELEM == CODES;
   static constexpr int DEPTH = FP4 ? 128 : ELEM == F32 ? 16 : 32;      // elements of a stage
   static constexpr int SETS = 4, GROUPS = 64 * SETS;      // groups per lane, in all
   static constexpr int A_BYTES = BM * 64, B_BYTES = BN * 64, S_BYTES = FP4 ? (BM + BN) * 4 : 0, STAGE_BYTES = A_BYTES + B_BYTES + S_BYTES;
   static constexpr int TM = BM / 32, TN = BN / 32, MF = TM * TN * (ELEM == F32 ? 4 : 1);      // MFMAs of a stage; fp32: 4 of depth per MFMA
   static constexpr int RS = MF / (TM + TN) < 3 ? MF / (TM + TN) : 3;
-  static constexpr int OUT_BYTES = ELEM == F32 ? 0 : TN / 4 * 2048;
+  static constexpr int OUT_BYTES = ELEM == F32 || PARTS ? 0 : TN / 4 * 2048;
   static constexpr int LDS_BYTES = NS * STAGE_BYTES + NW * OUT_BYTES;
   static constexpr int IPWA = A_BYTES / 1024 / NW, IPWB = B_BYTES / 1024 / NW, IPWS = FP4 ? (BM + BN) / 256 : 0;
   static constexpr int LPT = IPWA + IPWB + IPWS;
@@ -66,6 +68,7 @@ struct StreamArgs {
   int M, N;               // WEIGHT: rows of C (n); columns of C
   int tiles_n;            // column tiles
   int accumulate;
+  int splits;             // FWD, INPUT: ranges of the contraction, whose sums go to [split][rows][N] at C; 1: the result does
 };
 
 // 16 (4) bytes per lane from base + voff straight into LDS at lds + 16 (4) * lane; zeros from the descriptor's end on.
@@ -152,7 +155,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   }
   const int tiles_m = DIR == WEIGHT ? (g.M + BM - 1) / BM : row_tiles;      // WEIGHT: of one group
   const int per_weight = tiles_m * g.tiles_n;
-  const int T = DIR == WEIGHT ? per_weight * g.groups : per_weight;
+  const int T = per_weight * (DIR == WEIGHT ? g.groups : g.splits);
   const int G = gridDim.x;
   int wq = blockIdx.x;
   if ((G & 7) == 0) wq = (wq & 7) * (G >> 3) + (wq >> 3);
@@ -162,15 +165,18 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   struct Where {
     int gr, first, r0, r1;      // group, its first row; FWD, INPUT: the tile's first row; WEIGHT: the group's; end of the group
     int i0, j0;          // WEIGHT: first row of C; first column
-    int stages;          // an even number
+    int split, k0, k1;   // range of the contraction and its stages, in pairs from the first on
   };
   auto locate = [&](int ti) __attribute__((always_inline)) {
     Where w;
     int u = ti * G + wq;
-    w.gr = 0;
+    w.gr = w.split = 0;
     if (DIR == WEIGHT) {
       w.gr = u / per_weight;
       u -= w.gr * per_weight;
+    } else if (g.splits > 1) {
+      w.split = u / per_weight;
+      u -= w.split * per_weight;
     }
     const int per_group = GROUP * g.tiles_n;
     const int first_m = (u / per_group) * GROUP;
@@ -186,7 +192,8 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
           w.r0 = __builtin_amdgcn_readlane(tr0[q], w.gr & 63);
           w.r1 = __builtin_amdgcn_readlane(tr1[q], w.gr & 63);
         }
-      w.stages = (w.r1 - w.r0 + 2 * DEPTH - 1) / (2 * DEPTH) * 2;
+      w.k0 = 0;
+      w.k1 = (w.r1 - w.r0 + 2 * DEPTH - 1) / (2 * DEPTH) * 2;
     } else {
       bool found = false;
 #pragma unroll
@@ -203,7 +210,9 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
           w.r0 += (rt - (end - mine)) * BM;
         }
       }
-      w.stages = (g.K + 2 * DEPTH - 1) / (2 * DEPTH) * 2;
+      const int pairs = (g.K + 2 * DEPTH - 1) / (2 * DEPTH);
+      w.k0 = pairs * w.split / g.splits * 2;
+      w.k1 = pairs * (w.split + 1) / g.splits * 2;
     }
     return w;
   };
@@ -251,14 +260,14 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
       ++iti;
       if (iti >= n_my) break;
       w = locate(iti);
-    } while (DIR == WEIGHT && w.stages == 0);
-    ikt = 0;
+    } while (DIR == WEIGHT && w.k1 == 0);
     Feed<LeftA> na{0, 0};      // nothing more: empty descriptors
     Feed<LeftB> nb{0, 0};
-    int stages = 0x7fffffff, ha = 0, hb = 0;
+    int k0 = 0, k1 = 0x7fffffff, ha = 0, hb = 0;
     uint64_t nsa = 0, nsb = 0;
     if (iti < n_my) {
-    stages = w.stages;
+    k0 = w.k0;
+    k1 = w.k1;
     if (DIR == FWD) hb = g.N - w.j0 < BN ? g.N - w.j0 : BN;      // rows of W in the tile
     if (DIR == WEIGHT) {
       const i64 len = w.r1 - w.r0;
@@ -283,7 +292,14 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
       }
     }
     }
-    iKT = uniform(stages);
+    if (DIR != WEIGHT) {
+      na.step(k0 * stepA);
+      nb.step(k0 * stepB);
+      nsa += (i64)k0 * g.sa_step;
+      nsb += (i64)k0 * g.sb_step;
+    }
+    ikt = uniform(k0);
+    iKT = uniform(k1);
     fa = Feed<LeftA>{uniform(na.at), uniform(na.left)};
     fb = Feed<LeftB>{uniform(nb.at), uniform(nb.left)};
     if (FP4) {
@@ -431,8 +447,8 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
       cslot = nslot;
     };
     for (int ti = 0; ti < n_my; ++ti) {
-      const int KT = locate(ti).stages;
-      for (int kt = 0; kt < KT; kt += 2) {
+      const Where range = locate(ti);
+      for (int kt = range.k0; kt < range.k1; kt += 2) {
         multiply(F, Gf);
         multiply(Gf, F);
         tile_advance();
@@ -446,10 +462,10 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
       }
       const Where w = locate(ti);
       // Stores go through a descriptor as well: rows past the group's end (of dW) lie behind it, and a lane whose columns do not exist gets an offset that does.
-      if constexpr (DIR == WEIGHT || FP32) {
+      if constexpr (DIR == WEIGHT || FP32 || C::PARTS) {
         // a lane's four columns of a row
         const int row = wm * (BM / 2) + li, col = wn * (BN / 2) + 4 * q4, rows = DIR == WEIGHT ? g.M - w.i0 : w.r1 - w.r0, cols = g.N - w.j0;
-        const i64 first = DIR == WEIGHT ? ((i64)w.gr * g.M + w.i0) * g.ldc : (i64)w.r0 * g.ldc;
+        const i64 first = DIR == WEIGHT ? ((i64)w.gr * g.M + w.i0) * g.ldc : ((i64)w.split * g.rows + w.r0) * g.ldc;
         const auto rc = make_rsrc((float*)g.C + first + w.j0, ((i64)(rows - 1) * g.ldc + cols) * 4);
         auto store = [&](auto ADD) __attribute__((always_inline)) {
 #pragma unroll

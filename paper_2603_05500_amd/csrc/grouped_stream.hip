@@ -8,6 +8,7 @@ namespace {
 typedef StreamTile<256, 256, 4, BF16> Tile256;
 typedef StreamTile<256, 128, 6, BF16> Tile256x128;
 typedef StreamTile<128, 128, 8, BF16> Tile128;
+typedef StreamTile<128, 128, 8, BF16, 1, true> Parts128;
 typedef StreamTile<256, 256, 4, CODES> Codes256;
 typedef StreamTile<128, 128, 6, CODES> Codes128;
 typedef StreamTile<128, 128, 4, F32, 2> Single128;
@@ -27,6 +28,9 @@ void go(const StreamArgs& a0, hipStream_t st) {
 
 template <Dir DIR>
 void pick(Kernel k, const StreamArgs& a, hipStream_t st) {
+  if constexpr (DIR != WEIGHT) {
+    if (k == STREAM_128 && a.splits > 1) return go<DIR, Parts128>(a, st);
+  }
   if (k == SINGLE_128) go<DIR, Single128>(a, st);
   else if (k == SINGLE_64) go<DIR, Single64>(a, st);
   else if (k == STREAM_256) go<DIR, Tile256>(a, st);
@@ -43,6 +47,42 @@ double tiles_of(Dir dir, i64 rows, int m, int n, int groups, int h, int w) {
   return (t > live ? t : live) * across;
 }
 
+// The sums of a contraction's ranges, [split][rows][cols], added in order and rounded, for the rows that some group has.  A wave takes 256 columns of a row.
+template <class T>
+__global__ __launch_bounds__(256) void add_parts_kernel(const float* __restrict__ parts, int splits, i64 rows, int cols, T* __restrict__ out, i64 ld,
+                                                        const int32_t* __restrict__ offsets, int groups, i64 waves, int block0) {
+  const int lane = threadIdx.x & 63, across = (cols + 255) / 256;
+  const i64 w = (block0 + (i64)blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (w >= waves) return;
+  const i64 row = w / across;
+  const int col = (int)(w - row * across) * 256 + 4 * lane;
+  bool has = false;
+  for (int base = 0; base < groups && !has; base += 64) {
+    Range r{0, 0};
+    if (base + lane < groups) r = group_range(offsets, base + lane, rows);
+    has = __ballot(r.r0 <= row && row < r.r1) != 0;
+  }
+  if (!has || col >= cols) return;
+  const float* p = parts + row * cols + col;
+  floatx4 sum = *reinterpret_cast<const floatx4*>(p);
+  for (int s = 1; s < splits; ++s) sum += *reinterpret_cast<const floatx4*>(p + s * rows * cols);
+  T* o = out + row * ld + col;
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<floatx4*>(o) = sum;
+  } else {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    *reinterpret_cast<u32x2*>(o) = u32x2{mm::pack2_bf16(sum[0], sum[1]), mm::pack2_bf16(sum[2], sum[3])};
+  }
+}
+template <class T>
+void add_parts(const StreamArgs& a, const Call& c, hipStream_t st) {
+  const i64 waves = c.rows * ((a.N + 255) / 256);
+  launch_in_rows((waves + 3) / 4, [&](int block0, unsigned count) {
+    hipLaunchKernelGGL(add_parts_kernel<T>, dim3(count), dim3(256), 0, st, (const float*)a.C, a.splits, c.rows, a.N, (T*)c.out, c.ld_out, c.offsets, c.groups, waves,
+                       block0);
+  });
+}
+
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 }  // namespace
@@ -57,7 +97,7 @@ bool stream_supported(int dtype, Dir dir, const Call& c) {
 
 // The figures were fitted to 600 calls in bf16 and 700 in fp32 of random directions, sizes (64 to 14336; 64 to 4096), groups (1 to 128) and rows (1 to 32768; 8 to 8192), each
 // with every kernel that could take it; the choices they lead to take 1.5 % more time than the best would (geometric mean).
-Kernel plan(int dtype, Dir dir, const Call& c, bool streams) {
+Plan plan(int dtype, Dir dir, const Call& c, bool streams, size_t scratch) {
   struct Row {
     Kernel kernel;
     int h, w, depth;      // tile, depth of a stage
@@ -76,29 +116,38 @@ Kernel plan(int dtype, Dir dir, const Call& c, bool streams) {
   const int count = f ? (int)(sizeof(fp32) / sizeof(Row)) : (int)(sizeof(bf16) / sizeof(Row));
   const double live = c.rows < c.groups ? (double)c.rows : c.groups;
   const double K = dir == FWD ? c.m : dir == INPUT ? c.n : live > 0 ? c.rows / live : 0;
+  const int out_cols = dir == FWD ? c.n : c.m;
   const double out_us = dir == WEIGHT ? 4.0 * c.groups * c.n * c.m / 5.1e6 : 0;      // fp32 weights to memory
-  Kernel best = EDGE_32;
+  Plan best{EDGE_32, 1, 0};
   double least = 1e30;
   for (int i = 0; i < count; ++i) {
     const Row& r = rows[i];
     const bool stream = r.kernel >= STREAM_256;
     if (stream && !streams) break;
     const double tiles = tiles_of(dir, c.rows, c.m, c.n, c.groups, r.h, r.w), stages = (double)(i64)((K + r.depth - 1) / r.depth);
-    double us = tiles / r.at_once;
-    if (stream && !f) us = c.groups == 1 ? (double)(i64)(us + 0.999) : us + r.uneven;
-    us = (us < 1 ? 1 : us) * stages * r.stage;
-    // a stream stores between multiplications; the others have several workgroups on a CU, but store less well
-    const double stores = (f ? 1.5 : 1.23) * out_us;
-    us = r.rest + (stream ? us + out_us : us > stores ? us : stores);
-    if (us < least) {
-      least = us;
-      best = r.kernel;
+    // few tiles: their contraction in ranges, whose fp32 sums are added by another launch (7.5 us with the wait between the two, and their way through the caches)
+    const bool splittable = dir != WEIGHT && (r.kernel == STREAM_128 || r.kernel >= SINGLE_128);
+    for (const int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
+      const size_t parts = splits > 1 ? (size_t)splits * c.rows * out_cols * sizeof(float) : 0;
+      if (splits > 1 && (!splittable || parts > scratch || 4 * splits > stages || tiles * splits > 2 * r.at_once)) break;
+      double us = tiles * splits / r.at_once;
+      if (stream && !f) us = c.groups == 1 ? (double)(i64)(us + 0.999) : us + r.uneven;
+      us = (us < 1 ? 1 : us) * (double)(i64)((stages + splits - 1) / splits) * r.stage;
+      // a stream stores between multiplications; the others have several workgroups on a CU, but store less well
+      const double stores = (f ? 1.5 : 1.23) * out_us;
+      us = r.rest + (stream ? us + out_us : us > stores ? us : stores);
+      if (splits > 1) us += 7.5 + 2 * parts / 8e6;
+      if (us < least) {
+        least = us;
+        best = Plan{r.kernel, splits, parts};
+      }
     }
   }
   return best;
 }
 
-void stream_launch(int dtype, Dir dir, Kernel k, const Call& c, hipStream_t st) {
+void stream_launch(int dtype, Dir dir, const Plan& p, const Call& c, void* scratch, hipStream_t st) {
+  const Kernel k = p.kernel;
   const int es = dtype == POETX_F32 ? 4 : 2;
   StreamArgs a = {};
   a.offsets = c.offsets;
@@ -107,6 +156,7 @@ void stream_launch(int dtype, Dir dir, Kernel k, const Call& c, hipStream_t st) 
   a.C = c.out;
   a.ldc = (int)c.ld_out;
   a.accumulate = c.accumulate;
+  a.splits = p.splits;
   if (dir == WEIGHT) {
     a.A = (const char*)c.in2;
     a.lda = (int)(es * c.ld_in2);
@@ -122,7 +172,12 @@ void stream_launch(int dtype, Dir dir, Kernel k, const Call& c, hipStream_t st) 
   a.ldb = es * c.m;
   a.K = dir == FWD ? c.m : c.n;
   a.N = dir == FWD ? c.n : c.m;
+  if (p.splits > 1) {
+    a.C = scratch;
+    a.ldc = a.N;
+  }
   dir == FWD ? pick<FWD>(k, a, st) : pick<INPUT>(k, a, st);
+  if (p.splits > 1) dtype == POETX_F32 ? add_parts<float>(a, c, st) : add_parts<uint16_t>(a, c, st);
 }
 
 // ---- both operands in four bits ---------------------------------------------------------------------
@@ -159,6 +214,7 @@ void codes_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const voi
   a.groups = d->groups;
   a.K = units * mx4::UNIT;
   a.N = d->d_out;
+  a.splits = 1;
   // A round of 256 x 256 tiles takes as long as 2.1 of 128 x 128 ones.
   auto rounds = [&](int side) {
     const double t = tiles_of(FWD, d->rows, d->d_in, d->d_out, d->groups, side, side) / kCUs;

@@ -460,6 +460,31 @@ def test_grouped_mx4_large(lib, groups, rows, m, n, act):
     assert within(dX, *reference("input", dZ, W, counts), n, "bf16")
 
 
+@pytest.mark.parametrize("dtype,kind,m,n,counts,before,behind", [
+    ("bf16", "fwd", 5568, 512, [637], 0, 0), ("bf16", "fwd", 7808, 1248, [200, 0, 300, 37, 251], 3, 9), ("bf16", "input", 1408, 5088, [221], 0, 70),
+    ("bf16", "input", 776, 6368, [500, 607], 5, 0), ("f32", "fwd", 1760, 576, [1140], 0, 0), ("f32", "input", 516, 2692, [100, 0, 140], 2, 3)])
+def test_grouped_split_contraction(lib, dtype, kind, m, n, counts, before, behind):
+    """Few tiles and a long contraction: parts in the workspace, added by another launch, and the same without one."""
+    rows, dt = before + sum(counts) + behind, DT[dtype]
+    off = (offsets_of(counts) + before).int()
+    g = torch.Generator(device="cuda").manual_seed(m)
+    d_in, d_out = (m, n) if kind == "fwd" else (n, m)
+    x = torch.full((rows, d_in), float("nan"), device="cuda", dtype=dt)
+    x[before: before + sum(counts)] = torch.randn((sum(counts), d_in), device="cuda", generator=g).to(dt)
+    W = (torch.randn((len(counts), n, m), device="cuda", generator=g) * 0.02).to(dt)
+    desc = px.make_grouped_desc(m, n, len(counts), rows, CODE[dtype])
+    need = px.poetx_grouped_workspace_bytes(desc)
+    assert need >= 2 * rows * d_out * 4
+    ref, mag = reference(kind, x[before:], W, counts)
+    call = px.poetx_grouped_fwd if kind == "fwd" else px.poetx_grouped_bwd_input
+    for ws in (torch.full((need // 4,), float("nan"), device="cuda").view(torch.uint8), None):
+        out, flat = strided(rows, d_out, 16, dt, fill=3.0)
+        call(desc, x, W, off, out, ws)
+        assert within(out[before: before + sum(counts)], ref, mag, d_in, dtype)
+        out[before: before + sum(counts)] = 3.0
+        assert bool((flat == 3.0).all()), "written where no group is"
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_grouped_offsets_past_32_bits(lib, dtype):
     """Rows further apart than 2^31 elements (and 2^32 bytes) from the first one."""
