@@ -126,6 +126,9 @@ __device__ __forceinline__ void in_turn(std::integer_sequence<int, I...>, const 
 template <Dir DIR, class C>
 __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   constexpr bool FP4 = C::FP4, FP32 = C::ELEM == F32, A_K = DIR != WEIGHT, B_K = DIR == FWD;
+  // WIDE: rows come 64 deep, whole 128-byte lines.  Two stages are a unit, which arrives in two halves of its rows, one per stage; as it is needed as a whole, and its
+  // place is free, with its first stage, the last half is in flight a stage less, and the ring has to be deep.  As in the dense product, 64-byte pieces would ask for every line twice.
+  constexpr bool WIDE = A_K && B_K && C::ELEM == BF16 && C::NS >= 6;
   constexpr int DEPTH = C::DEPTH, ES = FP32 ? 4 : 2;      // bytes of an element (not of a code)
   static_assert(!FP4 || DIR == FWD, "codes are contracted along their rows");
   constexpr int BM = C::BM, BN = C::BN, NS = C::NS, STAGE_BYTES = C::STAGE_BYTES, A_BYTES = C::A_BYTES;
@@ -222,6 +225,10 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   // Rows along the output: where chunk c of row k lies.  bf16: as the transposing loads like it; fp32: a fragment's four rows 4 q + e, q = 0 .. 3, in four different 64 bytes.
   auto strided_chunk = [&](int c, int k) __attribute__((always_inline)) { return FP32 ? c ^ (4 * ((k >> 2) & 3)) : dense::kx16_chunk(c, k); };
   auto slot_offset = [&](int slot, bool kmajor, int width, int ld) __attribute__((always_inline)) {
+    if (WIDE) {
+      const int r = slot >> 3, c = (slot & 7) ^ ((r >> 1) & 7);
+      return (uint32_t)(r * ld + c * 16);
+    }
     if (kmajor) {
       const int r = slot >> 2, c = dense::xk16_chunk(slot & 3, r);
       return (uint32_t)(r * ld + c * 16);
@@ -240,9 +247,15 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
     const int r = (wave * IPWS + s) * 64 + lane;
     voffS[s] = (uint32_t)((r < BM ? r : r - BM) * 4);
   }
-  // lanes whose 16 bytes lie past the end of a row in its last, short stage: the chunk a lane fetches is the same in each of its loads
-  const int short_stage = !FP4 && DIR != WEIGHT && g.K % DEPTH ? g.K / DEPTH : -1;
-  const uint64_t past_end = __ballot(16 / ES * dense::xk16_chunk(lane & 3, lane >> 2) >= g.K % DEPTH);
+  // Lanes whose 16 bytes lie past the end of a row in its last, short stage (WIDE: unit): the chunk a lane fetches is the same in each of its loads (WIDE: in every other).
+  constexpr int PIECE = WIDE ? 2 * DEPTH : DEPTH;
+  const int short_piece = !FP4 && DIR != WEIGHT && g.K % PIECE ? g.K / PIECE : -1;
+  uint64_t past_end[2];
+#pragma unroll
+  for (int o = 0; o < 2; ++o) {
+    const int c = WIDE ? (lane & 7) ^ ((lane >> 4) + 4 * o) : dense::xk16_chunk(lane & 3, lane >> 2);
+    past_end[o] = __ballot(16 / ES * c >= g.K % PIECE);
+  }
 
   // ---- issue side
   typedef typename std::conditional<A_K, int, i64>::type LeftA;
@@ -311,27 +324,41 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   };
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   u32x4 ra, rb, rsa, rsb;
-  uint64_t masked = 0;
+  uint64_t masked[2] = {0, 0};
+  const int halfA = WIDE ? BM / 2 * g.lda : 0, halfB = WIDE ? BN / 2 * g.ldb : 0;
   auto stage_rsrc = [&]() __attribute__((always_inline)) {
     const bool on = ikt * DEPTH < g.K;      // not a stage that only evens their number (WEIGHT: has no rows)
-    ra = fa.rsrc(!A_K || on);
-    rb = fb.rsrc(!B_K || on);
+    if (WIDE) {
+      Feed<LeftA> ha = fa;
+      Feed<LeftB> hb = fb;
+      ha.step((ikt & 1) * halfA);
+      hb.step((ikt & 1) * halfB);
+      ra = ha.rsrc(true);
+      rb = hb.rsrc(true);
+    } else {
+      ra = fa.rsrc(!A_K || on);
+      rb = fb.rsrc(!B_K || on);
+    }
     if (FP4) {
       rsa = Feed<int>{fsa, fha}.rsrc(on);
       rsb = Feed<int>{fsb, fhb}.rsrc(on);
     } else {
-      masked = ikt == short_stage ? past_end : 0;
+      const bool is_short = (WIDE ? ikt >> 1 : ikt) == short_piece;
+      masked[0] = is_short ? past_end[0] : 0;
+      masked[1] = is_short ? past_end[1] : 0;
     }
   };
-  auto masked_off = [&](uint32_t v) __attribute__((always_inline)) {
+  auto masked_off = [&](uint32_t v, int load) __attribute__((always_inline)) {
     uint32_t o;
-    asm("v_cndmask_b32 %0, %1, %2, %3" : "=v"(o) : "v"(v), "v"(0xfffffff0u), "s"(masked));
+    asm("v_cndmask_b32 %0, %1, %2, %3" : "=v"(o) : "v"(v), "v"(0xfffffff0u), "s"(masked[WIDE ? load & 1 : 0]));
     return o;
   };
+  static_assert(!WIDE || (IPWA % 2 == 0 && IPWB % 2 == 0), "a wave's loads start with an even one");
   auto issue = [&](int i) __attribute__((always_inline)) {      // load i of the stage (a constant wherever this is called)
-    const uint32_t stage = lds_base + islot * STAGE_BYTES;
-    if (i < IPWA) dma16b(ra, !FP4 && A_K ? masked_off(voffA[i]) : voffA[i], stage + (wave * IPWA + i) * 1024);
-    else if (i < IPWA + IPWB) dma16b(rb, FP4 ? voffA[i - IPWA] : B_K ? masked_off(voffB[i - IPWA]) : voffB[i - IPWA], stage + A_BYTES + (wave * IPWB + i - IPWA) * 1024);
+    const uint32_t stage = lds_base + (WIDE ? (islot >> 1) * 2 : islot) * STAGE_BYTES, inA = WIDE ? (islot & 1) * A_BYTES : 0, inB = WIDE ? 2 * A_BYTES + (islot & 1) * C::B_BYTES : A_BYTES;
+    if (i < IPWA) dma16b(ra, !FP4 && A_K ? masked_off(voffA[i], i) : voffA[i], stage + inA + (wave * IPWA + i) * 1024);
+    else if (i < IPWA + IPWB)
+      dma16b(rb, FP4 ? voffA[i - IPWA] : B_K ? masked_off(voffB[i - IPWA], i - IPWA) : voffB[i - IPWA], stage + inB + (wave * IPWB + i - IPWA) * 1024);
     else {
       const int s = i - IPWA - IPWB;
       dma4b(scale_of_a(s) ? rsa : rsb, voffS[s], stage + A_BYTES + C::B_BYTES + (wave * IPWS + s) * 256);
@@ -340,15 +367,20 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   auto issue_advance = [&]() __attribute__((always_inline)) {
     islot = islot + 1 == NS ? 0 : islot + 1;
     ++ikt;
-    fa.step(stepA);
-    fb.step(stepB);
+    if (WIDE) {
+      fa.step((ikt & 1) == 0 ? 2 * stepA : 0);
+      fb.step((ikt & 1) == 0 ? 2 * stepB : 0);
+    } else {
+      fa.step(stepA);
+      fb.step(stepB);
+    }
     if (FP4) {
       fsa += g.sa_step;
       fsb += g.sb_step;
     }
     stage_rsrc();
   };
-  // after every second stage: tiles have even numbers of them, and so has the ring
+  // after every second stage: tiles have even numbers of them, and so has the ring (WIDE, a stage behind: after the first of a pair of multiplications)
   static_assert(NS % 2 == 0, "a tile's first stage is issued first of a pair");
   auto tile_advance = [&]() __attribute__((always_inline)) {
     if (ikt == iKT) {
@@ -358,12 +390,14 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   };
 
   // ---- fragments
-  // K major: the 16-row pieces lie 1024 bytes apart, as their swizzle is the same
+  // K major: the 16-row pieces lie 1024 (WIDE: 2048) bytes apart, as their swizzle is the same
+  constexpr int PIECE_BYTES = WIDE ? 2048 : 1024, B_AT = WIDE ? 2 * A_BYTES : A_BYTES;
   int fragA[A_K ? 1 : TM], fragB[B_K ? 1 : TN];
   const int q4 = lane >> 4, li = lane & 15;
   {
     const int k = 8 * q4 + (li >> 2);
     auto frag = [&](int x0, bool kmajor, int width) {
+      if (WIDE) return (x0 + li) * 128 + 16 * (q4 ^ (li >> 1));      // of a unit's first stage; the second's chunks are 4 further, bit 2 of the position
       if (kmajor) return (x0 + li) * 64 + 16 * dense::xk16_chunk(q4, li);
       if (FP32) return 4 * q4 * (width * 4) + 16 * strided_chunk((x0 + li) >> 2, 4 * q4) + 4 * (li & 3);
       return k * (width * 2) + 16 * dense::kx16_chunk((x0 >> 3) + ((li & 3) >> 1), k) + 8 * (li & 1);
@@ -371,7 +405,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
 #pragma unroll
     for (int a = 0; a < (A_K ? 1 : TM); ++a) fragA[a] = frag(wm * (BM / 2) + a * 16, A_K, BM);
 #pragma unroll
-    for (int c = 0; c < (B_K ? 1 : TN); ++c) fragB[c] = A_BYTES + frag(wn * (BN / 2) + c * 16, B_K, BN);
+    for (int c = 0; c < (B_K ? 1 : TN); ++c) fragB[c] = B_AT + frag(wn * (BN / 2) + c * 16, B_K, BN);
   }
   const int scaleA = A_BYTES + C::B_BYTES + wm * (BM / 2) * 4 + lane * 4, scaleB = A_BYTES + C::B_BYTES + (BM + wn * (BN / 2)) * 4 + lane * 4;
   auto load_frag = [&](const char* p, bool kmajor, int row_bytes) -> u32x4 {
@@ -390,16 +424,17 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
     u32x4 a[TM], b[TN];
     uint32_t sa[(TM + 3) / 4], sb[(TN + 3) / 4];      // CODES: a byte per piece
   };
-  // piece p, in the order the MFMAs first need them: A0 B0 A1 .. A(TM-1) B1 .. B(TN-1)
-  auto load_piece = [&](Frags& f, int slot, int p) __attribute__((always_inline)) {
-    const char* st = lds + slot * STAGE_BYTES;
+  // piece p, in the order the MFMAs first need them: A0 B0 A1 .. A(TM-1) B1 .. B(TN-1); odd: of the second stage of a unit
+  auto load_piece = [&](Frags& f, int slot, int p, bool odd) __attribute__((always_inline)) {
+    const char* st = lds + (WIDE ? slot & ~1 : slot) * STAGE_BYTES;
+    const int flip = WIDE && odd ? 64 : 0;
     if (p != 1 && p <= TM) {
       const int a = p ? p - 1 : 0;
-      f.a[a] = load_frag(st + fragA[A_K ? 0 : a] + (A_K ? a * 1024 : 0), A_K, BM * 2);
+      f.a[a] = load_frag(st + (fragA[A_K ? 0 : a] ^ flip) + (A_K ? a * PIECE_BYTES : 0), A_K, BM * 2);
       if (FP4 && a % 4 == 0) f.sa[a / 4] = *reinterpret_cast<const uint32_t*>(st + scaleA + a * 64);
     } else {
       const int b = p == 1 ? 0 : p - TM;
-      f.b[b] = load_frag(st + fragB[B_K ? 0 : b] + (B_K ? b * 1024 : 0), B_K, BN * 2);
+      f.b[b] = load_frag(st + (fragB[B_K ? 0 : b] ^ flip) + (B_K ? b * PIECE_BYTES : 0), B_K, BN * 2);
       if (FP4 && b % 4 == 0) f.sb[b / 4] = *reinterpret_cast<const uint32_t*>(st + scaleB + b * 64);
     }
   };
@@ -413,33 +448,32 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   next_tile();
   stage_rsrc();
 #pragma unroll 1
-  for (int t = 0; t < NS; t += 2) {
+  for (int t = 0; t < NS - (WIDE ? 1 : 0); ++t) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-#pragma unroll
-      for (int i = 0; i < LPT; ++i) issue(i);
-      issue_advance();
-    }
+    for (int i = 0; i < LPT; ++i) issue(i);
+    issue_advance();
     tile_advance();
   }
-  mm::wait_vmcnt_and_barrier<(NS - 1) * LPT>();
+  mm::wait_vmcnt_and_barrier<(WIDE ? NS - 3 : NS - 1) * LPT>();
   Frags F, Gf;
   int cslot = 0;
 #pragma unroll
-  for (int p = 0; p < TM + TN; ++p) load_piece(F, 0, p);
+  for (int p = 0; p < TM + TN; ++p) load_piece(F, 0, p, false);
 
   // once per wave: wave W issues its loads W quarters of the way from one to the next
   auto run = [&](auto WC) __attribute__((always_inline)) {
     constexpr int W = decltype(WC)::value;
-    auto multiply = [&](const Frags& X, Frags& Y) __attribute__((always_inline)) {
-      mm::wait_all_reads_and_barrier<(NS - 2) * LPT>();
+    auto multiply = [&](const Frags& X, Frags& Y, auto ODD) __attribute__((always_inline)) {      // ODD: the stage in X is the second of a unit
+      constexpr bool odd = decltype(ODD)::value;
+      // Every wave holds this stage in registers and the next one has landed (WIDE: with the other half of its unit).  Stages up to kt + NS - 1 are issued, WIDE one less.
+      mm::wait_all_reads_and_barrier<(WIDE ? odd ? NS - 4 : NS - 3 : NS - 2) * LPT>();
       const int nslot = cslot + 1 == NS ? 0 : cslot + 1;
       in_turn(std::make_integer_sequence<int, MF>{}, [&](auto I) __attribute__((always_inline)) {
         constexpr int i = decltype(I)::value, a = i % TM, b = i / TM % TN;
         if constexpr (FP4) mfma_fp4<b % 4, a % 4>(acc[a][b], X.b[b], X.a[a], X.sb[b / 4], X.sa[a / 4]);
         else if constexpr (FP32) mfma_fp32(acc[a][b], X.b[b][i / (TM * TN)], X.a[a][i / (TM * TN)]);
         else dense::mfma16(acc[a][b], __builtin_bit_cast(bf16x8, X.b[b]), __builtin_bit_cast(bf16x8, X.a[a]));
-        if constexpr (i % RS == 0 && i / RS < TM + TN) load_piece(Y, nslot, i / RS);
+        if constexpr (i % RS == 0 && i / RS < TM + TN) load_piece(Y, nslot, i / RS, !odd);
         if constexpr (i % DS == W * DS / 4 && i / DS < LPT) issue(i / DS);
         if constexpr (i == MF - 1) issue_advance();
         __builtin_amdgcn_sched_barrier(0);
@@ -449,9 +483,10 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
     for (int ti = 0; ti < n_my; ++ti) {
       const Where range = locate(ti);
       for (int kt = range.k0; kt < range.k1; kt += 2) {
-        multiply(F, Gf);
-        multiply(Gf, F);
-        tile_advance();
+        multiply(F, Gf, std::false_type{});
+        if (WIDE) tile_advance();
+        multiply(Gf, F, std::true_type{});
+        if (!WIDE) tile_advance();
       }
       if constexpr (FP32) {      // as settle() does
         asm volatile("s_nop 15\n\ts_nop 3");
