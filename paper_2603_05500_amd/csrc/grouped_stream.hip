@@ -95,8 +95,8 @@ bool stream_supported(int dtype, Dir dir, const Call& c) {
          (dir == WEIGHT ? c.ld_in2 % v == 0 && aligned16(c.in2) && c.ld_in2 < wide : aligned16(c.w));
 }
 
-// The figures were fitted to 600 calls in bf16 and 700 in fp32 of random directions, sizes (64 to 14336; 64 to 4096), groups (1 to 128) and rows (1 to 32768; 8 to 8192), each
-// with every kernel that could take it; the choices they lead to take 1.5 % more time than the best would (geometric mean).
+// The figures were fitted to 650 calls in bf16 and 700 in fp32 of random directions, sizes (64 to 14336; 64 to 4096), groups (1 to 128) and rows (1 to 32768; 8 to 8192), each
+// with every kernel that could take it; the choices they lead to take 2 % more time than the best would (geometric mean).
 Plan plan(int dtype, Dir dir, const Call& c, bool streams, size_t scratch) {
   struct Row {
     Kernel kernel;
@@ -106,9 +106,9 @@ Plan plan(int dtype, Dir dir, const Call& c, bool streams, size_t scratch) {
     double uneven;        // bf16 streams, which go round by round: part of a round that the last one takes more than its share, where groups end inside tiles
     double rest;          // us
   };
-  static const Row bf16[] = {{EDGE_32, 32, 32, 128, 0.64, 400, 0, 3.5},      {EDGE_32_DEEP, 32, 32, 512, 1.1, 137, 0, 5.1}, {EDGE_64, 64, 64, 64, 0.80, 433, 0, 2.9},
-                             {EDGE_128, 128, 128, 64, 1.58, 224, 0, 3.2},    {STREAM_256, 256, 256, 32, 0.67, kCUs, 0.45, 11.8}, {STREAM_256x128, 256, 128, 32, 0.52, kCUs, 0.33, 7.5},
-                             {STREAM_128, 128, 128, 32, 0.315, kCUs, 0.65, 7.7}};
+  static const Row bf16[] = {{EDGE_32, 32, 32, 128, 0.63, 465, 0, 3.6},   {EDGE_32_DEEP, 32, 32, 512, 0.88, 118, 0, 5.0},     {EDGE_64, 64, 64, 64, 0.73, 546, 0, 3.2},
+                             {EDGE_128, 128, 128, 64, 1.51, 282, 0, 4.0}, {STREAM_256, 256, 256, 32, 0.645, kCUs, 0.39, 9.1}, {STREAM_256x128, 256, 128, 32, 0.52, kCUs, 0.28, 7.9},
+                             {STREAM_128, 128, 128, 32, 0.32, kCUs, 0.58, 7.9}};
   static const Row fp32[] = {{EDGE_32, 32, 32, 64, 0.87, 356, 0, 3.9}, {EDGE_64, 64, 64, 32, 1.08, 260, 0, 3.6}, {SINGLE_128, 128, 128, 16, 1.42, 253, 0, 10.2},
                              {SINGLE_64, 64, 64, 16, 0.42, 295, 0, 7.0}};
   const bool f = dtype == POETX_F32;
@@ -125,6 +125,7 @@ Plan plan(int dtype, Dir dir, const Call& c, bool streams, size_t scratch) {
     const bool stream = r.kernel >= STREAM_256;
     if (stream && !streams) break;
     const double tiles = tiles_of(dir, c.rows, c.m, c.n, c.groups, r.h, r.w), stages = (double)(i64)((K + r.depth - 1) / r.depth);
+    const double stage = r.stage * (dir == FWD && (r.kernel == STREAM_256x128 || r.kernel == STREAM_128) ? 0.9 : 1.0);      // whole lines
     // few tiles: their contraction in ranges, whose fp32 sums are added by another launch (7.5 us with the wait between the two, and their way through the caches)
     const bool splittable = dir != WEIGHT && (r.kernel == STREAM_128 || r.kernel >= SINGLE_128);
     for (const int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
@@ -132,9 +133,9 @@ Plan plan(int dtype, Dir dir, const Call& c, bool streams, size_t scratch) {
       if (splits > 1 && (!splittable || parts > scratch || 4 * splits > stages || tiles * splits > 2 * r.at_once)) break;
       double us = tiles * splits / r.at_once;
       if (stream && !f) us = c.groups == 1 ? (double)(i64)(us + 0.999) : us + r.uneven;
-      us = (us < 1 ? 1 : us) * (double)(i64)((stages + splits - 1) / splits) * r.stage;
+      us = (us < 1 ? 1 : us) * (double)(i64)((stages + splits - 1) / splits) * stage;
       // a stream stores between multiplications; the others have several workgroups on a CU, but store less well
-      const double stores = (f ? 1.5 : 1.23) * out_us;
+      const double stores = (f ? 1.5 : 1.35) * out_us;
       us = r.rest + (stream ? us + out_us : us > stores ? us : stores);
       if (splits > 1) us += 7.5 + 2 * parts / 8e6;
       if (us < least) {
