@@ -15,7 +15,8 @@
  *    major n x m (out x in).
  *  - Activations are FEATURE MAJOR: X is m x N, Z is n x N, row major with the
  *    token index contiguous (leading dimension = N).  This is the column form
- *    of Eq. 4: Z = P^T W R^T X.
+ *    of Eq. 4: Z = P^T W R^T X.  (The grouped products take rows of features, with a
+ *    leading dimension of their own: a router picks rows.)
  *  - A permutation is an int32 vector pi of length d holding a bijection of
  *    {0..d-1}.  Psi[i, pi[i]] = 1, so (Psi V)[i,:] = V[pi[i],:] and
  *    (Psi^T V)[pi[i],:] = V[i,:]                              (Sec. 3.2, Eq. 5).
@@ -170,7 +171,8 @@ int poetx_version(void);
 
 /* Test hook (process-wide, not for production use): on != 0 routes every call,
  * whatever its dtype, through the plain fp32-FMA kernels instead of the
- * matrix-core kernels, so that the two kernel families can be compared. */
+ * matrix-core kernels, so that the two kernel families can be compared.  The calls on
+ * 4-bit buffers, the grouped products and poetx_group_order have one family and ignore it. */
 void poetx_debug_force_fma(int on);
 
 /* Stage timing for benchmarks (process-wide; off unless begun).  Between

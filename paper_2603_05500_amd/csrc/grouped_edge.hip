@@ -1,6 +1,7 @@
 // Grouped products of any sizes, strides and alignments, bf16 and fp32: the edge-handling matrix-core product, one output tile of one
 // group per workgroup.  A workgroup finds its group from the offsets on the device; the grid has room for the most tiles that any offsets could
-// give, and the workgroups beyond the actual number leave.
+// give, and the workgroups beyond the actual number leave.  Short groups of wide operands are bound by the latency of their few stages, the rest by the loads' bounds checks:
+// the streams take what is aligned and large enough to fill the chip.
 #include "edge_gemm.h"
 #include "grouped.h"
 

@@ -15,6 +15,9 @@
 //  - A stage is 64 bytes of a row whatever they hold: 32 bf16, 16 fp32, or 128 codes with a word of four scales.  An MFMA of 16 x 16 x 128 codes takes as long
 //    as one of 16 x 16 x 32 bf16: the same stream carries four times the products.  The fp32 ones take eight times as long for the bytes: smaller tiles and several
 //    workgroups per CU.
+// What bounds it: large bf16 products by power, as the dense one (16384 rows, 8 groups of 8192 x 4096: 960 to 1015 us, 1.08 to 1.15 PFLOP/s with the ragged tiles); products of codes by the
+// loads of a stage, which take as long as its multiplications (16384 x 4096 by 14336 x 4096 480 us, 4.0 PFLOP/s; without loads 384); many small groups by the weights' bytes (8190 rows,
+// 57 groups of 1376 x 2048, input gradient 92 to 103 us); weight gradients by their stores (8192 rows, 16 groups of 1376 x 2048 104 us for 180 MB).
 #pragma once
 #include <utility>
 
@@ -28,8 +31,6 @@ namespace grouped {
 using dense::floatx4;
 using mm::bf16x8;
 using mx4::u32x4;
-
-
 
 enum Elem { BF16, F32, CODES };
 
@@ -279,31 +280,31 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
     int k0 = 0, k1 = 0x7fffffff, ha = 0, hb = 0;
     uint64_t nsa = 0, nsb = 0;
     if (iti < n_my) {
-    k0 = w.k0;
-    k1 = w.k1;
-    if (DIR == FWD) hb = g.N - w.j0 < BN ? g.N - w.j0 : BN;      // rows of W in the tile
-    if (DIR == WEIGHT) {
-      const i64 len = w.r1 - w.r0;
-      na.at = (uint64_t)(g.A + (i64)w.r0 * g.lda + ES * w.i0);
-      na.left = (len - 1) * (i64)g.lda + ES * (i64)(g.M - w.i0);
-      nb.at = (uint64_t)(g.B + (i64)w.r0 * g.ldb + ES * w.j0);
-      nb.left = (len - 1) * (i64)g.ldb + ES * (i64)(g.N - w.j0);
-    } else {
-      ha = w.r1 - w.r0 < BM ? w.r1 - w.r0 : BM;
-      const int row = FP4 ? g.K / 2 : ES * g.K;      // bytes of a row
-      na.at = (uint64_t)(g.A + (i64)w.r0 * g.lda);
-      na.left = (ha - 1) * (LeftA)g.lda + row;
-      if (DIR == FWD) {
-        const i64 first = (i64)w.gr * g.N + w.j0;
-        nb.at = (uint64_t)(g.B + first * g.ldb);
-        nb.left = (hb - 1) * (LeftB)g.ldb + row;
-        nsa = (uint64_t)(g.SA + mx4::position(w.first, w.gr) + (w.r0 - w.first));      // a word per row
-        nsb = (uint64_t)(g.SB + (i64)w.gr * ((g.N + 63) / 64 * 64) + w.j0);
+      k0 = w.k0;
+      k1 = w.k1;
+      if (DIR == FWD) hb = g.N - w.j0 < BN ? g.N - w.j0 : BN;      // rows of W in the tile
+      if (DIR == WEIGHT) {
+        const i64 len = w.r1 - w.r0;
+        na.at = (uint64_t)(g.A + (i64)w.r0 * g.lda + ES * w.i0);
+        na.left = (len - 1) * (i64)g.lda + ES * (i64)(g.M - w.i0);
+        nb.at = (uint64_t)(g.B + (i64)w.r0 * g.ldb + ES * w.j0);
+        nb.left = (len - 1) * (i64)g.ldb + ES * (i64)(g.N - w.j0);
       } else {
-        nb.at = (uint64_t)(g.B + (i64)w.gr * g.K * g.ldb + ES * w.j0);
-        nb.left = (i64)(g.K - 1) * g.ldb + ES * (i64)(g.N - w.j0);
+        ha = w.r1 - w.r0 < BM ? w.r1 - w.r0 : BM;
+        const int row = FP4 ? g.K / 2 : ES * g.K;      // bytes of a row
+        na.at = (uint64_t)(g.A + (i64)w.r0 * g.lda);
+        na.left = (ha - 1) * (LeftA)g.lda + row;
+        if (DIR == FWD) {
+          const i64 first = (i64)w.gr * g.N + w.j0;
+          nb.at = (uint64_t)(g.B + first * g.ldb);
+          nb.left = (hb - 1) * (LeftB)g.ldb + row;
+          nsa = (uint64_t)(g.SA + mx4::position(w.first, w.gr) + (w.r0 - w.first));      // a word per row
+          nsb = (uint64_t)(g.SB + (i64)w.gr * ((g.N + 63) / 64 * 64) + w.j0);
+        } else {
+          nb.at = (uint64_t)(g.B + (i64)w.gr * g.K * g.ldb + ES * w.j0);
+          nb.left = (i64)(g.K - 1) * g.ldb + ES * (i64)(g.N - w.j0);
+        }
       }
-    }
     }
     if (DIR != WEIGHT) {
       na.step(k0 * stepA);
