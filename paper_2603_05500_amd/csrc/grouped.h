@@ -100,8 +100,11 @@ struct Plan {
   Kernel kernel;
   int splits;
   size_t parts;
+  double us;
 };
 Plan plan(int dtype, Dir dir, const Call& c, bool streams, size_t scratch);
+// Output tiles of h x w that a call has, about.
+double tiles_of(Dir dir, i64 rows, int m, int n, int groups, int h, int w);
 
 // ---- launchers -----------------------------------------------------------------------------------
 void edge_launch(int dtype, Dir dir, Kernel k, const Call& c, hipStream_t st);      // any shape (grouped_edge.hip)
@@ -113,8 +116,12 @@ bool codes_supported(const poetx_grouped_desc* d, const void* Z, i64 ldz);
 size_t codes_workspace_bytes(const poetx_grouped_desc* d);
 void codes_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, void* ws, hipStream_t st);
 
+// Z = X W^T with W a 4-bit buffer, decoded on the way (grouped_values.hip): whole 16-byte vectors; false where it is better written out first, for which there are `scratch` bytes
+bool values_supported(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Z, i64 ldz);
+bool values_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, size_t scratch, hipStream_t st);
+
 // the forward of a handful of rows per group (grouped_few.hip): any sizes, strides and alignments
-enum Weight { DENSE_WEIGHT, VALUES_MX4, CODES_MX4 };      // CODES: of X as well
+enum Weight { DENSE_WEIGHT, VALUES_MX4, VALUES_STREAMED_MX4, CODES_MX4 };      // STREAMED: values_launch() takes the call; CODES: of X as well
 bool few_supported(int dtype, Dir dir, i64 rows, int m, int n, int groups, Weight w);
 void few_dense(int dtype, const Call& c, hipStream_t st);
 void few_values(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, hipStream_t st);      // 4-bit weight

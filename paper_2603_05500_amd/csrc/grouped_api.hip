@@ -144,7 +144,8 @@ int poetx_grouped_fwd(const poetx_grouped_desc* d, const void* X, int64_t ldx, c
   if (rc != POETX_OK || d->rows == 0) return rc;
   hipStream_t st = (hipStream_t)stream;
   const bool mx4 = d->flags & POETX_GROUPED_W_MX4, both = d->flags & POETX_GROUPED_X_MX4;
-  const bool few = mx4 && grouped::few_supported(d->dtype, grouped::FWD, d->rows, d->d_in, d->d_out, d->groups, both ? grouped::CODES_MX4 : grouped::VALUES_MX4);
+  const bool values = mx4 && !both && grouped::values_supported(d, X, ldx, Z, ldz);
+  const bool few = mx4 && grouped::few_supported(d->dtype, grouped::FWD, d->rows, d->d_in, d->d_out, d->groups, both ? grouped::CODES_MX4 : values ? grouped::VALUES_STREAMED_MX4 : grouped::VALUES_MX4);
   if (both && few) {
     {
       StageTimer tm(POETX_STAGE_DEQUANT, st);
@@ -163,6 +164,7 @@ int poetx_grouped_fwd(const poetx_grouped_desc* d, const void* X, int64_t ldx, c
     grouped::few_values(d, X, ldx, W, offsets, Z, ldz, st);
     return launch_status();
   }
+  if (values && grouped::values_launch(d, X, ldx, W, offsets, Z, ldz, parts_bytes(d), st)) return launch_status();
   const void* w = dense_weight(d, W, offsets, ws, st);
   if (d->flags & POETX_GROUPED_X_MX4) {
     char* values = (char*)ws + dequantised_bytes(d);

@@ -252,12 +252,13 @@ void pick(const FewArgs& a, hipStream_t st) {
 
 // Where it pays: up to so many rows per group, or few tiles in all.  us, these / the streams and edge kernels: bf16 64 experts of 1376 x 2048 with 8 rows each 76 / 86, 32 each 101 / 91;
 // both in four bits, 14336 x 4096, 16 rows 11 / 24, 64 experts with 32 rows each 51 / 37, 256 x 8192, four with 30 in all 9 / 33;
-// a 4-bit weight against its values in the workspace: 14336 x 4096, 128 rows 49 / 66, 64 experts with 64 rows each 96 / 194.
+// a 4-bit weight against the stream that decodes it: 14336 x 4096, 32 rows 18.3 / 20.6, 64 rows 33 / 21, 4096 x 4096, 64 rows 17.0 / 20.0, 64 experts with 16 rows each 50 / 33;
+// against its values in the workspace, for what that stream does not take: 14336 x 4096, 128 rows 49 / 66, 64 experts with 64 rows each 96 / 194.
 // few tiles: bf16 1024 x 4096, 64 rows 9.5 / 13.8, 128 rows 16.5 / 14.6, 1024 x 1024, 128 rows 5.6 / 7.0; fp32 128 x 1749, 179 rows 7.4 / 32, 1024 x 2048, 256 rows 19 / 38.
 bool few_supported(int dtype, Dir dir, i64 rows, int m, int n, int groups, Weight w) {
   if (dir != FWD) return false;
   const i64 most = dtype == POETX_F32 ? 4 : w == VALUES_MX4 ? 128 : 16;
-  const i64 few = dtype == POETX_F32 ? 1024 : w != DENSE_WEIGHT ? 768 : m <= 2048 ? 640 : 320;
+  const i64 few = dtype == POETX_F32 ? 1024 : w == VALUES_STREAMED_MX4 ? 2048 : w != DENSE_WEIGHT ? 768 : m <= 2048 ? 640 : 320;
   return rows <= most * groups || small_tiles(rows, groups, n) <= few;
 }
 void few_dense(int dtype, const Call& c, hipStream_t st) {

@@ -38,7 +38,9 @@ void pick(Kernel k, const StreamArgs& a, hipStream_t st) {
   else go<DIR, Tile128>(a, st);
 }
 
-// Output tiles of h x w: a group's last tile is half empty on average, and a group with rows has at least one.
+}  // namespace
+
+// A group's last tile is half empty on average, and a group with rows has at least one.
 double tiles_of(Dir dir, i64 rows, int m, int n, int groups, int h, int w) {
   const double across = ceil_div(dir == FWD ? n : m, w);
   if (dir == WEIGHT) return (double)groups * ceil_div(n, h) * across;
@@ -46,6 +48,8 @@ double tiles_of(Dir dir, i64 rows, int m, int n, int groups, int h, int w) {
   const double live = rows < groups ? (double)rows : groups, t = (double)rows / h + 0.5 * live;
   return (t > live ? t : live) * across;
 }
+
+namespace {
 
 // The sums of a contraction's ranges, [split][rows][cols], added in order and rounded, for the rows that some group has.  A wave takes 256 columns of a row.
 template <class T>
@@ -118,8 +122,7 @@ Plan plan(int dtype, Dir dir, const Call& c, bool streams, size_t scratch) {
   const double K = dir == FWD ? c.m : dir == INPUT ? c.n : live > 0 ? c.rows / live : 0;
   const int out_cols = dir == FWD ? c.n : c.m;
   const double out_us = dir == WEIGHT ? 4.0 * c.groups * c.n * c.m / 5.1e6 : 0;      // fp32 weights to memory
-  Plan best{EDGE_32, 1, 0};
-  double least = 1e30;
+  Plan best{EDGE_32, 1, 0, 1e30};
   for (int i = 0; i < count; ++i) {
     const Row& r = rows[i];
     const bool stream = r.kernel >= STREAM_256;
@@ -138,10 +141,7 @@ Plan plan(int dtype, Dir dir, const Call& c, bool streams, size_t scratch) {
       const double stores = (f ? 1.5 : 1.35) * out_us;
       us = r.rest + (stream ? us + out_us : us > stores ? us : stores);
       if (splits > 1) us += 7.5 + 2 * parts / 8e6;
-      if (us < least) {
-        least = us;
-        best = Plan{r.kernel, splits, parts};
-      }
+      if (us < best.us) best = Plan{r.kernel, splits, parts, us};
     }
   }
   return best;

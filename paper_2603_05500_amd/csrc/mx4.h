@@ -34,6 +34,11 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t amax_bits) {
   return f == 255 ? 255 : f > 2 ? f - 2 : 0;
 }
 
+// codes 2 I and 2 I + 1 of eight (elements in order, the first in the low four bits) -> two bf16 values
+template <int I>
+__device__ __forceinline__ uint32_t to_bf16x2(uint32_t c, float s) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, I));
+}
 // eight codes (elements in order, the first in the low four bits) -> bf16 values
 __device__ __forceinline__ u32x4 to_bf16(uint32_t c, float s) {
   u32x4 o;

@@ -460,6 +460,71 @@ def test_grouped_mx4_large(lib, groups, rows, m, n, act):
     assert within(dX, *reference("input", dZ, W, counts), n, "bf16")
 
 
+@pytest.mark.parametrize("groups,rows,m,n,before,behind", [
+    (1, 272, 136, 2056, 0, 0), (1, 300, 1416, 2056, 3, 130), (5, 700, 1032, 1000, 1, 0), (200, 5000, 264, 520, 0, 7), (300, 9000, 128, 136, 0, 0),      # tiles of 64 x 128
+    (16, 8192, 512, 512, 0, 0), (2, 2100, 2056, 3000, 0, 5), (1, 1990, 1000, 2048, 9, 9),                                                              # 128 x 128
+    (4, 5000, 2600, 2072, 2, 3), (8, 4096, 1000, 2056, 0, 0), (1, 2100, 2632, 2056, 65, 65)])                                                          # 128 x 256
+def test_grouped_mx4_decoded_on_the_way(lib, groups, rows, m, n, before, behind):
+    """More rows than a handful, with NaN in every row of X that no group has, between its rows and in the weight of a group without rows."""
+    counts = spread(groups, rows)
+    off = (offsets_of(counts) + before).int()
+    g = torch.Generator(device="cuda").manual_seed(groups + rows + m)
+    X, _ = strided(before + rows + behind, m, 24, torch.bfloat16, 8)
+    X[before: before + rows] = torch.randn((rows, m), device="cuda", generator=g).bfloat16()
+    values = (torch.randn((groups, n, m), device="cuda", generator=g) * 0.02).bfloat16()
+    for k, c in enumerate(counts):
+        if c == 0:
+            values[k] = float("nan")
+    Q = quantised(values.view(groups * n, m))
+    W = torch.empty((groups * n, m), dtype=torch.bfloat16, device="cuda")
+    px.poetx_mx4_dequantize(Q, W)
+    desc = px.make_grouped_desc(m, n, groups, before + rows + behind, px.BF16, px.GROUPED_W_MX4)
+    ws = torch.full((px.poetx_grouped_workspace_bytes(desc),), 255, dtype=torch.uint8, device="cuda")
+    Z, flat = strided(before + rows + behind, n, 16, torch.bfloat16, 8, fill=3.0)
+    px.poetx_grouped_fwd(desc, X, Q, off, Z, ws)
+    assert within(Z[before: before + rows], *reference("fwd", X[before: before + rows], W.view(groups, n, m), counts), m, "bf16")
+    again = torch.empty((before + rows + behind, n), dtype=torch.bfloat16, device="cuda")
+    px.poetx_grouped_fwd(desc, X, Q, off, again, ws)
+    assert torch.equal(again[before: before + rows], Z[before: before + rows])
+    Z[before: before + rows] = 3.0
+    assert bool((flat == 3.0).all()), "written where no group is"
+
+
+def test_grouped_mx4_decoded_not_finite(lib):
+    """An infinity or NaN of X stays in its row, one of the weight in its block's column of the groups that read it."""
+    m, n, counts = 392, 2056, [130, 0, 400]
+    G, rows = len(counts), sum(counts)
+    g = torch.Generator(device="cuda").manual_seed(11)
+    X = torch.randn((rows, m), device="cuda", generator=g).bfloat16()
+    W = (torch.randn((G, n, m), device="cuda", generator=g) * 0.02).bfloat16()
+    X[129, 391], X[130, 0], X[529, 128], W[2, 2055, 391], W[0, 0, 5] = float("nan"), float("inf"), float("-inf"), float("nan"), float("inf")
+    desc = px.make_grouped_desc(m, n, G, rows, px.BF16, px.GROUPED_W_MX4)
+    ws = torch.empty(px.poetx_grouped_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    Z = torch.empty((rows, n), dtype=torch.bfloat16, device="cuda")
+    px.poetx_grouped_fwd(desc, X, quantised(W.view(G * n, m)), offsets_of(counts), Z, ws)
+    want = torch.zeros_like(Z, dtype=torch.bool)
+    want[129] = want[130] = want[529] = True
+    want[130:, 2055] = want[:130, 0] = True
+    assert torch.equal(~torch.isfinite(Z), want)
+
+
+def test_grouped_mx4_decoded_past_32_bits(lib):
+    """Rows of X and Z more than 2^32 bytes from the first."""
+    m, n, rows, ld = 136, 2056, 2600, 1 << 21
+    counts = [1100, 0, 1500]
+    g = torch.Generator(device="cuda").manual_seed(5)
+    X = torch.empty((rows, ld), dtype=torch.bfloat16, device="cuda")[:, :m]
+    Z = torch.empty((rows, ld), dtype=torch.bfloat16, device="cuda")[:, :n]
+    X.copy_(torch.randn((rows, m), device="cuda", generator=g).bfloat16())
+    Q = quantised((torch.randn((3 * n, m), device="cuda", generator=g) * 0.02).bfloat16())
+    W = torch.empty((3 * n, m), dtype=torch.bfloat16, device="cuda")
+    px.poetx_mx4_dequantize(Q, W)
+    desc = px.make_grouped_desc(m, n, 3, rows, px.BF16, px.GROUPED_W_MX4)
+    ws = torch.empty(px.poetx_grouped_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    px.poetx_grouped_fwd(desc, X, Q, offsets_of(counts), Z, ws)
+    assert within(Z, *reference("fwd", X, W.view(3, n, m), counts), m, "bf16")
+
+
 @pytest.mark.parametrize("dtype,kind,m,n,counts,before,behind", [
     ("bf16", "fwd", 5568, 512, [637], 0, 0), ("bf16", "fwd", 7808, 1248, [200, 0, 300, 37, 251], 3, 9), ("bf16", "input", 1408, 5088, [221], 0, 70),
     ("bf16", "input", 776, 6368, [500, 607], 5, 0), ("f32", "fwd", 1760, 576, [1140], 0, 0), ("f32", "input", 516, 2692, [100, 0, 140], 2, 3)])
