@@ -91,12 +91,13 @@ template <class Left>
 struct Feed {
   uint64_t at;
   Left left;
-  __device__ __forceinline__ u32x4 rsrc(bool on) const {      // empty if !on
-    const int high = sizeof(Left) == 8 ? (int)((i64)left >> 32) : left < 0 ? -1 : 0;      // compared in halves: there is no scalar comparison of 64 bits
-    const uint32_t low = (uint32_t)left, most = 0x7ffffff0u;                                // a stage or a tile spans less
-    const uint32_t n = high < 0 || !on ? 0u : high > 0 || low > most ? most : low;
-    return u32x4{(uint32_t)uniform((int)at), (uint32_t)uniform((int)(at >> 32)) & 0xffffu, (uint32_t)uniform((int)n), 0x00020000u};
+  __device__ __forceinline__ uint32_t bytes(bool on) const {      // none if !on
+    if constexpr (sizeof(Left) == 4) return (uint32_t)uniform(on && left > 0 ? (int)left : 0);
+    const int high = (int)((i64)left >> 32);      // compared in halves: there is no scalar comparison of 64 bits
+    const uint32_t low = (uint32_t)left, most = 0x7ffffff0u;      // a stage or a tile spans less
+    return (uint32_t)uniform((int)(high < 0 || !on ? 0u : high > 0 || low > most ? most : low));
   }
+  __device__ __forceinline__ void base(u32x4& r) const { r[0] = (uint32_t)uniform((int)at), r[1] = (uint32_t)uniform((int)(at >> 32)) & 0xffffu, r[3] = 0x00020000u; }
   __device__ __forceinline__ void step(Left bytes) {
     at += bytes;
     left -= bytes;
@@ -241,8 +242,8 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   for (int s = 0; s < IPWA; ++s) voffA[s] = slot_offset((wave * IPWA + s) * 64 + lane, A_K, BM, g.lda);
 #pragma unroll
   for (int s = 0; s < (FP4 ? 0 : IPWB); ++s) voffB[s] = slot_offset((wave * IPWB + s) * 64 + lane, B_K, BN, g.ldb);
-  // scales: loads 0 .. BM / 64 - 1 are A's, the others B's
-  auto scale_of_a = [&](int s) __attribute__((always_inline)) { return (wave * IPWS + s) * 64 < BM; };
+  // scales: the first two waves bring A's, the others B's
+  const bool scales_a = wave < 2;
 #pragma unroll
   for (int s = 0; s < IPWS; ++s) {
     const int r = (wave * IPWS + s) * 64 + lane;
@@ -263,11 +264,12 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   typedef typename std::conditional<B_K, int, i64>::type LeftB;
   Feed<LeftA> fa;
   Feed<LeftB> fb;
-  uint64_t fsa = 0, fsb = 0;      // FP4: scales of the tile's rows in this stage, and their bytes
-  int fha = 0, fhb = 0;
+  Feed<int> fs{0, 0};      // FP4: scales of the tile's rows in this stage
+  const int step_s = scales_a ? g.sa_step : g.sb_step;
   int iti = -1, ikt = 0, iKT = 0, islot = 0;
   const LeftA stepA = A_K ? 64 : DEPTH * (LeftA)g.lda;
   const LeftB stepB = B_K ? 64 : DEPTH * (LeftB)g.ldb;
+  const int halfA = WIDE ? BM / 2 * g.lda : 0, halfB = WIDE ? BN / 2 * g.ldb : 0;
   auto next_tile = [&]() __attribute__((always_inline)) {
     Where w;
     do {
@@ -316,78 +318,75 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
     iKT = uniform(k1);
     fa = Feed<LeftA>{uniform(na.at), uniform(na.left)};
     fb = Feed<LeftB>{uniform(nb.at), uniform(nb.left)};
+    fb.step(-(WIDE ? 2 * stepB - halfB : stepB));      // the step to the tile's first stage is yet to come
     if (FP4) {
-      fsa = uniform(nsa);
-      fsb = uniform(nsb);
-      fha = uniform((ha + 63) / 64 * 256);
-      fhb = uniform((hb + 63) / 64 * 256);
+      fs = Feed<int>{uniform(scales_a ? nsa : nsb) - step_s, uniform(((scales_a ? ha : hb) + 63) / 64 * 256)};
     }
   };
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-  u32x4 ra, rb, rsa, rsb;
-  uint64_t masked[2] = {0, 0};
-  const int halfA = WIDE ? BM / 2 * g.lda : 0, halfB = WIDE ? BN / 2 * g.ldb : 0;
-  auto stage_rsrc = [&]() __attribute__((always_inline)) {
-    const bool on = ikt * DEPTH < g.K;      // not a stage that only evens their number (WEIGHT: has no rows)
-    if (WIDE) {
-      Feed<LeftA> ha = fa;
-      Feed<LeftB> hb = fb;
-      ha.step((ikt & 1) * halfA);
-      hb.step((ikt & 1) * halfB);
-      ra = ha.rsrc(true);
-      rb = hb.rsrc(true);
-    } else {
-      ra = fa.rsrc(!A_K || on);
-      rb = fb.rsrc(!B_K || on);
-    }
-    if (FP4) {
-      rsa = Feed<int>{fsa, fha}.rsrc(on);
-      rsb = Feed<int>{fsb, fhb}.rsrc(on);
-    } else {
-      const bool is_short = (WIDE ? ikt >> 1 : ikt) == short_piece;
-      masked[0] = is_short ? past_end[0] : 0;
-      masked[1] = is_short ? past_end[1] : 0;
-    }
+  u32x4 ra{}, rb{}, rs{};
+  uint64_t masked_a[2] = {0, 0}, masked_b[2] = {0, 0};
+  uint32_t slot_a = lds_base, slot_b = lds_base + (WIDE ? 2 * A_BYTES : A_BYTES);      // where the operands' stage in issue goes
+  // The descriptors of a stage come a few instructions at a time, between the multiplications of another: A's for the next stage once its loads of this one are out, B's and the
+  // scales' for this one ahead of their first load.  All at once they held up the next multiplications (fp32 4096 rows, 4 groups of 2048 x 2048 384 us, 345 so;
+  // codes 16384 x 4096 by 14336 x 4096 532, 521 with their quantising; bf16, bound by LDS on small tiles and by power on large ones, the same).  WIDE: the stages of a unit are the halves of its rows.
+  auto bytes_on = [&](int kt) __attribute__((always_inline)) { return kt * DEPTH < g.K; };      // not a stage that only evens their number (WEIGHT: has no rows)
+  auto mask = [&](uint64_t (&m)[2], int kt) __attribute__((always_inline)) {
+    const bool is_short = (WIDE ? kt >> 1 : kt) == short_piece;
+    m[0] = is_short ? past_end[0] : 0;
+    if (WIDE) m[1] = is_short ? past_end[1] : 0;
   };
-  auto masked_off = [&](uint32_t v, int load) __attribute__((always_inline)) {
+  auto set_a = [&](int part, int kt) __attribute__((always_inline)) {
+    if (part == 0) fa.base(ra);
+    if (part == 1) ra[2] = fa.bytes(WIDE || !A_K || bytes_on(kt));
+    if (part == 2 && A_K && !FP4) mask(masked_a, kt);
+  };
+  auto next_a = [&](int part) __attribute__((always_inline)) {      // parts 0 .. 3
+    if (part == 0) fa.step(WIDE ? (ikt & 1 ? 2 * stepA - halfA : (LeftA)halfA) : stepA);
+    else set_a(part - 1, ikt + 1);
+  };
+  auto next_b = [&](int part) __attribute__((always_inline)) {      // parts 0 .. 5
+    if (part == 0) fb.step(WIDE ? (ikt & 1 ? (LeftB)halfB : 2 * stepB - halfB) : stepB);
+    if (part == 1) fb.base(rb);
+    if (part == 2) rb[2] = fb.bytes(WIDE || !B_K || bytes_on(ikt));
+    if (part == 3 && B_K && !FP4) mask(masked_b, ikt);
+    if (FP4 && part == 4) {
+      fs.at += step_s;
+      fs.base(rs);
+    }
+    if (FP4 && part == 5) rs[2] = fs.bytes(bytes_on(ikt));
+  };
+  auto masked_off = [&](uint32_t v, const uint64_t (&m)[2], int load) __attribute__((always_inline)) {
     uint32_t o;
-    asm("v_cndmask_b32 %0, %1, %2, %3" : "=v"(o) : "v"(v), "v"(0xfffffff0u), "s"(masked[WIDE ? load & 1 : 0]));
+    asm("v_cndmask_b32 %0, %1, %2, %3" : "=v"(o) : "v"(v), "v"(0xfffffff0u), "s"(m[WIDE ? load & 1 : 0]));
     return o;
   };
+  static_assert(IPWA * DS >= 6 && IPWA * DS + 4 <= MF, "B's descriptor ahead of its loads, A's behind its own");
   static_assert(!WIDE || (IPWA % 2 == 0 && IPWB % 2 == 0), "a wave's loads start with an even one");
   auto issue = [&](int i) __attribute__((always_inline)) {      // load i of the stage (a constant wherever this is called)
-    const uint32_t stage = lds_base + (WIDE ? (islot >> 1) * 2 : islot) * STAGE_BYTES, inA = WIDE ? (islot & 1) * A_BYTES : 0, inB = WIDE ? 2 * A_BYTES + (islot & 1) * C::B_BYTES : A_BYTES;
-    if (i < IPWA) dma16b(ra, !FP4 && A_K ? masked_off(voffA[i], i) : voffA[i], stage + inA + (wave * IPWA + i) * 1024);
+    if (i < IPWA) dma16b(ra, !FP4 && A_K ? masked_off(voffA[i], masked_a, i) : voffA[i], slot_a + (wave * IPWA + i) * 1024);
     else if (i < IPWA + IPWB)
-      dma16b(rb, FP4 ? voffA[i - IPWA] : B_K ? masked_off(voffB[i - IPWA], i - IPWA) : voffB[i - IPWA], stage + inB + (wave * IPWB + i - IPWA) * 1024);
+      dma16b(rb, FP4 ? voffA[i - IPWA] : B_K ? masked_off(voffB[i - IPWA], masked_b, i - IPWA) : voffB[i - IPWA], slot_b + (wave * IPWB + i - IPWA) * 1024);
     else {
       const int s = i - IPWA - IPWB;
-      dma4b(scale_of_a(s) ? rsa : rsb, voffS[s], stage + A_BYTES + C::B_BYTES + (wave * IPWS + s) * 256);
+      dma4b(rs, voffS[s], slot_b + C::B_BYTES + (wave * IPWS + s) * 256);
     }
   };
   auto issue_advance = [&]() __attribute__((always_inline)) {
     islot = islot + 1 == NS ? 0 : islot + 1;
     ++ikt;
-    if (WIDE) {
-      fa.step((ikt & 1) == 0 ? 2 * stepA : 0);
-      fb.step((ikt & 1) == 0 ? 2 * stepB : 0);
-    } else {
-      fa.step(stepA);
-      fb.step(stepB);
-    }
-    if (FP4) {
-      fsa += g.sa_step;
-      fsb += g.sb_step;
-    }
-    stage_rsrc();
+    slot_a = lds_base + (WIDE ? (islot >> 1) * 2 * STAGE_BYTES + (islot & 1) * A_BYTES : islot * STAGE_BYTES);
+    slot_b = WIDE ? lds_base + (islot >> 1) * 2 * STAGE_BYTES + 2 * A_BYTES + (islot & 1) * C::B_BYTES : slot_a + A_BYTES;
+  };
+  auto start_tile = [&]() __attribute__((always_inline)) {
+    next_tile();
+#pragma unroll
+    for (int i = 0; i < 3; ++i) set_a(i, ikt);
   };
   // after every second stage: tiles have even numbers of them, and so has the ring (WIDE, a stage behind: after the first of a pair of multiplications)
   static_assert(NS % 2 == 0, "a tile's first stage is issued first of a pair");
   auto tile_advance = [&]() __attribute__((always_inline)) {
-    if (ikt == iKT) {
-      next_tile();
-      stage_rsrc();
-    }
+    if (ikt == iKT) start_tile();
   };
 
   // ---- fragments
@@ -446,12 +445,15 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
 #pragma unroll
     for (int c = 0; c < TN; ++c) acc[a][c] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  next_tile();
-  stage_rsrc();
+  start_tile();
 #pragma unroll 1
   for (int t = 0; t < NS - (WIDE ? 1 : 0); ++t) {
 #pragma unroll
+    for (int i = 0; i < 6; ++i) next_b(i);
+#pragma unroll
     for (int i = 0; i < LPT; ++i) issue(i);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) next_a(i);
     issue_advance();
     tile_advance();
   }
@@ -476,6 +478,8 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
         else dense::mfma16(acc[a][b], __builtin_bit_cast(bf16x8, X.b[b]), __builtin_bit_cast(bf16x8, X.a[a]));
         if constexpr (i % RS == 0 && i / RS < TM + TN) load_piece(Y, nslot, i / RS, !odd);
         if constexpr (i % DS == W * DS / 4 && i / DS < LPT) issue(i / DS);
+        if constexpr (i < 6) next_b(i);
+        if constexpr (i >= IPWA * DS && i < IPWA * DS + 4) next_a(i - IPWA * DS);
         if constexpr (i == MF - 1) issue_advance();
         __builtin_amdgcn_sched_barrier(0);
       });

@@ -128,7 +128,7 @@ Plan plan(int dtype, Dir dir, const Call& c, bool streams, size_t scratch) {
     const bool stream = r.kernel >= STREAM_256;
     if (stream && !streams) break;
     const double tiles = tiles_of(dir, c.rows, c.m, c.n, c.groups, r.h, r.w), stages = (double)(i64)((K + r.depth - 1) / r.depth);
-    const double stage = r.stage * (dir == FWD && (r.kernel == STREAM_256x128 || r.kernel == STREAM_128) ? 0.9 : 1.0);      // whole lines
+    const double stage = r.stage * (dir == FWD && stream && r.kernel != STREAM_256 ? 0.9 : 1.0);      // bf16: whole lines; fp32: the fewest instructions beside the multiplications
     // few tiles: their contraction in ranges, whose fp32 sums are added by another launch (7.5 us with the wait between the two, and their way through the caches)
     const bool splittable = dir != WEIGHT && (r.kernel == STREAM_128 || r.kernel >= SINGLE_128);
     for (const int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
