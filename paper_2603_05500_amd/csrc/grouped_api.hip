@@ -72,7 +72,7 @@ size_t operand_bytes(const poetx_grouped_desc* d) {
 }
 size_t workspace_bytes(const poetx_grouped_desc* d) { return d->rows == 0 ? 0 : operand_bytes(d) + parts_bytes(d); }
 
-// The products of a 4-bit weight run on its values, made in the workspace.
+// A 4-bit weight's values, made in the workspace, for the products that do not decode it themselves.
 const void* dense_weight(const poetx_grouped_desc* d, const void* W, const int32_t* offsets, void* ws, hipStream_t st) {
   if (!(d->flags & POETX_GROUPED_W_MX4)) return W;
   StageTimer tm(POETX_STAGE_DEQUANT, st);

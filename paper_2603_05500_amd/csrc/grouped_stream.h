@@ -72,12 +72,18 @@ struct StreamArgs {
   int splits;             // FWD, INPUT: ranges of the contraction, whose sums go to [split][rows][N] at C; 1: the result does
 };
 
-// 16 (4) bytes per lane from base + voff straight into LDS at lds + 16 (4) * lane; zeros from the descriptor's end on.
+// 16 (4) bytes per lane from base + voff straight into LDS at lds + 16 (4) * lane; zeros from the descriptor's end on.  Between M0's write and its use there has to be
+// an instruction.
 __device__ __forceinline__ void dma16b(const u32x4& rsrc, uint32_t voff, uint32_t lds) {
-  asm volatile("buffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "{m0}"(lds) : "memory");
+  asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "{m0}"(lds) : "memory");
 }
 __device__ __forceinline__ void dma4b(const u32x4& rsrc, uint32_t voff, uint32_t lds) {
-  asm volatile("buffer_load_dword %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "{m0}"(lds) : "memory");
+  asm volatile("s_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "{m0}"(lds) : "memory");
+}
+// The same, the lanes in `off` behind the descriptor's end.
+__device__ __forceinline__ void dma16b_but(uint64_t off, const u32x4& rsrc, uint32_t voff, uint32_t lds) {
+  uint32_t v;
+  asm volatile("v_cndmask_b32 %0, %1, %2, %3\n\tbuffer_load_dwordx4 %0, %4, 0 offen lds" : "=&v"(v) : "v"(voff), "v"(0xfffffff0u), "s"(off), "s"(rsrc), "{m0}"(lds) : "memory");
 }
 
 // The same value in every lane, in scalar registers.
@@ -356,18 +362,19 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
     }
     if (FP4 && part == 5) rs[2] = fs.bytes(bytes_on(ikt));
   };
-  auto masked_off = [&](uint32_t v, const uint64_t (&m)[2], int load) __attribute__((always_inline)) {
-    uint32_t o;
-    asm("v_cndmask_b32 %0, %1, %2, %3" : "=v"(o) : "v"(v), "v"(0xfffffff0u), "s"(m[WIDE ? load & 1 : 0]));
-    return o;
-  };
   static_assert(IPWA * DS >= 6 && IPWA * DS + 4 <= MF, "B's descriptor ahead of its loads, A's behind its own");
   static_assert(!WIDE || (IPWA % 2 == 0 && IPWB % 2 == 0), "a wave's loads start with an even one");
   auto issue = [&](int i) __attribute__((always_inline)) {      // load i of the stage (a constant wherever this is called)
-    if (i < IPWA) dma16b(ra, !FP4 && A_K ? masked_off(voffA[i], masked_a, i) : voffA[i], slot_a + (wave * IPWA + i) * 1024);
-    else if (i < IPWA + IPWB)
-      dma16b(rb, FP4 ? voffA[i - IPWA] : B_K ? masked_off(voffB[i - IPWA], masked_b, i - IPWA) : voffB[i - IPWA], slot_b + (wave * IPWB + i - IPWA) * 1024);
-    else {
+    if (i < IPWA) {
+      const uint32_t at = slot_a + (wave * IPWA + i) * 1024;
+      if (!FP4 && A_K) dma16b_but(masked_a[WIDE ? i & 1 : 0], ra, voffA[i], at);
+      else dma16b(ra, voffA[i], at);
+    } else if (i < IPWA + IPWB) {
+      const int l = i - IPWA;
+      const uint32_t at = slot_b + (wave * IPWB + l) * 1024;
+      if (!FP4 && B_K) dma16b_but(masked_b[WIDE ? l & 1 : 0], rb, voffB[l], at);
+      else dma16b(rb, FP4 ? voffA[l] : voffB[l], at);
+    } else {
       const int s = i - IPWA - IPWB;
       dma4b(rs, voffS[s], slot_b + C::B_BYTES + (wave * IPWS + s) * 256);
     }

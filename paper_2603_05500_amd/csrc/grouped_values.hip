@@ -82,9 +82,7 @@ __global__ __launch_bounds__(256) void grouped_values_kernel(ValuesArgs g, int f
   mask();
   auto issue = [&](int i) __attribute__((always_inline)) {      // load i of the unit
     if (i < IPWA) {
-      uint32_t o;
-      asm("v_cndmask_b32 %0, %1, %2, %3" : "=v"(o) : "v"(voffA[i]), "v"(0xfffffff0u), "s"(masked[i & 1]));
-      dma16b(ra, o, stage + (wave * IPWA + i) * 1024);
+      dma16b_but(masked[i & 1], ra, voffA[i], stage + (wave * IPWA + i) * 1024);
     } else if (i < IPWA + IPWB) {
       dma16b(rb, voffB[i - IPWA], stage + A_BYTES + (wave * IPWB + i - IPWA) * 1024);
     } else {
