@@ -16,7 +16,7 @@
 //    as one of 16 x 16 x 32 bf16: the same stream carries four times the products.  The fp32 ones take eight times as long for the bytes: smaller tiles and several
 //    workgroups per CU.
 // What bounds it: large bf16 products by power, as the dense one (16384 rows, 8 groups of 8192 x 4096: 960 to 1015 us, 1.08 to 1.15 PFLOP/s with the ragged tiles); products of codes by the
-// loads of a stage, which take as long as its multiplications (16384 x 4096 by 14336 x 4096 480 us, 4.0 PFLOP/s; without loads 384); many small groups by the weights' bytes (8190 rows,
+// loads of a stage, which take as long as its multiplications (16384 x 4096 by 14336 x 4096 465 us, 4.1 PFLOP/s; without loads 384); many small groups by the weights' bytes (8190 rows,
 // 57 groups of 1376 x 2048, input gradient 92 to 103 us); weight gradients by their stores (8192 rows, 16 groups of 1376 x 2048 104 us for 180 MB).
 #pragma once
 #include <utility>

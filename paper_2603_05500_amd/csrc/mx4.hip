@@ -112,7 +112,7 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint32_t* __r
 
 // What the streaming product of two 4-bit operands reads, in one launch: the rows of X as codes [rows][units] of 64 bytes, and both operands' scales in the order
 // in which its fragments take them (mx4.h).  Read from a buffer's rows, 4 bytes of a line each, the scales were half of the product's requests to L2, and a byte per fragment from LDS
-// a sixth of its time: 16384 x 4096 times 14336 x 4096 with scales in rows, in words by unit, so: 708, 594, 480 us for the product; this launch takes 50 to 55 there.
+// a sixth of its time: 16384 x 4096 times 14336 x 4096 with scales in rows, in words by unit, so: 708, 594, 465 us for the product; this launch takes 50 to 55 there.
 // Workgroups below `quantising` take 64 positions x UPL units of X, the others 64 rows x 64 units of the weight's scales.
 struct OperandArgs {
   const uint16_t* X;
