@@ -111,18 +111,23 @@ void edge_launch(int dtype, Dir dir, Kernel k, const Call& c, hipStream_t st);  
 // whole 16-byte vectors (grouped_stream.hip)
 bool stream_supported(int dtype, Dir dir, const Call& c);
 void stream_launch(int dtype, Dir dir, const Plan& p, const Call& c, void* scratch, hipStream_t st);
+// fp32 sums of a contraction's ranges, [split][rows][cols], added in order into c.out
+void add_parts(int dtype, const void* parts, int splits, int cols, const Call& c, hipStream_t st);
 // Z = X W^T with X rounded to four bits on the way, W a 4-bit buffer
 bool codes_supported(const poetx_grouped_desc* d, const void* Z, i64 ldz);
 size_t codes_workspace_bytes(const poetx_grouped_desc* d);
 void codes_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, void* ws, hipStream_t st);
 
-// Z = X W^T with W a 4-bit buffer, decoded on the way (grouped_values.hip): whole 16-byte vectors; false where it is better written out first, for which there are `scratch` bytes
+// Z = X W^T with W a 4-bit buffer, decoded on the way (grouped_values.hip): whole 16-byte vectors.  False where another way is the better one: the kernel for a handful of rows if `few`,
+// otherwise the weight written out first, for whose product there are `scratch` bytes.  ws: for sums of parts of the contraction.
 bool values_supported(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Z, i64 ldz);
-bool values_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, size_t scratch, hipStream_t st);
+bool values_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, bool few, void* ws, size_t ws_bytes, size_t scratch,
+                   hipStream_t st);
 
 // the forward of a handful of rows per group (grouped_few.hip): any sizes, strides and alignments
 enum Weight { DENSE_WEIGHT, VALUES_MX4, VALUES_STREAMED_MX4, CODES_MX4 };      // STREAMED: values_launch() takes the call; CODES: of X as well
 bool few_supported(int dtype, Dir dir, i64 rows, int m, int n, int groups, Weight w);
+double few_values_us(const poetx_grouped_desc* d);      // of few_values(), about
 void few_dense(int dtype, const Call& c, hipStream_t st);
 void few_values(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, hipStream_t st);      // 4-bit weight
 void few_codes(const poetx_grouped_desc* d, const void* Xq, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, hipStream_t st);               // 4-bit rows too

@@ -159,12 +159,12 @@ int poetx_grouped_fwd(const poetx_grouped_desc* d, const void* X, int64_t ldx, c
     grouped::codes_launch(d, X, ldx, W, offsets, Z, ldz, ws, st);
     return launch_status();
   }
+  if (values && grouped::values_launch(d, X, ldx, W, offsets, Z, ldz, few, ws, workspace_bytes(d), parts_bytes(d), st)) return launch_status();
   if (few) {
     StageTimer tm(POETX_STAGE_DENSE, st);
     grouped::few_values(d, X, ldx, W, offsets, Z, ldz, st);
     return launch_status();
   }
-  if (values && grouped::values_launch(d, X, ldx, W, offsets, Z, ldz, parts_bytes(d), st)) return launch_status();
   const void* w = dense_weight(d, W, offsets, ws, st);
   if (d->flags & POETX_GROUPED_X_MX4) {
     char* values = (char*)ws + dequantised_bytes(d);

@@ -79,17 +79,20 @@ __global__ __launch_bounds__(256) void add_parts_kernel(const float* __restrict_
   }
 }
 template <class T>
-void add_parts(const StreamArgs& a, const Call& c, hipStream_t st) {
-  const i64 waves = c.rows * ((a.N + 255) / 256);
+void add(const float* parts, int splits, int cols, const Call& c, hipStream_t st) {
+  const i64 waves = c.rows * ((cols + 255) / 256);
   launch_in_rows((waves + 3) / 4, [&](int block0, unsigned count) {
-    hipLaunchKernelGGL(add_parts_kernel<T>, dim3(count), dim3(256), 0, st, (const float*)a.C, a.splits, c.rows, a.N, (T*)c.out, c.ld_out, c.offsets, c.groups, waves,
-                       block0);
+    hipLaunchKernelGGL(add_parts_kernel<T>, dim3(count), dim3(256), 0, st, parts, splits, c.rows, cols, (T*)c.out, c.ld_out, c.offsets, c.groups, waves, block0);
   });
 }
 
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 }  // namespace
+
+void add_parts(int dtype, const void* parts, int splits, int cols, const Call& c, hipStream_t st) {
+  dtype == POETX_F32 ? add<float>((const float*)parts, splits, cols, c, st) : add<uint16_t>((const float*)parts, splits, cols, c, st);
+}
 
 bool stream_supported(int dtype, Dir dir, const Call& c) {
   const int es = dtype == POETX_F32 ? 4 : 2, v = 16 / es;
@@ -178,7 +181,7 @@ void stream_launch(int dtype, Dir dir, const Plan& p, const Call& c, void* scrat
     a.ldc = a.N;
   }
   dir == FWD ? pick<FWD>(k, a, st) : pick<INPUT>(k, a, st);
-  if (p.splits > 1) dtype == POETX_F32 ? add_parts<float>(a, c, st) : add_parts<uint16_t>(a, c, st);
+  if (p.splits > 1) add_parts(dtype, a.C, p.splits, a.N, c, st);
 }
 
 // ---- both operands in four bits ---------------------------------------------------------------------

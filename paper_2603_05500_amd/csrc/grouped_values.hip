@@ -24,19 +24,24 @@ struct ValuesArgs {
   const int32_t* offsets;
   i64 rows;
   int m, n, groups, units, tiles_n;
+  int splits;      // PARTS: ranges of the contraction, whose fp32 sums go to parts, [split][rows][n]
+  float* parts;
 };
 
-template <int BM, int BN, int NS>
+template <int BM, int BN, int NS, bool PARTS>
 __global__ __launch_bounds__(256) void grouped_values_kernel(ValuesArgs g, int first) {
   constexpr int A_BYTES = BM * 256, B_BYTES = BN * 64, STAGE_BYTES = A_BYTES + B_BYTES + BN * 4;
   constexpr int IPWA = BM / 16, IPWB = BN / 64, LPU = IPWA + IPWB + 1, TM = BM / 32, TN = BN / 32, MF = TM * TN;
   constexpr int OUT_LD = BN + 8;      // elements of a row of the tile on its way out: 16-byte chunks of 8 rows in different banks
-  static_assert(BN <= 256 && IPWA % 2 == 0 && (NS - 1) * LPU < 64 && NS >= 3 && BM * OUT_LD * 2 <= NS * STAGE_BYTES, "values tile");
+  typedef typename std::conditional<PARTS, float, uint16_t>::type Out;
+  static_assert(BN <= 256 && IPWA % 2 == 0 && (NS - 1) * LPU < 64 && NS >= 3 && BM * OUT_LD * (int)sizeof(Out) <= NS * STAGE_BYTES, "values tile");
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  const int total = count_row_tiles(g.offsets, g.groups, g.rows, BM) * g.tiles_n;
+  const int tiles = count_row_tiles(g.offsets, g.groups, g.rows, BM) * g.tiles_n, total = PARTS ? tiles * g.splits : tiles;
   const int bx = first + (int)blockIdx.x;
   if (bx >= total) return;
-  const int id = xcd_run(bx, total);
+  int id = xcd_run(bx, total);
+  const int split = PARTS ? id / tiles : 0, u0 = PARTS ? g.units * split / g.splits : 0, u1 = PARTS ? g.units * (split + 1) / g.splits : g.units;
+  id -= split * tiles;
   const RowTile t = find_row_tile(g.offsets, g.groups, g.rows, BM, id / g.tiles_n);
   const int n0 = id % g.tiles_n * BN;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1, q4 = lane >> 4, li = lane & 15;
@@ -63,17 +68,17 @@ __global__ __launch_bounds__(256) void grouped_values_kernel(ValuesArgs g, int f
   const i64 wrow = (i64)t.g * g.n + n0;
   // an operand's descriptor at the unit in issue, and the bytes from there on
   u32x4 ra{}, rb{}, rs{};
-  int left_a = uniform((rows - 1) * lda + 2 * g.m), left_b = uniform(cols * ldb), left_s = uniform(cols * g.units * 4);
+  int left_a = uniform((rows - 1) * lda + 2 * g.m - 256 * u0), left_b = uniform(cols * ldb - 64 * u0), left_s = uniform((cols * g.units - u0) * 4);
   auto start = [&](u32x4& r, const void* at, int left) __attribute__((always_inline)) {
     r = u32x4{(uint32_t)uniform((int)(uint64_t)at), (uint32_t)uniform((int)((uint64_t)at >> 32)) & 0xffffu, (uint32_t)left, 0x00020000u};
   };
-  start(ra, g.X + (i64)t.r0 * g.ldx, left_a);
-  start(rb, g.codes + wrow * ldb, left_b);
-  start(rs, g.scales + wrow * g.units * 4, left_s);
+  start(ra, g.X + (i64)t.r0 * g.ldx + u0 * mx4::UNIT, left_a);
+  start(rb, g.codes + wrow * ldb + u0 * 64, left_b);
+  start(rs, g.scales + (wrow * g.units + u0) * 4, left_s);
   const int short_unit = g.m % mx4::UNIT ? g.units - 1 : -1;
   const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   uint32_t stage = lds_base;
-  int iu = 0;
+  int iu = u0;
   uint64_t masked[2];
   auto mask = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -92,7 +97,7 @@ __global__ __launch_bounds__(256) void grouped_values_kernel(ValuesArgs g, int f
   // on to the next unit, a little at a time; behind the last one the descriptors are empty
   auto step = [&](u32x4& r, int& left, int bytes) __attribute__((always_inline)) {
     const uint64_t at = ((uint64_t)r[1] << 32 | r[0]) + bytes;
-    left = iu < g.units ? left - bytes : 0;
+    left = iu < u1 ? left - bytes : 0;
     r[0] = (uint32_t)at;
     r[1] = (uint32_t)(at >> 32);
     r[2] = left > 0 ? left : 0;
@@ -146,7 +151,7 @@ __global__ __launch_bounds__(256) void grouped_values_kernel(ValuesArgs g, int f
     w[0][b] = mx4::to_bf16(code[b][0], scale[b]);
   }
   int slot = 0;
-  for (int u = 0; u < g.units; ++u) {
+  for (int u = u0; u < u1; ++u) {
     in_turn(std::make_integer_sequence<int, 4>{}, [&](auto P) __attribute__((always_inline)) {
       constexpr int p = decltype(P)::value;
       if constexpr (p == 3) {
@@ -181,32 +186,35 @@ __global__ __launch_bounds__(256) void grouped_values_kernel(ValuesArgs g, int f
   for (int a = 0; a < TM; ++a)
 #pragma unroll
     for (int b = 0; b < TN; ++b) asm volatile("" : "+a"(acc[a][b]));
-  // ---- out, as bf16 through LDS, so that every instruction writes whole lines
+  // ---- out through LDS, so that every instruction writes whole lines
   mm::wait_vmcnt_and_barrier<0>();      // no load is left, and every wave has read its last fragments
-  uint16_t* out = (uint16_t*)lds;
+  Out* out = (Out*)lds;
 #pragma unroll
   for (int a = 0; a < TM; ++a)
 #pragma unroll
     for (int b = 0; b < TN; ++b) {
       typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-      *reinterpret_cast<u32x2*>(out + (wm * (BM / 2) + a * 16 + li) * OUT_LD + wn * (BN / 2) + b * 16 + 4 * q4) =
-          u32x2{mm::pack2_bf16(acc[a][b][0], acc[a][b][1]), mm::pack2_bf16(acc[a][b][2], acc[a][b][3])};
+      Out* at = out + (wm * (BM / 2) + a * 16 + li) * OUT_LD + wn * (BN / 2) + b * 16 + 4 * q4;
+      if constexpr (PARTS) *reinterpret_cast<floatx4*>(at) = acc[a][b];
+      else *reinterpret_cast<u32x2*>(at) = u32x2{mm::pack2_bf16(acc[a][b][0], acc[a][b][1]), mm::pack2_bf16(acc[a][b][2], acc[a][b][3])};
     }
   __syncthreads();
-  for (int i = tid; i < BM * BN / 8; i += 256) {
-    const int row = i / (BN / 8), col = i % (BN / 8) * 8;
-    if (row < rows && col < cols) *reinterpret_cast<u32x4*>(g.Z + (t.r0 + row) * g.ldz + n0 + col) = *reinterpret_cast<const u32x4*>(out + row * OUT_LD + col);
+  constexpr int V = 16 / sizeof(Out);
+  for (int i = tid; i < BM * BN / V; i += 256) {
+    const int row = i / (BN / V), col = i % (BN / V) * V;
+    Out* at = PARTS ? (Out*)g.parts + ((i64)split * g.rows + t.r0 + row) * g.n : (Out*)g.Z + (t.r0 + row) * g.ldz;
+    if (row < rows && col < cols) *reinterpret_cast<u32x4*>(at + n0 + col) = *reinterpret_cast<const u32x4*>(out + row * OUT_LD + col);
   }
 }
 
-template <int BM, int BN, int NS>
+template <int BM, int BN, int NS, bool PARTS = false>
 void go(ValuesArgs a, hipStream_t st) {
   constexpr int BYTES = NS * (BM * 256 + BN * 68);
-  auto kern = grouped_values_kernel<BM, BN, NS>;
+  auto kern = grouped_values_kernel<BM, BN, NS, PARTS>;
   static const bool configured = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, BYTES) == hipSuccess;
   (void)configured;
   a.tiles_n = ceil_div(a.n, BN);
-  launch_in_rows((a.groups == 1 ? (a.rows + BM - 1) / BM : most_row_tiles(a.rows, a.groups, BM)) * a.tiles_n,
+  launch_in_rows((a.groups == 1 ? (a.rows + BM - 1) / BM : most_row_tiles(a.rows, a.groups, BM)) * a.tiles_n * (PARTS ? a.splits : 1),
                  [&](int first, unsigned count) { hipLaunchKernelGGL(kern, dim3(count), dim3(256), BYTES, st, a, first); });
 }
 
@@ -216,11 +224,14 @@ bool values_supported(const poetx_grouped_desc* d, const void* X, i64 ldx, const
   return d->d_in % 8 == 0 && d->d_out % 8 == 0 && ldx % 8 == 0 && ldz % 8 == 0 && ((uintptr_t)X & 15) == 0 && ((uintptr_t)Z & 15) == 0 && ldx < (1 << 22) &&
          d->d_in < (1 << 22);
 }
-// The tile that is the fastest by a model of their times, if any is faster than the weight written out and a product of its values.
-// Fitted to 9800 calls of random sizes (256 to 14336), groups (1 to 64) and rows (8 to 16384), each in every way that can take it; with few_supported() the choices take 2 % more
-// time than the best would.  us, 64 x 128 / 128 x 128 / 128 x 256 / values: 14336 x 4096, 128 rows 22.6 / 29 / 46 / 66, 512 rows 71 / 61 / 52 / 88; 2048 x 5632, 1999 rows 52 / 44 / 66 / 69;
-// 64 experts of 1376 x 2048 with 128 rows each 65 / 69 / 81 / 162.  64 x 128 four stages deep, one workgroup per CU: 23.7, 85, 60, 86.
-bool values_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, size_t scratch, hipStream_t st) {
+// The tile and number of ranges of the contraction that are the fastest by a model of their times, if they are faster than the other way: the kernel for a handful of rows (few; here only
+// split contractions are weighed against it, few_supported() having chosen between it and whole ones), or the weight written out and a product of its values.
+// Fitted to 9800 calls of random sizes (256 to 14336), groups (1 to 64) and rows (8 to 16384), each in every way that can take it, and for the ranges to 1800 with few tiles; the choices take
+// 2 to 3 % more time than the best would.  us, 64 x 128 / 128 x 128 / 128 x 256 / values: 14336 x 4096, 128 rows 22.6 / 29 / 46 / 66, 512 rows 71 / 61 / 52 / 88; 2048 x 5632, 1999 rows
+// 52 / 44 / 66 / 69; 64 experts of 1376 x 2048 with 128 rows each 65 / 69 / 81 / 162.  64 x 128 four stages deep, one workgroup per CU: 23.7, 85, 60, 86.
+// Whole / in ranges / few rows: 1152 x 12032, 219 rows 51 / 20 / 41, 832 x 7232, 223 rows 33 / 16 / 25.
+bool values_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, bool few, void* ws, size_t ws_bytes, size_t scratch,
+                   hipStream_t st) {
   struct Tile {
     int h, w;
     double rest, unit;      // us: of a launch; of a unit of a round of 256 tiles
@@ -229,24 +240,38 @@ bool values_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const vo
   };
   static const Tile tiles[] = {{64, 128, 4.4, 0.62, 0.73, 0.05}, {128, 128, 5.1, 1.04, 0.61, 0}, {128, 256, 6.7, 1.71, 0.67, 0}};
   const int units = mx4::units(d->d_in);
-  int best = 0;
+  int best = 0, ranges = 1;
   double least = 1e30;
   for (int i = 0; i < 3; ++i) {
     const Tile& t = tiles[i];
-    const double rounds = tiles_of(FWD, d->rows, d->d_in, d->d_out, d->groups, t.h, t.w) / 256, filled = t.alone + (1 - t.alone) * (rounds < 1 ? rounds : 1);
-    const double whole = d->groups == 1 ? (double)(i64)(rounds + 0.999) : rounds + t.uneven;
-    const double us = t.rest + units * t.unit * (rounds > 1 ? whole : filled);
-    if (us < least) least = us, best = i;
+    const double whole = tiles_of(FWD, d->rows, d->d_in, d->d_out, d->groups, t.h, t.w) / 256;
+    for (const int splits : {1, 2, 3, 4, 6, 8}) {
+      const size_t parts = splits > 1 ? (size_t)splits * d->rows * d->d_out * sizeof(float) : 0;
+      if (splits > 1 && (t.w > 128 || 2 * splits > units || parts > ws_bytes)) break;
+      if (splits == 1 && few) continue;
+      const double rounds = whole * splits, filled = t.alone + (1 - t.alone) * (rounds < 1 ? rounds : 1);
+      const double last = d->groups == 1 ? (double)(i64)(rounds + 0.999) : rounds + t.uneven;
+      double us = t.rest + (units + splits - 1) / splits * t.unit * (rounds > 1 ? last : filled);
+      if (splits > 1) us += 4.5 + 2 * parts / 6e6;      // the launch that adds them, and their way through the caches
+      if (us < least) least = us, best = i, ranges = splits;
+    }
   }
   const Call c{X, nullptr, Wq, Z, ldx, 0, ldz, offsets, d->rows, d->d_in, d->d_out, d->groups, 0};
   const double written = 2.5 + (double)(d->rows < d->groups ? d->rows : d->groups) * d->d_out * d->d_in * 2.53 / 5.5e6;
-  if (least >= written + plan(POETX_BF16, FWD, c, stream_supported(POETX_BF16, FWD, c), scratch).us) return false;
+  if (least >= (few ? few_values_us(d) : written + plan(POETX_BF16, FWD, c, stream_supported(POETX_BF16, FWD, c), scratch).us)) return false;
   StageTimer tm(POETX_STAGE_DENSE, st);
   const mx4::View w = mx4::view(Wq, (i64)d->groups * d->d_out, d->d_in);
-  const ValuesArgs a{(const uint16_t*)X, ldx, w.codes, w.scales, (uint16_t*)Z, ldz, offsets, d->rows, d->d_in, d->d_out, d->groups, units, 0};
-  if (best == 0) go<64, 128, 3>(a, st);
-  else if (best == 1) go<128, 128, 3>(a, st);
-  else go<128, 256, 3>(a, st);
+  const ValuesArgs a{(const uint16_t*)X, ldx, w.codes, w.scales, (uint16_t*)Z, ldz, offsets, d->rows, d->d_in, d->d_out, d->groups, units, 0, ranges, (float*)ws};
+  if (ranges > 1) {
+    best == 0 ? go<64, 128, 3, true>(a, st) : go<128, 128, 3, true>(a, st);
+    add_parts(POETX_BF16, ws, ranges, d->d_out, c, st);
+  } else if (best == 0) {
+    go<64, 128, 3>(a, st);
+  } else if (best == 1) {
+    go<128, 128, 3>(a, st);
+  } else {
+    go<128, 256, 3>(a, st);
+  }
   return true;
 }
 

@@ -463,7 +463,8 @@ def test_grouped_mx4_large(lib, groups, rows, m, n, act):
 @pytest.mark.parametrize("groups,rows,m,n,before,behind", [
     (1, 272, 136, 2056, 0, 0), (1, 300, 1416, 2056, 3, 130), (5, 700, 1032, 1000, 1, 0), (200, 5000, 264, 520, 0, 7), (300, 9000, 128, 136, 0, 0),      # tiles of 64 x 128
     (16, 8192, 512, 512, 0, 0), (2, 2100, 2056, 3000, 0, 5), (1, 1990, 1000, 2048, 9, 9),                                                              # 128 x 128
-    (4, 5000, 2600, 2072, 2, 3), (8, 4096, 1000, 2056, 0, 0), (1, 2100, 2632, 2056, 65, 65)])                                                          # 128 x 256
+    (4, 5000, 2600, 2072, 2, 3), (8, 4096, 1000, 2056, 0, 0), (1, 2100, 2632, 2056, 65, 65),                                                           # 128 x 256
+    (1, 219, 12040, 1152, 0, 0), (8, 106, 11848, 640, 7, 0), (3, 355, 10912, 1568, 0, 9), (1, 1474, 12544, 352, 2, 2)])                                # contractions in parts
 def test_grouped_mx4_decoded_on_the_way(lib, groups, rows, m, n, before, behind):
     """More rows than a handful, with NaN in every row of X that no group has, between its rows and in the weight of a group without rows."""
     counts = spread(groups, rows)
