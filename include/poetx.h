@@ -419,8 +419,8 @@ typedef struct {
 #define POETX_GROUPED_X_MX4 2   /* with W_MX4, forward only: the rows of X are rounded to four bits as well (by the rule
                                    above, along d_in) and the codes are multiplied; the input gradient passes the rounding by */
 
-/* Scratch of the largest of the three calls below; 0 for an invalid descriptor.  16-byte aligned.  4-bit weights need it (values of the weight, or codes of
- * X).  Dense ones use it where a product has few tiles, for fp32 sums of parts of its contraction, and run without (ws = NULL, or smaller) with the contraction
+/* Scratch of the largest of the three calls below; 0 for an invalid descriptor.  16-byte aligned.  4-bit weights need it (values of the weight, sums of
+ * parts of the contraction, or codes of X).  Dense ones use it where a product has few tiles, for fp32 sums of parts of its contraction, and run without (ws = NULL, or smaller) with the contraction
  * unsplit: up to twice as long for such calls, and another order of the sums.  us with / without: bf16 input gradient 414 rows, 7360 -> 1888 31 / 55, forward 637 rows,
  * 5568 -> 512 23 / 36. */
 size_t poetx_grouped_workspace_bytes(const poetx_grouped_desc* desc);
