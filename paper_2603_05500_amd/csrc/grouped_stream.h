@@ -17,7 +17,7 @@
 //    workgroups per CU.
 // What bounds it: large bf16 products by power, as the dense one (16384 rows, 8 groups of 8192 x 4096: 960 to 1015 us, 1.08 to 1.15 PFLOP/s with the ragged tiles); products of codes by the
 // loads of a stage, which take as long as its multiplications (16384 x 4096 by 14336 x 4096 465 us, 4.1 PFLOP/s; without loads 384); many small groups by the weights' bytes (8190 rows,
-// 57 groups of 1376 x 2048, input gradient 92 to 103 us); weight gradients by their stores (8192 rows, 16 groups of 1376 x 2048 104 us for 180 MB).
+// 57 groups of 1376 x 2048, input gradient 92 to 103 us); weight gradients by their stores (8192 rows, 16 groups of 1376 x 2048 93 us for 180 MB).
 #pragma once
 #include <utility>
 
@@ -168,9 +168,21 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   const int per_weight = tiles_m * g.tiles_n;
   const int T = per_weight * (DIR == WEIGHT ? g.groups : g.splits);
   const int G = gridDim.x;
+  // WEIGHT: a group's tiles take as long as it has rows.  Groups go by their size, the largest first, and workgroups through every other round backwards, so that their shares are
+  // alike: 8192 rows, 15 of 16 groups of 1376 x 2048 that have 340 to 1200 of them each, 76 us as they come, 71 so.  Over many rounds shares are alike anyway (12 of 64 groups: 137, 139).
+  // tsum: how many groups come before.
+  const bool by_size = DIR == WEIGHT && g.groups <= 64 && T < 8 * G;
+  if (by_size) {
+    const int mine = tr1[0] - tr0[0];
+    for (int j = 0; j < g.groups; ++j) {
+      const int other = __builtin_amdgcn_readlane(mine, j);
+      tsum[0] += other > mine || (other == mine && j < lane);
+    }
+  }
   int wq = blockIdx.x;
   if ((G & 7) == 0) wq = (wq & 7) * (G >> 3) + (wq >> 3);
-  const int n_my = wq < T ? (T - 1 - wq) / G + 1 : 0;
+  auto place = [&](int ti) { return DIR == WEIGHT && (ti & 1) ? G - 1 - wq : wq; };      // in a round
+  const int n_my = T / G + (place(T / G) < T % G);
   if (n_my == 0) return;
 
   struct Where {
@@ -180,11 +192,12 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   };
   auto locate = [&](int ti) __attribute__((always_inline)) {
     Where w;
-    int u = ti * G + wq;
+    int u = ti * G + place(ti);
     w.gr = w.split = 0;
     if (DIR == WEIGHT) {
       w.gr = u / per_weight;
       u -= w.gr * per_weight;
+      if (by_size) w.gr = __builtin_ctzll(__ballot(tsum[0] == w.gr));
     } else if (g.splits > 1) {
       w.split = u / per_weight;
       u -= w.split * per_weight;
