@@ -114,10 +114,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void slice_kernel(SliceArgs g, Epi e
     const T* a = A0 + (A_K ? k : k * g.lda);
     const T* b = B0 + k * g.ldb;
     const uint32_t at = ring_base + (t % NS) * S::SLICE;
+    // between the write of M0 and a load that uses it there has to be an instruction
 #pragma unroll
-    for (int s = 0; s < NA; ++s) asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(voffA[s]), "s"(a), "{m0}"(at + s * 1024) : "memory");
+    for (int s = 0; s < NA; ++s) asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voffA[s]), "s"(a), "{m0}"(at + s * 1024) : "memory");
 #pragma unroll
-    for (int s = 0; s < NB; ++s) asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(voffB[s]), "s"(b), "{m0}"(at + (NA + s) * 1024) : "memory");
+    for (int s = 0; s < NB; ++s) asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voffB[s]), "s"(b), "{m0}"(at + (NA + s) * 1024) : "memory");
   };
 
   // fp32: a wave's slices go to two sums in turn, which halves the chain that rounding errors add up along.  rms error against 64 bits over 120 products, forward, relative to

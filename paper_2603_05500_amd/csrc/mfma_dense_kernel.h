@@ -129,11 +129,11 @@ __device__ __forceinline__ void pack_pair(const floatx4& x, const floatx4& y, ui
 // 16 bytes per lane from (uniform base + per-lane byte offset + OFF) straight into LDS at
 // lds_group + OFF + 16 * lane: the instruction offset moves the LDS address and the global address
 // alike, so the per-lane offsets of a group of loads are biased by -OFF and the whole group shares
-// one value of M0 (written once by the compiler, which tracks it as an operand).  Completion is
-// tracked by hand through vmcnt.
+// one value of M0 (written by the compiler, which tracks it as an operand).  Between that write and a load
+// there has to be an instruction, which the compiler does not see to here.  Completion is tracked by hand through vmcnt.
 template <int OFF>
 __device__ inline void dma16g(const void* sbase, uint32_t voff, uint32_t lds_group) {
-  asm volatile("global_load_lds_dwordx4 %0, %1 offset:%2" ::"v"(voff), "s"(sbase), "n"(OFF), "{m0}"(lds_group) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 offset:%2" ::"v"(voff), "s"(sbase), "n"(OFF), "{m0}"(lds_group) : "memory");
 }
 // load s of a wave's group of up to four (s is a constant wherever this is called)
 __device__ inline void dma16g_s(int s, const void* sbase, uint32_t voff, uint32_t lds_group) {

@@ -50,8 +50,9 @@ struct DenseQ8Args {
   float* parts;          // whose products go here in fp32, [split][M][N], instead of to C
 };
 
+// as the dense product's loads (mfma_dense_kernel.h)
 __device__ inline void dma4s(const void* sbase, uint32_t voff, uint32_t lds_addr) {
-  asm volatile("global_load_lds_dword %0, %1" ::"v"(voff), "s"(sbase), "{m0}"(lds_addr) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(voff), "s"(sbase), "{m0}"(lds_addr) : "memory");
 }
 
 // A_KMAJOR: forward (weight rows are output rows, contraction along a row).  Otherwise backward

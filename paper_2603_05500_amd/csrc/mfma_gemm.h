@@ -116,9 +116,10 @@ struct Cfg {
 // memory clobber keeps the compiler from moving LDS accesses across the barrier.
 // 16 bytes per lane from global memory straight into LDS at lds_addr + 16 * lane.  Inline
 // asm (not the builtin) so that the compiler does not drain vmcnt before later LDS reads:
-// completion is tracked by hand with wait_vmcnt_and_barrier.  lds_addr is wave uniform.
+// completion is tracked by hand with wait_vmcnt_and_barrier.  lds_addr is wave uniform.  Between the
+// write of M0 and its use the instruction set asks for another instruction.
 __device__ inline void dma16(const void* gptr, uint32_t lds_addr) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_addr), "v"(gptr) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_addr), "v"(gptr) : "memory");
 }
 
 // This wave's LDS accesses have been carried out, and every other wave's; memory traffic stays in flight, which __syncthreads() would wait for.
