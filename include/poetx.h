@@ -399,8 +399,8 @@ int poetx_mx4_dequantize(const void* Q, int64_t rows, int32_t cols, int32_t dtyp
  * POETX_GROUPED_W_MX4 one 4-bit buffer of groups * d_out rows of d_in; bf16 only.  offsets: groups + 1 int32 on the
  * device, non-decreasing, 0 <= offsets <= rows.  They are read on the device alone, so a router's answer needs no
  * copy to the host.  Groups may be empty.  Rows that no group has are neither read nor written; offsets outside
- * 0 .. rows are taken as the nearer end and a decreasing pair as an empty group, so that nothing outside the tensors is
- * ever touched.  Products of bf16 are exact and summed in fp32, and a result is rounded once.
+ * 0 .. rows are taken as the nearer end, and one below those before it as the largest of them (a decreasing pair is an
+ * empty group), so that nothing outside the tensors is ever touched and no row belongs to two groups.  Products of bf16 are exact and summed in fp32, and a result is rounded once.
  * Every sum has one order, so results are reproducible run to run.
  * Which kernels run follows from the descriptor, the strides, the alignment and the scratch, never from the offsets: tensors of whole 16-byte
  * vectors (pointers, leading dimensions, d_in and d_out) with up to 256 groups on streaming matrix-core kernels, a handful of forward rows per group on

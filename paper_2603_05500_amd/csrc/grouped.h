@@ -22,16 +22,58 @@ struct Call {
   int accumulate;
 };
 
-// First row and end of group g, inside the tensor whatever the offsets say.
+// First row and end of a group.  Offsets are taken inside the tensor, and none below those before it: whatever they say, groups share no row, so that every row
+// has one result and the grids, which are made for that, hold every tile.
 struct Range {
   int r0, r1;
 };
-__device__ __forceinline__ Range group_range(const int32_t* offsets, int g, i64 rows) {
-  const int last = (int)rows;
-  const int a = offsets[g], b = offsets[g + 1];
-  const int r0 = a < 0 ? 0 : a > last ? last : a;
-  const int r1 = b < r0 ? r0 : b > last ? last : b;
-  return Range{r0, r1};
+__device__ __forceinline__ int offset_at(const int32_t* offsets, int g, i64 rows) {
+  const int a = offsets[g], last = (int)rows;
+  return a < 0 ? 0 : a > last ? last : a;
+}
+// Group g's as far as its own two offsets say: no less than the whole, and the same rows in all the groups together.
+__device__ __forceinline__ Range own_range(const int32_t* offsets, int g, i64 rows) {
+  const int r0 = offset_at(offsets, g, rows), r1 = offset_at(offsets, g + 1, rows);
+  return Range{r0, r1 < r0 ? r0 : r1};
+}
+// Group base + lane's two offsets, past the last group twice the last one; and its range from them.  end: the furthest end below base, 0 at first; moved on.
+__device__ __forceinline__ Range lane_offsets(const int32_t* offsets, int groups, i64 rows, int base) {
+  const int g = base + (int)(threadIdx.x & 63);
+  return Range{offset_at(offsets, g < groups ? g : groups, rows), offset_at(offsets, g + 1 < groups ? g + 1 : groups, rows)};
+}
+__device__ __forceinline__ Range in_order(Range own, int& end) {
+  if (__builtin_expect(__ballot(own.r1 < own.r0 || own.r0 < end) != 0, 0)) {
+    const int lane = threadIdx.x & 63;
+    int most = own.r0 > end ? own.r0 : end;
+#pragma unroll 1
+    for (int s = 1; s < 64; s *= 2) {
+      const int o = __shfl_up(most, s);
+      if (lane >= s && o > most) most = o;
+    }
+    own.r0 = most;
+    own.r1 = own.r1 > most ? own.r1 : most;
+  }
+  end = __builtin_amdgcn_readlane(own.r1, 63);
+  return own;
+}
+// Of group g alone, the same one in every lane.
+__device__ inline Range group_range(const int32_t* offsets, int g, i64 rows) {
+  Range r = own_range(offsets, g, rows);
+  int most = r.r0;
+  for (int j = (int)(threadIdx.x & 63); j < g; j += 64) {
+    const int o = offset_at(offsets, j, rows);
+    most = o > most ? o : most;
+  }
+  if (__builtin_expect(__ballot(most > r.r0) != 0, 0)) {
+#pragma unroll 1
+    for (int s = 1; s < 64; s *= 2) {
+      const int o = __shfl_xor(most, s);
+      most = o > most ? o : most;
+    }
+    r.r0 = most;
+    r.r1 = r.r1 > most ? r.r1 : most;
+  }
+  return r;
 }
 
 // Sum over a wave of the values of lower lanes and this one.
@@ -47,15 +89,10 @@ __device__ __forceinline__ int wave_scan(int v) {
 
 // Tiles of `height` rows of all groups; a group's last tile may be short.
 __device__ inline int count_row_tiles(const int32_t* offsets, int groups, i64 rows, int height) {
-  const int lane = threadIdx.x & 63;
-  int total = 0;
+  int total = 0, end = 0;
   for (int base = 0; base < groups; base += 64) {
-    int t = 0;
-    if (base + lane < groups) {
-      const Range r = group_range(offsets, base + lane, rows);
-      t = (r.r1 - r.r0 + height - 1) / height;
-    }
-    total += __builtin_amdgcn_readlane(wave_scan(t), 63);
+    const Range r = in_order(lane_offsets(offsets, groups, rows, base), end);
+    total += __builtin_amdgcn_readlane(wave_scan((r.r1 - r.r0 + height - 1) / height), 63);
   }
   return total;
 }
@@ -64,15 +101,10 @@ struct RowTile {
   int g, r0, r1;
 };
 __device__ inline RowTile find_row_tile(const int32_t* offsets, int groups, i64 rows, int height, int u) {
-  const int lane = threadIdx.x & 63;
+  int end = 0;
   for (int base = 0; base < groups; base += 64) {
-    int t = 0;
-    Range r{0, 0};
-    if (base + lane < groups) {
-      r = group_range(offsets, base + lane, rows);
-      t = (r.r1 - r.r0 + height - 1) / height;
-    }
-    const int sum = wave_scan(t), all = __builtin_amdgcn_readlane(sum, 63);
+    const Range r = in_order(lane_offsets(offsets, groups, rows, base), end);
+    const int t = (r.r1 - r.r0 + height - 1) / height, sum = wave_scan(t), all = __builtin_amdgcn_readlane(sum, 63);
     if (u < all) {
       const int l = __builtin_ctzll(__ballot(sum > u));      // all > u: some lane has it
       const int before = __builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(t, l);
@@ -83,7 +115,7 @@ __device__ inline RowTile find_row_tile(const int32_t* offsets, int groups, i64 
   return RowTile{0, 0, 0};
 }
 
-// Row tiles that any offsets of so many groups and rows can have.
+// Row tiles that any offsets of so many groups and rows can have: groups share no row.
 inline i64 most_row_tiles(i64 rows, int groups, int height) { return rows / height + (rows < groups ? rows : groups); }
 
 // Workgroup bx of `total` that work: consecutive ones go to the 8 XCDs in turn, so that XCD's take contiguous runs of the work.

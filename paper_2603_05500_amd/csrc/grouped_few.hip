@@ -46,7 +46,7 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(FewArgs a, int fir
   const int rt_no = bx / a.tiles_n, n0 = bx % a.tiles_n * (16 * RT);
   RowTile t;
   if (a.groups == 1) {
-    const Range r = group_range(a.offsets, 0, a.rows);
+    const Range r = own_range(a.offsets, 0, a.rows);
     t = RowTile{0, r.r0 + rt_no * (16 * NT), r.r1};
   } else {
     t = find_row_tile(a.offsets, a.groups, a.rows, 16 * NT, rt_no);

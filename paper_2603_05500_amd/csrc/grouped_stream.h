@@ -150,12 +150,13 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   // ---- the groups: lane l of set q has group 64 q + l
   constexpr int kTableSets = C::SETS;
   int tr0[kTableSets], tr1[kTableSets], tsum[kTableSets];
-  int row_tiles = 0;
+  int row_tiles = 0, end = 0;
+  Range own[kTableSets];
+#pragma unroll
+  for (int q = 0; q < kTableSets; ++q) own[q] = 64 * q < g.groups ? lane_offsets(g.offsets, g.groups, g.rows, 64 * q) : Range{0, 0};
 #pragma unroll
   for (int q = 0; q < kTableSets; ++q) {
-    const int gr = 64 * q + lane;
-    Range r{0, 0};
-    if (gr < g.groups) r = group_range(g.offsets, gr, g.rows);
+    const Range r = 64 * q < g.groups ? in_order(own[q], end) : Range{0, 0};
     tr0[q] = r.r0;
     tr1[q] = r.r1;
     tsum[q] = 0;

@@ -63,7 +63,7 @@ __global__ __launch_bounds__(256) void add_parts_kernel(const float* __restrict_
   bool has = false;
   for (int base = 0; base < groups && !has; base += 64) {
     Range r{0, 0};
-    if (base + lane < groups) r = group_range(offsets, base + lane, rows);
+    if (base + lane < groups) r = own_range(offsets, base + lane, rows);
     has = __ballot(r.r0 <= row && row < r.r1) != 0;
   }
   if (!has || col >= cols) return;

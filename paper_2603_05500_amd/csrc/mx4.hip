@@ -85,7 +85,7 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint32_t* __r
   i64 block = block0 + (i64)blockIdx.x, base = 0;
   if constexpr (GROUPS) {
     const int g = (int)(block / per_group);
-    const grouped::Range r = grouped::group_range(offsets, g, rows);
+    const grouped::Range r = grouped::own_range(offsets, g, rows);
     if (r.r0 == r.r1) return;
     block -= (i64)g * per_group;
     base = g * total;
@@ -134,14 +134,10 @@ __global__ __launch_bounds__(256) void mx4_operands_kernel(OperandArgs a, int bl
     const int across = (a.units + UPL - 1) / UPL, u0 = bx % across * UPL;
     const i64 p0 = (i64)(bx / across) * 64;
     // the group that has these positions, if any
-    int local = -1, r0 = 0, r1 = 0;
+    int local = -1, r0 = 0, r1 = 0, end = 0;
     for (int base = 0; base < a.groups && local < 0; base += 64) {
-      grouped::Range r{0, 0};
-      i64 at = -1;
-      if (base + lane < a.groups) {
-        r = grouped::group_range(a.offsets, base + lane, a.rows);
-        at = p0 - mx4::position(r.r0, base + lane);
-      }
+      const grouped::Range r = grouped::in_order(grouped::lane_offsets(a.offsets, a.groups, a.rows, base), end);
+      const i64 at = p0 - mx4::position(r.r0, base + lane);
       const uint64_t has = __ballot(at >= 0 && at < r.r1 - r.r0);
       if (has) {
         const int l = __builtin_ctzll(has);

@@ -1,0 +1,86 @@
+"""Offsets that are not in order, or point outside the rows: every kernel of the grouped calls gives every row the group that the header says, and touches nothing else.
+
+The oracle takes offsets inside 0 .. rows and none below those before it, so that group g has the rows from the largest of offsets[0 .. g] to the largest of offsets[0 .. g + 1].
+Bounds as in test_gpu_grouped.py."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2603_05500_amd as px
+from tests.test_gpu_grouped import CODE, DT, quantised, reference, strided, within
+
+pytestmark = pytest.mark.gpu
+
+
+def disorder(kind, groups, rows):
+    """groups + 1 int32 offsets."""
+    rng = np.random.default_rng(groups + rows)
+    off = np.sort(rng.integers(0, rows + 1, groups + 1))
+    if kind == "back and forth":              # most rows claimed by several pairs, the last tenth by one
+        off = np.where(np.arange(groups + 1) % 2, rows * 9 // 10, 0)
+        off[-1] = rows
+    elif kind == "some anywhere":
+        off[1::3] = rng.integers(0, rows + 1, len(off[1::3]))
+    elif kind == "outside":
+        off = off * 2 - rows // 2
+        off[0], off[groups // 2], off[-1] = -2 ** 31, -7, 2 ** 31 - 1
+    elif kind == "last first":
+        off = off[::-1].copy()
+    elif kind == "below":
+        off = off - rows - 1
+    elif kind == "above":
+        off = off + rows
+    return off
+
+
+KINDS = ["back and forth", "some anywhere", "outside", "last first", "below", "above"]
+CALLS = [
+    # dtype, weight, act, groups, rows, d_in, d_out
+    ("bf16", "dense", "same", 4, 100, 128, 128), ("f32", "dense", "same", 4, 100, 128, 128),                                              # a handful of rows
+    ("bf16", "dense", "same", 5, 1000, 130, 258), ("f32", "dense", "same", 5, 1000, 130, 258),                                            # edges
+    ("bf16", "dense", "same", 300, 2000, 128, 136),
+    ("bf16", "dense", "same", 8, 5000, 1032, 3000), ("bf16", "dense", "same", 64, 6000, 520, 1376), ("bf16", "dense", "same", 200, 3000, 256, 512),      # streams
+    ("f32", "dense", "same", 8, 3000, 512, 768), ("bf16", "dense", "same", 5, 788, 7808, 1248), ("f32", "dense", "same", 3, 1140, 1760, 576),            # split contractions
+    ("bf16", "mx4", "same", 64, 300, 256, 1376), ("bf16", "mx4", "same", 5, 700, 1032, 1000), ("bf16", "mx4", "same", 16, 8192, 512, 512),               # 4-bit weights
+    ("bf16", "mx4", "same", 4, 5000, 2600, 2072), ("bf16", "mx4", "same", 8, 106, 11848, 640), ("bf16", "mx4", "same", 4, 3000, 200, 500),
+    ("bf16", "mx4", "mx4", 64, 300, 256, 1376), ("bf16", "mx4", "mx4", 8, 5000, 1032, 3000), ("bf16", "mx4", "mx4", 4, 3000, 200, 500),                  # both
+]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype,weight,act,groups,rows,m,n", CALLS)
+def test_offsets_not_in_order(lib, dtype, weight, act, groups, rows, m, n, kind):
+    offsets = disorder(kind, groups, rows)
+    ends = np.maximum.accumulate(np.clip(offsets, 0, rows))
+    counts, first, last = np.diff(ends).tolist(), int(ends[0]), int(ends[-1])
+    off, dt = torch.from_numpy(offsets.astype(np.int32)).cuda(), DT[dtype]
+    g = torch.Generator(device="cuda").manual_seed(groups + rows)
+    X, dZ = (torch.full((rows, d), float("nan"), device="cuda", dtype=dt) for d in (m, n))      # rows of no group stay NaN
+    for t in (X, dZ):
+        t[first: last] = torch.randn((last - first, t.shape[1]), device="cuda", generator=g).to(dt)
+    W = (torch.randn((groups, n, m), device="cuda", generator=g) * 0.02).to(dt)
+    Wx, Xr, flags = W, X[first: last], 0
+    if weight == "mx4":
+        Wx, flags = quantised(W.view(groups * n, m)), px.GROUPED_W_MX4
+        px.poetx_mx4_dequantize(Wx, W.view(groups * n, m))
+    if act == "mx4":
+        flags |= px.GROUPED_X_MX4
+        if last > first:
+            Xr = torch.empty_like(Xr)
+            px.poetx_mx4_dequantize(quantised(X[first: last]), Xr)
+    desc = px.make_grouped_desc(m, n, groups, rows, CODE[dtype], flags)
+    ws = torch.full((max(256, px.poetx_grouped_workspace_bytes(desc)),), 255, dtype=torch.uint8, device="cuda")
+    for call, x, xr, d, contraction, which in ((px.poetx_grouped_fwd, X, Xr, n, m, "fwd"), (px.poetx_grouped_bwd_input, dZ, dZ[first: last], m, n, "input")):
+        out, flat = strided(rows, d, 8, dt, 8, fill=3.0)
+        call(desc, x, Wx, off, out, ws)
+        assert within(out[first: last], *reference(which, xr, W, counts), contraction, dtype), which
+        out[first: last] = 3.0
+        assert bool((flat == 3.0).all()), (which, "written where no group is")
+    if weight == "dense":
+        flat = torch.full((groups * n * m + 64,), 3.0, device="cuda")
+        dW = flat[: groups * n * m].view(groups, n, m)
+        px.poetx_grouped_bwd_weight(desc, X, dZ, off, dW, False, ws)
+        ref, mag = reference("weight", X[first: last], None, counts, dZ[first: last])
+        assert within(dW, ref, mag, rows, "f32") and bool((flat[groups * n * m:] == 3.0).all())
