@@ -437,7 +437,7 @@ int poetx_grouped_bwd_weight(const poetx_grouped_desc* desc, const void* X, int6
 /* The order that puts rows group by group: ids[n] (int32, the group of each row; a value outside 0 .. groups - 1 is a
  * row that no group takes) -> offsets[groups + 1], order[n]: order[offsets[g] .. offsets[g+1] - 1] are the rows of g,
  * ascending; order past offsets[groups] is -1.  With several choices per token, row i of ids[n] is choice i % k of token i / k.
- * ws: poetx_group_order_workspace_bytes(n, groups) bytes.  Up to POETX_GROUP_ORDER_MAX groups. */
+ * ws: poetx_group_order_workspace_bytes(n, groups) bytes, apart from the other arrays.  Up to POETX_GROUP_ORDER_MAX groups. */
 #define POETX_GROUP_ORDER_MAX 512
 size_t poetx_group_order_workspace_bytes(int64_t n, int32_t groups);
 int poetx_group_order(const int32_t* ids, int64_t n, int32_t groups, int32_t* offsets, int32_t* order, void* ws, size_t ws_bytes,

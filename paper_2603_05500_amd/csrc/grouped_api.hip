@@ -217,7 +217,10 @@ int poetx_group_order(const int32_t* ids, int64_t n, int32_t groups, int32_t* of
   const size_t ib = 4 * (size_t)n, ob = 4 * ((size_t)groups + 1);
   if (overlap(ids, ib, order, ib) || overlap(ids, ib, offsets, ob) || overlap(order, ib, offsets, ob)) return POETX_ERR_INVALID_ARG;
   const size_t need = group_order_workspace_bytes(n, groups);
-  if (need > 0 && (!ws || ws_bytes < need)) return POETX_ERR_WORKSPACE;
+  if (need > 0) {
+    if (!ws || ((uintptr_t)ws & 3) || ws_bytes < need) return POETX_ERR_WORKSPACE;
+    if (overlap(ws, need, ids, ib) || overlap(ws, need, order, ib) || overlap(ws, need, offsets, ob)) return POETX_ERR_INVALID_ARG;
+  }
   StageTimer tm(POETX_STAGE_LAYOUT, (hipStream_t)stream);
   group_order_launch(ids, n, groups, offsets, order, ws, (hipStream_t)stream);
   return launch_status();
