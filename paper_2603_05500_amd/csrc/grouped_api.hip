@@ -149,7 +149,7 @@ int poetx_grouped_fwd(const poetx_grouped_desc* d, const void* X, int64_t ldx, c
   if (both && few) {
     {
       StageTimer tm(POETX_STAGE_DEQUANT, st);
-      mx4_quantize_launch(POETX_BF16, X, d->rows, d->d_in, ldx, ws, st);
+      mx4_quantize_launch(POETX_BF16, X, d->rows, d->d_in, ldx, ws, st, offsets, d->groups);
     }
     StageTimer tm(POETX_STAGE_DENSE, st);
     grouped::few_codes(d, ws, W, offsets, Z, ldz, st);
@@ -170,7 +170,7 @@ int poetx_grouped_fwd(const poetx_grouped_desc* d, const void* X, int64_t ldx, c
     char* values = (char*)ws + dequantised_bytes(d);
     char* codes = values + align256((size_t)d->rows * d->d_in * 2);
     StageTimer tm(POETX_STAGE_DEQUANT, st);
-    mx4_quantize_launch(POETX_BF16, X, d->rows, d->d_in, ldx, codes, st);
+    mx4_quantize_launch(POETX_BF16, X, d->rows, d->d_in, ldx, codes, st, offsets, d->groups);
     mx4_dequantize_launch(codes, d->rows, d->d_in, POETX_BF16, values, d->d_in, st);
     X = values;
     ldx = d->d_in;

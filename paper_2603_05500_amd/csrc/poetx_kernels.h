@@ -173,7 +173,8 @@ void skew_materialize_tiled_launch(const float* theta, int b, i64 nb, float* Qf,
 void skew_project_tiled_launch(const float* M, int b, i64 nb, float* dtheta, int accumulate, hipStream_t st);
 
 // ---- 4-bit buffers (mx4.hip; layout: mx4.h) -----------------------------------------------------
-void mx4_quantize_launch(int dtype, const void* X, i64 rows, int cols, i64 ld, void* Q, hipStream_t st);
+// offsets: only the rows that one of `groups` groups has (bf16)
+void mx4_quantize_launch(int dtype, const void* X, i64 rows, int cols, i64 ld, void* Q, hipStream_t st, const int32_t* offsets = nullptr, int groups = 0);
 // codes of X (rows x units x 64 bytes), and the scales of X and of the buffer Wq (groups * n rows) in the streaming product's order (mx4.h)
 void mx4_operands_launch(const void* X, i64 rows, int cols, i64 ld, const int32_t* offsets, int groups, int n, const void* Wq, void* codes, void* xs, void* wst,
                          hipStream_t st);

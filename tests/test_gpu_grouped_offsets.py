@@ -84,3 +84,24 @@ def test_offsets_not_in_order(lib, dtype, weight, act, groups, rows, m, n, kind)
         px.poetx_grouped_bwd_weight(desc, X, dZ, off, dW, False, ws)
         ref, mag = reference("weight", X[first: last], None, counts, dZ[first: last])
         assert within(dW, ref, mag, rows, "f32") and bool((flat[groups * n * m:] == 3.0).all())
+
+
+@pytest.mark.parametrize("groups,rows,m,n,before,behind", [(6, 200, 256, 384, 37, 90), (1, 9, 4096, 1024, 3, 5), (8, 4000, 1032, 3000, 100, 301),
+                                                           (4, 3000, 200, 500, 1, 77)])      # few rows; streamed codes; values
+def test_rows_of_no_group_leave_no_trace(lib, groups, rows, m, n, before, behind):
+    """With both operands in four bits: what rows of no group hold shows neither in the output nor in the scratch."""
+    total = before + rows + behind
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    X = torch.randn((total, m), device="cuda", generator=g).bfloat16()
+    Q = quantised((torch.randn((groups * n, m), device="cuda", generator=g) * 0.02).bfloat16())
+    off = (torch.arange(groups + 1, device="cuda") * rows // groups + before).int()
+    desc = px.make_grouped_desc(m, n, groups, total, px.BF16, px.GROUPED_W_MX4 | px.GROUPED_X_MX4)
+    after = []
+    for other in (0.0, 5.0):
+        X[:before] = X[before + rows:] = other
+        ws = torch.full((px.poetx_grouped_workspace_bytes(desc),), 170, dtype=torch.uint8, device="cuda")
+        Z = torch.full((total, n), 3.0, dtype=torch.bfloat16, device="cuda")
+        px.poetx_grouped_fwd(desc, X, Q, off, Z, ws)
+        after.append((ws, Z))
+    assert torch.equal(after[0][0], after[1][0]) and torch.equal(after[0][1], after[1][1])
+    assert not bool((after[0][1][before: before + rows] == 3.0).all())
