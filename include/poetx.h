@@ -419,10 +419,13 @@ typedef struct {
 #define POETX_GROUPED_X_MX4 2   /* with W_MX4, forward only: the rows of X are rounded to four bits as well (by the rule
                                    above, along d_in) and the codes are multiplied; the input gradient passes the rounding by */
 
-/* Scratch of the largest of the three calls below; 0 for an invalid descriptor.  16-byte aligned.  4-bit weights need it (values of the weight, sums of
- * parts of the contraction, or codes of X).  Dense ones use it where a product has few tiles, for fp32 sums of parts of its contraction, and run without (ws = NULL, or smaller) with the contraction
- * unsplit: up to twice as long for such calls, and another order of the sums.  us with / without: bf16 input gradient 414 rows, 7360 -> 1888 31 / 55, forward 637 rows,
- * 5568 -> 512 23 / 36. */
+/* Scratch of the largest of the three calls below; 0 for an invalid descriptor.  16-byte aligned, apart from the tensors.  What runs in less of it (ws = NULL, smaller, or not aligned):
+ *   dense weights      every call.  The scratch is for fp32 sums of parts of the contraction where a product has few tiles; without them it takes up to twice as long for such calls, in another
+ *                      order of the sums.  us with / without: bf16 input gradient 414 rows, 7360 -> 1888 31 / 55, forward 637 rows, 5568 -> 512 23 / 36.
+ *   W_MX4              the forward, which can always decode the weight on the way; bytes for sums of parts are used if there are any.  The size asked for holds the weight's values as well, for the input
+ *                      gradient, which needs them, and for the forwards that are faster so.  us in all of it / none: 1 row by 14336 x 4096 10 / 10, 4096 rows 411 / 399,
+ *                      16384 rows by 4096 x 4096 411 / 446, few tiles (219 rows, 12032 -> 1152) 20 / 41, no whole 16-byte vectors (4096 rows, 4001 -> 4001) 396 / 670.
+ *   W_MX4 and X_MX4    nothing: codes of X, re-laid scales, or the values of both are made there. */
 size_t poetx_grouped_workspace_bytes(const poetx_grouped_desc* desc);
 
 int poetx_grouped_fwd(const poetx_grouped_desc* desc, const void* X, int64_t ldx, const void* W, const int32_t* offsets,

@@ -151,9 +151,9 @@ size_t codes_workspace_bytes(const poetx_grouped_desc* d);
 void codes_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, void* ws, hipStream_t st);
 
 // Z = X W^T with W a 4-bit buffer, decoded on the way (grouped_values.hip): whole 16-byte vectors.  False where another way is the better one: the kernel for a handful of rows if `few`,
-// otherwise the weight written out first, for whose product there are `scratch` bytes.  ws: for sums of parts of the contraction.
+// otherwise the weight written out first if `whole`, the workspace holding it, with `scratch` bytes for its product.  ws: for sums of parts of the contraction.
 bool values_supported(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Z, i64 ldz);
-bool values_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, bool few, void* ws, size_t ws_bytes, size_t scratch,
+bool values_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, bool few, bool whole, void* ws, size_t ws_bytes, size_t scratch,
                    hipStream_t st);
 
 // the forward of a handful of rows per group (grouped_few.hip): any sizes, strides and alignments

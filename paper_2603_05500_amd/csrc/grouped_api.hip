@@ -92,9 +92,11 @@ void product(const poetx_grouped_desc* d, grouped::Dir dir, const grouped::Call&
   else grouped::edge_launch(dtype, dir, p.kernel, c, st);
 }
 
-// Forward and input gradient: in is rows x d_i, out rows x d_o.
+inline bool enough(const poetx_grouped_desc* d, const void* ws, size_t ws_bytes) { return ws && ((uintptr_t)ws & 15) == 0 && ws_bytes >= workspace_bytes(d); }
+
+// Forward and input gradient: in is rows x d_i, out rows x d_o.  needs_ws: the call cannot do without its scratch.
 int check_rows_call(const poetx_grouped_desc* d, const void* in, i64 ld_in, int d_i, const void* W, const int32_t* offsets, const void* out, i64 ld_out,
-                    int d_o, const void* ws, size_t ws_bytes) {
+                    int d_o, bool needs_ws, const void* ws, size_t ws_bytes) {
   const int rc = check_desc(d);
   if (rc != POETX_OK) return rc;
   if (!W || !offsets || (d->rows > 0 && (!in || !out))) return POETX_ERR_INVALID_ARG;
@@ -104,8 +106,7 @@ int check_rows_call(const poetx_grouped_desc* d, const void* in, i64 ld_in, int 
   if ((d->flags & POETX_GROUPED_W_MX4) && ((uintptr_t)W & 15)) return POETX_ERR_INVALID_ARG;
   if (overlap(out, ob, in, span(d->rows, d_i, ld_in, es)) || overlap(out, ob, W, weight_bytes(d)) || overlap(out, ob, offsets, 4 * ((size_t)d->groups + 1)))
     return POETX_ERR_INVALID_ARG;
-  // dense weights do without (see the header)
-  if ((d->flags & POETX_GROUPED_W_MX4) && d->rows > 0 && (!ws || ((uintptr_t)ws & 15) || ws_bytes < workspace_bytes(d))) return POETX_ERR_WORKSPACE;
+  if (needs_ws && d->rows > 0 && !enough(d, ws, ws_bytes)) return POETX_ERR_WORKSPACE;
   return POETX_OK;
 }
 
@@ -140,10 +141,11 @@ size_t poetx_grouped_workspace_bytes(const poetx_grouped_desc* desc) { return ch
 
 int poetx_grouped_fwd(const poetx_grouped_desc* d, const void* X, int64_t ldx, const void* W, const int32_t* offsets, void* Z, int64_t ldz, void* ws,
                       size_t ws_bytes, void* stream) {
-  const int rc = check_rows_call(d, X, ldx, d ? d->d_in : 0, W, offsets, Z, ldz, d ? d->d_out : 0, ws, ws_bytes);
+  // dense weights do without scratch, and so does a 4-bit one: it can always be decoded on the way (see the header)
+  const int rc = check_rows_call(d, X, ldx, d ? d->d_in : 0, W, offsets, Z, ldz, d ? d->d_out : 0, d && (d->flags & POETX_GROUPED_X_MX4), ws, ws_bytes);
   if (rc != POETX_OK || d->rows == 0) return rc;
   hipStream_t st = (hipStream_t)stream;
-  const bool mx4 = d->flags & POETX_GROUPED_W_MX4, both = d->flags & POETX_GROUPED_X_MX4;
+  const bool mx4 = d->flags & POETX_GROUPED_W_MX4, both = d->flags & POETX_GROUPED_X_MX4, whole = mx4 && enough(d, ws, ws_bytes);
   const bool values = mx4 && !both && grouped::values_supported(d, X, ldx, Z, ldz);
   const bool few = mx4 && grouped::few_supported(d->dtype, grouped::FWD, d->rows, d->d_in, d->d_out, d->groups, both ? grouped::CODES_MX4 : values ? grouped::VALUES_STREAMED_MX4 : grouped::VALUES_MX4);
   if (both && few) {
@@ -159,8 +161,11 @@ int poetx_grouped_fwd(const poetx_grouped_desc* d, const void* X, int64_t ldx, c
     grouped::codes_launch(d, X, ldx, W, offsets, Z, ldz, ws, st);
     return launch_status();
   }
-  if (values && grouped::values_launch(d, X, ldx, W, offsets, Z, ldz, few, ws, workspace_bytes(d), parts_bytes(d), st)) return launch_status();
-  if (few) {
+  if (values) {
+    const size_t sums = whole ? workspace_bytes(d) : ws && ((uintptr_t)ws & 15) == 0 ? ws_bytes : 0;
+    if (grouped::values_launch(d, X, ldx, W, offsets, Z, ldz, few, whole, ws, sums, parts_bytes(d), st)) return launch_status();
+  }
+  if (mx4 && !both && (few || !whole)) {
     StageTimer tm(POETX_STAGE_DENSE, st);
     grouped::few_values(d, X, ldx, W, offsets, Z, ldz, st);
     return launch_status();
@@ -181,7 +186,7 @@ int poetx_grouped_fwd(const poetx_grouped_desc* d, const void* X, int64_t ldx, c
 
 int poetx_grouped_bwd_input(const poetx_grouped_desc* d, const void* dZ, int64_t lddz, const void* W, const int32_t* offsets, void* dX, int64_t lddx,
                             void* ws, size_t ws_bytes, void* stream) {
-  const int rc = check_rows_call(d, dZ, lddz, d ? d->d_out : 0, W, offsets, dX, lddx, d ? d->d_in : 0, ws, ws_bytes);
+  const int rc = check_rows_call(d, dZ, lddz, d ? d->d_out : 0, W, offsets, dX, lddx, d ? d->d_in : 0, d && (d->flags & POETX_GROUPED_W_MX4), ws, ws_bytes);
   if (rc != POETX_OK || d->rows == 0) return rc;
   hipStream_t st = (hipStream_t)stream;
   const void* w = dense_weight(d, W, offsets, ws, st);

@@ -230,7 +230,7 @@ bool values_supported(const poetx_grouped_desc* d, const void* X, i64 ldx, const
 // 2 to 3 % more time than the best would.  us, 64 x 128 / 128 x 128 / 128 x 256 / values: 14336 x 4096, 128 rows 22.6 / 29 / 46 / 66, 512 rows 71 / 61 / 52 / 88; 2048 x 5632, 1999 rows
 // 52 / 44 / 66 / 69; 64 experts of 1376 x 2048 with 128 rows each 65 / 69 / 81 / 162.  64 x 128 four stages deep, one workgroup per CU: 23.7, 85, 60, 86.
 // Whole / in ranges / few rows: 1152 x 12032, 219 rows 51 / 20 / 41, 832 x 7232, 223 rows 33 / 16 / 25.
-bool values_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, bool few, void* ws, size_t ws_bytes, size_t scratch,
+bool values_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, bool few, bool whole, void* ws, size_t ws_bytes, size_t scratch,
                    hipStream_t st) {
   struct Tile {
     int h, w;
@@ -258,7 +258,7 @@ bool values_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const vo
   }
   const Call c{X, nullptr, Wq, Z, ldx, 0, ldz, offsets, d->rows, d->d_in, d->d_out, d->groups, 0};
   const double written = 2.5 + (double)(d->rows < d->groups ? d->rows : d->groups) * d->d_out * d->d_in * 2.53 / 5.5e6;
-  if (least >= (few ? few_values_us(d) : written + plan(POETX_BF16, FWD, c, stream_supported(POETX_BF16, FWD, c), scratch).us)) return false;
+  if (few ? least >= few_values_us(d) : whole && least >= written + plan(POETX_BF16, FWD, c, stream_supported(POETX_BF16, FWD, c), scratch).us) return false;
   StageTimer tm(POETX_STAGE_DENSE, st);
   const mx4::View w = mx4::view(Wq, (i64)d->groups * d->d_out, d->d_in);
   const ValuesArgs a{(const uint16_t*)X, ldx, w.codes, w.scales, (uint16_t*)Z, ldz, offsets, d->rows, d->d_in, d->d_out, d->groups, units, 0, ranges, (float*)ws};
