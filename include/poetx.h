@@ -400,7 +400,8 @@ int poetx_mx4_dequantize(const void* Q, int64_t rows, int32_t cols, int32_t dtyp
  * device, non-decreasing, 0 <= offsets <= rows.  They are read on the device alone, so a router's answer needs no
  * copy to the host.  Groups may be empty.  Rows that no group has are neither read nor written; offsets outside
  * 0 .. rows are taken as the nearer end, and one below those before it as the largest of them (a decreasing pair is an
- * empty group), so that nothing outside the tensors is ever touched and no row belongs to two groups.  Products of bf16 are exact and summed in fp32, and a result is rounded once.
+ * empty group), so that nothing outside the tensors is ever touched and no row of Z or dX belongs to two groups;
+ * the weight gradient of a group sums over the rows that its own two offsets name.  Products of bf16 are exact and summed in fp32, and a result is rounded once.
  * Every sum has one order, so results are reproducible run to run.
  * Which kernels run follows from the descriptor, the strides, the alignment and the scratch, never from the offsets: tensors of whole 16-byte
  * vectors (pointers, leading dimensions, d_in and d_out) with up to 256 groups on streaming matrix-core kernels, a handful of forward rows per group on

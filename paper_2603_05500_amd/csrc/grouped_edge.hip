@@ -39,7 +39,7 @@ __global__ __launch_bounds__(64 * WAVES) void grouped_edge_kernel(Call c, int ti
     const int total = c.groups * tiles_y * tiles_x;
     const int id = xcd_run(bx, total);
     const int gr = id / (tiles_y * tiles_x), t = id % (tiles_y * tiles_x), i0 = t % tiles_y * TILE, j0 = t / tiles_y * TILE;
-    const Range r = group_range(c.offsets, gr, c.rows);
+    const Range r = own_range(c.offsets, gr, c.rows);
     g.A = edge::Op{(const T*)c.in2 + (i64)r.r0 * c.ld_in2 + i0, c.ld_in2, 0, nullptr, r.r1 - r.r0, c.n - i0, 0, 0, 1};
     g.B = edge::Op{(const T*)c.in + (i64)r.r0 * c.ld_in + j0, c.ld_in, 0, nullptr, r.r1 - r.r0, c.m - j0, 0, 0, 1};
     g.stages = (r.r1 - r.r0 + BK - 1) / BK;

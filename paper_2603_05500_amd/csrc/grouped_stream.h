@@ -153,10 +153,15 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   int row_tiles = 0, end = 0;
   Range own[kTableSets];
 #pragma unroll
-  for (int q = 0; q < kTableSets; ++q) own[q] = 64 * q < g.groups ? lane_offsets(g.offsets, g.groups, g.rows, 64 * q) : Range{0, 0};
+  for (int q = 0; q < kTableSets; ++q) {
+    const int gr = 64 * q + lane;
+    own[q] = Range{0, 0};
+    if (DIR == WEIGHT && gr < g.groups) own[q] = own_range(g.offsets, gr, g.rows);
+    if (DIR != WEIGHT && 64 * q < g.groups) own[q] = lane_offsets(g.offsets, g.groups, g.rows, 64 * q);
+  }
 #pragma unroll
   for (int q = 0; q < kTableSets; ++q) {
-    const Range r = 64 * q < g.groups ? in_order(own[q], end) : Range{0, 0};
+    const Range r = DIR != WEIGHT && 64 * q < g.groups ? in_order(own[q], end) : own[q];
     tr0[q] = r.r0;
     tr1[q] = r.r1;
     tsum[q] = 0;

@@ -60,13 +60,7 @@ __global__ __launch_bounds__(256) void add_parts_kernel(const float* __restrict_
   if (w >= waves) return;
   const i64 row = w / across;
   const int col = (int)(w - row * across) * 256 + 4 * lane;
-  bool has = false;
-  for (int base = 0; base < groups && !has; base += 64) {
-    Range r{0, 0};
-    if (base + lane < groups) r = own_range(offsets, base + lane, rows);
-    has = __ballot(r.r0 <= row && row < r.r1) != 0;
-  }
-  if (!has || col >= cols) return;
+  if (row < offset_at(offsets, 0, rows) || row >= furthest_end(offsets, groups, rows) || col >= cols) return;
   const float* p = parts + row * cols + col;
   floatx4 sum = *reinterpret_cast<const floatx4*>(p);
   for (int s = 1; s < splits; ++s) sum += *reinterpret_cast<const floatx4*>(p + s * rows * cols);
