@@ -1,12 +1,12 @@
-"""A layer of experts on POET-X weights, forward and backward, as one would run it in training.
+"""A layer of experts on POET-X weights, forward and backward: the products that a training step makes of it.
 
     python examples/experts.py                      # experts in four bits, activations in bf16
     python examples/experts.py --activations mx4    # activations of the forward products in four bits as well
     python examples/experts.py --weights dense      # experts that are trained themselves: weight gradients too
 
-Each expert is y = W2 relu(W1 x)^2.  Its base weights carry learned orthogonal factors (blocks of a Cayley-Neumann series
-under a permutation), which are folded in once, as in the outer loop's merge step; frozen experts are then kept in four
-bits.  A router gives every token its experts; tokens are put in the experts' order on the device, and the products of all
+Each expert is y = W2 relu(W1 x)^2.  Its base weights carry orthogonal factors (blocks of a Cayley-Neumann series under a
+permutation; random here), which are folded in once, as in the outer loop's merge step, and not trained any further; frozen
+experts are then kept in four bits, and gradients go to the inputs and the router's shares.  A router gives every token its experts; tokens are put in the experts' order on the device, and the products of all
 experts are one launch each, whatever the router says: no group size ever comes to the host.
 """
 from __future__ import annotations

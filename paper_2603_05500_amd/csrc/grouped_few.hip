@@ -1,7 +1,8 @@
 // Forward products where groups have a handful of rows each (generation; a router's many experts): Z = X W_g^T as one read of the weights.
 //
-// What bounds it: the bytes of the weights.  A wave streams 16 RT rows of a weight straight into registers, all loads of a step in flight at once, as
-// the first operand of 16 x 16 MFMAs whose second one is up to 16 NT rows of X; the waves of a workgroup split the contraction and meet in LDS.
+// What bounds it: the bytes of the weights, and their latency where a wave has a step or two.  A wave streams 16 RT rows of a weight straight into registers, as
+// the first operand of 16 x 16 MFMAs whose second one is up to 16 NT rows of X; the waves of a workgroup split the contraction and meet in LDS.  The compiler decides how many of a step's
+// loads go out before its first wait: 17 of 21 of (16 weight rows, 16 rows, 4 waves, 4 units) on 4-bit values, but 9 of 26 of (32,16,4,4), 16 of them of X, 9 to 12 of the dense ones.
 // A lane's load is 16 bytes of one weight row, whatever they hold:
 //   DENSE   8 bf16, one MFMA of depth 32
 //   SINGLE  4 fp32, four MFMAs of depth 4, the groups of 16 lanes holding every fourth four
@@ -72,7 +73,7 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(FewArgs a, int fir
 #pragma unroll
     for (int c = 0; c < NT; ++c) acc[r][c] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  auto steps = [&](int s, auto N_, auto WHOLE_) __attribute__((always_inline)) {      // that many units of 128, their loads in flight together; WHOLE: inside the rows
+  auto steps = [&](int s, auto N_, auto WHOLE_) __attribute__((always_inline)) {      // that many units of 128; WHOLE: inside the rows
     constexpr int N = decltype(N_)::value;
     constexpr bool WHOLE = decltype(WHOLE_)::value;
     auto values = [&](const auto* row, int k) __attribute__((always_inline)) { return WHOLE ? load16(row + k) : edge::load_branched(row, k, a.m, true); };
@@ -231,7 +232,7 @@ i64 small_tiles(i64 rows, int groups, int n) {
 }
 
 // Tiles of 16 x 16 where there are few in all, whatever the rows; otherwise as many rows of X as an average group has, and more weight rows per wave, as each wave reads its rows of X
-// anew.  us, by (weight rows, rows of X, waves, units in flight), weights from memory:
+// anew.  us, by (weight rows, rows of X, waves, units of a step), weights from memory:
 //   4 bits:  4096 x 4096, 1 row (16,16,4,4) 4.1  (32,16,4,4) 6.0; 16 rows 6.8, 8.2; 14336 x 4096, 1 row (16,16,4,4) 11.2  (32,16,4,4) 9.9  (64,16,8,4) 11.0; 16 rows 21.6, 14.6, 12.5;
 //            eight of 64 experts of 1376 x 2048 a row each 5.8, 6.1, 7.4; all of them with 8 each 45.6, 32.6, 35.8; 14336 x 4096, 32 rows (64,32,4,1) 18.6  (64,64,4,1) 22.7;
 //            1024 x 4096, 64 rows (16,16,4,4) 6.8  (64,64,4,1) 25.8; 4096 x 4096, 128 rows (16,16,4,4) 39  (64,32,4,1) 17.9  (64,64,4,1) 26.7; eight experts, 512 rows 32.9, 19.4, 23.6

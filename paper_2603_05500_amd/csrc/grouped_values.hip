@@ -228,7 +228,7 @@ bool values_supported(const poetx_grouped_desc* d, const void* X, i64 ldx, const
 // split contractions are weighed against it, few_supported() having chosen between it and whole ones), or the weight written out and a product of its values.
 // Fitted to 9800 calls of random sizes (256 to 14336), groups (1 to 64) and rows (8 to 16384), each in every way that can take it, and for the ranges to 1800 with few tiles; the choices take
 // 2 to 3 % more time than the best would.  us, 64 x 128 / 128 x 128 / 128 x 256 / values: 14336 x 4096, 128 rows 22.6 / 29 / 46 / 66, 512 rows 71 / 61 / 52 / 88; 2048 x 5632, 1999 rows
-// 52 / 44 / 66 / 69; 64 experts of 1376 x 2048 with 128 rows each 65 / 69 / 81 / 162.  64 x 128 four stages deep, one workgroup per CU: 23.7, 85, 60, 86.
+// 52 / 44 / 66 / 69 (three weights in turn; 128 x 128 41 to 43 with the one in the caches); 64 experts of 1376 x 2048 with 128 rows each 65 / 69 / 81 / 162.  64 x 128 four stages deep, one workgroup per CU: 23.7, 85, 60, 86.
 // Whole / in ranges / few rows: 1152 x 12032, 219 rows 51 / 20 / 41, 832 x 7232, 223 rows 33 / 16 / 25.
 bool values_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, bool few, bool whole, void* ws, size_t ws_bytes, size_t scratch,
                    hipStream_t st) {
