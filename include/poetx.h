@@ -172,7 +172,7 @@ int poetx_version(void);
 /* Test hook (process-wide, not for production use): on != 0 routes every call,
  * whatever its dtype, through the plain fp32-FMA kernels instead of the
  * matrix-core kernels, so that the two kernel families can be compared.  The calls on
- * 4-bit buffers, the grouped products and poetx_group_order have one family and ignore it. */
+ * 4-bit and 8-bit buffers, the grouped products, the gated block and poetx_group_order have one family and ignore it. */
 void poetx_debug_force_fma(int on);
 
 /* Stage timing for benchmarks (process-wide; off unless begun).  Between
@@ -419,6 +419,8 @@ typedef struct {
 #define POETX_GROUPED_W_MX4 1   /* W in four bits                                                                  */
 #define POETX_GROUPED_X_MX4 2   /* with W_MX4, forward only: the rows of X are rounded to four bits as well (by the rule
                                    above, along d_in) and the codes are multiplied; the input gradient passes the rounding by */
+#define POETX_GROUPED_X_MX8 4   /* weight gradient only (the other two calls: POETX_ERR_UNSUPPORTED), not with X_MX4: X is an 8-bit buffer (see
+                                   poetx_mx8_bytes) of rows x d_in, and ldx is ignored.  Its values are what the product takes */
 
 /* Scratch of the largest of the three calls below; 0 for an invalid descriptor.  16-byte aligned, apart from the tensors.  What runs in less of it (ws = NULL, smaller, or not aligned):
  *   dense weights      every call.  The scratch is for fp32 sums of parts of the contraction where a product has few tiles; without them it takes up to twice as long for such calls, in another
@@ -426,7 +428,8 @@ typedef struct {
  *   W_MX4              the forward, which can always decode the weight on the way; bytes for sums of parts are used if there are any.  The size asked for holds the weight's values as well, for the input
  *                      gradient, which needs them, and for the forwards that are faster so.  us in all of it / none: 1 row by 14336 x 4096 10 / 10, 4096 rows 411 / 399,
  *                      16384 rows by 4096 x 4096 411 / 446, few tiles (219 rows, 12032 -> 1152) 20 / 41, no whole 16-byte vectors (4096 rows, 4001 -> 4001) 396 / 670.
- *   W_MX4 and X_MX4    nothing: codes of X, re-laid scales, or the values of both are made there. */
+ *   W_MX4 and X_MX4    nothing: codes of X, re-laid scales, or the values of both are made there.
+ *   X_MX8              nothing: X's values are made there. */
 size_t poetx_grouped_workspace_bytes(const poetx_grouped_desc* desc);
 
 int poetx_grouped_fwd(const poetx_grouped_desc* desc, const void* X, int64_t ldx, const void* W, const int32_t* offsets,
@@ -446,6 +449,72 @@ int poetx_grouped_bwd_weight(const poetx_grouped_desc* desc, const void* X, int6
 size_t poetx_group_order_workspace_bytes(int64_t n, int32_t groups);
 int poetx_group_order(const int32_t* ids, int64_t n, int32_t groups, int32_t* offsets, int32_t* order, void* ws, size_t ws_bytes,
                       void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Activations in eight bits: what a training step keeps for its backward pass (the step after the memory-saving variants of
+ * Sec. 3.5, for the activations that recomputation has to start from).  As in the 4-bit buffers, 32 neighbouring elements of a
+ * row share one power of two; each is a signed byte:
+ *   value[i][k] = code[i][k] / 64 * 2^(scale[i][k/32] - 127)
+ *   scale = clamp(floor(log2(max |x|)) + 127, 0, 254); 0 for 32 zeros; 255 where one of them is infinite or NaN: all 32
+ *           then stand for NaN (and have codes 0)
+ *   code  = 64 x 2^(127 - scale) rounded to the nearest whole number, ties to the even one, clamped to [-127, 127].
+ * An element is off by at most 2^-7 of the power of two at or below its block's largest (2^-6 where it is clamped).  A buffer
+ * (poetx_mx8_bytes bytes, 16-byte aligned): rows of cols rounded up to 128 codes; from the next multiple of 256 bytes on the
+ * scale bytes, a row of (cols rounded up to 128) / 32 per row.  Codes and scales past cols are zeros, and have to be in a
+ * buffer that a caller builds itself.  X / out: rows x cols, leading dimension ld >= cols, any alignment of the element type.
+ * out: the values, exact in either type (a code of -128 under scale 254, which quantising never gives, is an infinity).
+ * out must not overlap Q. */
+size_t poetx_mx8_bytes(int64_t rows, int32_t cols);
+int poetx_mx8_quantize(const void* X, int32_t dtype, int64_t rows, int32_t cols, int64_t ld, void* Q, void* stream);
+int poetx_mx8_dequantize(const void* Q, int64_t rows, int32_t cols, int32_t dtype, void* out, int64_t ld, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * The gated feed-forward block over groups of rows (a layer of experts; one group is a plain block), from its input to the
+ * product that its down projection takes:
+ *   G_r = Wg_g X_r,  U_r = Wu_g X_r,  H_r = act(G_r) U_r      for the rows r of every group g
+ *   dG_r = dH_r U_r act'(G_r),  dU_r = dH_r act(G_r)
+ * act: POETX_GATED_SILU  g / (1 + e^-g);  POETX_GATED_GELU  g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2.
+ * A group's weights lie one below the other, W: groups x 2 d_hidden x d_in, gate then up, in `dtype` or with POETX_GATED_W_MX4 one
+ * 4-bit buffer of groups * 2 d_hidden rows of d_in (bf16 only).  So the rest of the backward pass is the grouped products' with
+ * d_out = 2 d_hidden: dG and dU side by side in one rows x 2 d_hidden matrix are the dZ of poetx_grouped_bwd_input (dX) and
+ * poetx_grouped_bwd_weight (dW).
+ * Rows are tokens, row major with leading dimensions of their own; offsets as in the grouped products: on the device,
+ * groups + 1 of them, and whatever they say, no row belongs to two groups.  Rows that no group has are neither read nor written (poetx_gated_bwd: rows before the first
+ * offset and behind the furthest).
+ * Products of bf16 are exact and summed in fp32; H, dG and dU are computed in fp32 from these sums (poetx_gated_bwd: from what was
+ * kept) and rounded once, and so is what is kept.  Every sum has one order: results are reproducible run to run.
+ *   G, U          rows x d_hidden, both with leading dimension ldgu (e.g. the halves of one matrix); with
+ *                 POETX_GATED_HELD_MX8 8-bit buffers of rows x d_hidden (poetx_mx8_bytes), ldgu being ignored.  16-byte aligned then
+ * Outputs must not overlap the span of an input from its first to its last element, nor each other (the two of a pair may lie
+ * between each other's rows). */
+typedef enum { POETX_GATED_SILU = 0, POETX_GATED_GELU = 1 } poetx_gated_activation;
+typedef struct {
+  int32_t d_in;        /* m */
+  int32_t d_hidden;    /* n */
+  int32_t groups;
+  int32_t dtype;       /* poetx_dtype of X, H, dH, dG, dU, of a dense W and of G, U unless they are 8-bit buffers */
+  int64_t rows;
+  int32_t flags;       /* POETX_GATED_* bits */
+  int32_t activation;  /* poetx_gated_activation */
+} poetx_gated_desc;
+
+#define POETX_GATED_W_MX4 1      /* W in four bits */
+#define POETX_GATED_HELD_MX8 2   /* G and U are kept in eight bits */
+
+/* Scratch of the larger of poetx_gated_fwd and poetx_gated_bwd_recompute, 16-byte aligned, apart from the tensors; 0 for an
+ * invalid descriptor. */
+size_t poetx_gated_workspace_bytes(const poetx_gated_desc* desc);
+
+/* H (out).  G, U (out): kept for the backward pass, or both NULL. */
+int poetx_gated_fwd(const poetx_gated_desc* desc, const void* X, int64_t ldx, const void* W, const int32_t* offsets, void* H, int64_t ldh,
+                    void* G, void* U, int64_t ldgu, void* ws, size_t ws_bytes, void* stream);
+/* dG, dU (out; leading dimension lddgu) from dH and what the forward kept.  H (out): made again for the weight gradient of the
+ * down projection, or NULL. */
+int poetx_gated_bwd(const poetx_gated_desc* desc, const void* dH, int64_t lddh, const void* G, const void* U, int64_t ldgu, const int32_t* offsets,
+                    void* dG, void* dU, int64_t lddgu, void* H, int64_t ldh, void* stream);
+/* The same where nothing was kept: G and U are made again from X, by the forward's products, and stay on the chip. */
+int poetx_gated_bwd_recompute(const poetx_gated_desc* desc, const void* dH, int64_t lddh, const void* X, int64_t ldx, const void* W,
+                              const int32_t* offsets, void* dG, void* dU, int64_t lddgu, void* H, int64_t ldh, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -21,7 +21,9 @@ FLAG_RECOMPUTE_B = 1
 FLAG_W_INT8 = 2
 FLAG_W_INT8_FUSED = 8
 FLAG_BLOCK_GRADS = 4
-GROUPED_W_MX4, GROUPED_X_MX4 = 1, 2
+GROUPED_W_MX4, GROUPED_X_MX4, GROUPED_X_MX8 = 1, 2, 4
+GATED_W_MX4, GATED_HELD_MX8 = 1, 2
+GATED_SILU, GATED_GELU = 0, 1
 FEATURE_MAJOR, TOKEN_MAJOR = 0, 1
 
 EXPORTS = (
@@ -35,6 +37,8 @@ EXPORTS = (
     "poetx_mx4_bytes", "poetx_mx4_quantize", "poetx_mx4_dequantize",
     "poetx_grouped_workspace_bytes", "poetx_grouped_fwd", "poetx_grouped_bwd_input", "poetx_grouped_bwd_weight",
     "poetx_group_order_workspace_bytes", "poetx_group_order",
+    "poetx_mx8_bytes", "poetx_mx8_quantize", "poetx_mx8_dequantize",
+    "poetx_gated_workspace_bytes", "poetx_gated_fwd", "poetx_gated_bwd", "poetx_gated_bwd_recompute",
 )
 STAGES = ("cnp_fwd", "apply", "dense", "blockgrad", "cnp_bwd", "apply_grad", "layout", "dequant")
 
@@ -48,6 +52,11 @@ class LinearDesc(Structure):
 class GroupedDesc(Structure):
     _fields_ = [("d_in", c_int32), ("d_out", c_int32), ("groups", c_int32), ("dtype", c_int32), ("rows", c_int64),
                 ("flags", c_int32), ("reserved", c_int32)]
+
+
+class GatedDesc(Structure):
+    _fields_ = [("d_in", c_int32), ("d_hidden", c_int32), ("groups", c_int32), ("dtype", c_int32), ("rows", c_int64),
+                ("flags", c_int32), ("activation", c_int32)]
 
 
 class PoetxError(RuntimeError):
@@ -145,6 +154,23 @@ def load_library(path: str | None = None):
     lib.poetx_group_order_workspace_bytes.argtypes = [c_int64, c_int32]
     lib.poetx_group_order.restype = c_int
     lib.poetx_group_order.argtypes = [c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.poetx_mx8_bytes.restype = c_size_t
+    lib.poetx_mx8_bytes.argtypes = [c_int64, c_int32]
+    lib.poetx_mx8_quantize.restype = c_int
+    lib.poetx_mx8_quantize.argtypes = [c_void_p, c_int32, c_int64, c_int32, c_int64, c_void_p, c_void_p]
+    lib.poetx_mx8_dequantize.restype = c_int
+    lib.poetx_mx8_dequantize.argtypes = [c_void_p, c_int64, c_int32, c_int32, c_void_p, c_int64, c_void_p]
+    lib.poetx_gated_workspace_bytes.restype = c_size_t
+    lib.poetx_gated_workspace_bytes.argtypes = [POINTER(GatedDesc)]
+    lib.poetx_gated_fwd.restype = c_int
+    lib.poetx_gated_fwd.argtypes = [POINTER(GatedDesc), c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_int64,
+                                    c_void_p, c_size_t, c_void_p]
+    lib.poetx_gated_bwd.restype = c_int
+    lib.poetx_gated_bwd.argtypes = [POINTER(GatedDesc), c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int64,
+                                    c_void_p, c_int64, c_void_p]
+    lib.poetx_gated_bwd_recompute.restype = c_int
+    lib.poetx_gated_bwd_recompute.argtypes = [POINTER(GatedDesc), c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_int64,
+                                              c_void_p, c_int64, c_void_p, c_size_t, c_void_p]
     _lib = lib
     return lib
 
@@ -431,13 +457,97 @@ def poetx_grouped_bwd_input(desc, dZ, W, offsets, dX, ws=None):
 
 
 def poetx_grouped_bwd_weight(desc, X, dZ, offsets, dW, accumulate, ws=None):
-    """dW: groups x d_out x d_in float32."""
+    """dW: groups x d_out x d_in float32.  With GROUPED_X_MX8 X is an 8-bit buffer of rows x d_in, and ws is needed."""
     lib, dt = load_library(), _grouped_type(desc)
-    x, ldx = _matrix(X, dt, (desc.rows, desc.d_in))
+    if desc.flags & GROUPED_X_MX8:
+        x, ldx = _buffer(X, lib.poetx_mx8_bytes(desc.rows, desc.d_in)), desc.d_in
+    else:
+        x, ldx = _matrix(X, dt, (desc.rows, desc.d_in))
     dz, lddz = _matrix(dZ, dt, (desc.rows, desc.d_out))
     assert dW.dtype is _torch().float32 and dW.numel() == desc.groups * desc.d_out * desc.d_in, "dW: groups x d_out x d_in float32"
     _check(lib.poetx_grouped_bwd_weight(ctypes.byref(desc), x, ldx, dz, lddz, _vector(offsets, desc.groups + 1), _ptr(dW), int(bool(accumulate)),
                                         *_scratch(ws), _stream()), "poetx_grouped_bwd_weight")
+
+
+def poetx_mx8_bytes(rows: int, cols: int) -> int:
+    return load_library().poetx_mx8_bytes(rows, cols)
+
+
+def poetx_mx8_quantize(X, Q):
+    """X: rows x cols (f32 or bf16, rows may be strided) -> Q: uint8 buffer of poetx_mx8_bytes(rows, cols) bytes."""
+    lib, shape = load_library(), X.shape
+    rows, cols = shape
+    x, ld = _matrix(X, X.dtype, shape)
+    _check(lib.poetx_mx8_quantize(x, dtype_code(X), rows, cols, ld, _buffer(Q, lib.poetx_mx8_bytes(rows, cols)), _stream()), "poetx_mx8_quantize")
+
+
+def poetx_mx8_dequantize(Q, out):
+    lib, shape = load_library(), out.shape
+    rows, cols = shape
+    o, ld = _matrix(out, out.dtype, shape)
+    _check(lib.poetx_mx8_dequantize(_buffer(Q, lib.poetx_mx8_bytes(rows, cols)), rows, cols, dtype_code(out), o, ld, _stream()), "poetx_mx8_dequantize")
+
+
+def make_gated_desc(d_in, d_hidden, groups, rows, dtype, activation=GATED_SILU, flags=0) -> GatedDesc:
+    return GatedDesc(d_in, d_hidden, groups, dtype, rows, flags, activation)
+
+
+def poetx_gated_workspace_bytes(desc: GatedDesc) -> int:
+    return load_library().poetx_gated_workspace_bytes(ctypes.byref(desc))
+
+
+def _gated_weight(lib, desc, W):
+    if desc.flags & GATED_W_MX4:
+        return _buffer(W, lib.poetx_mx4_bytes(desc.groups * 2 * desc.d_hidden, desc.d_in))
+    assert W.dtype is _grouped_type(desc) and W.is_contiguous() and W.is_cuda and W.numel() == desc.groups * 2 * desc.d_hidden * desc.d_in, \
+        "W: groups x 2 d_hidden x d_in, gate then up"
+    return W.data_ptr()
+
+
+def _pair(desc, A, B):
+    """Two rows x d_hidden matrices of one leading dimension."""
+    dt, shape = _grouped_type(desc), (desc.rows, desc.d_hidden)
+    (a, lda), (b, ldb) = _matrix(A, dt, shape), _matrix(B, dt, shape)
+    assert lda == ldb, "both matrices of a pair have one leading dimension"
+    return a, b, lda
+
+
+def _held(lib, desc, G, U):
+    if G is None and U is None:
+        return None, None, 0
+    if desc.flags & GATED_HELD_MX8:
+        size = lib.poetx_mx8_bytes(desc.rows, desc.d_hidden)
+        return _buffer(G, size), _buffer(U, size), 0
+    return _pair(desc, G, U)
+
+
+def poetx_gated_fwd(desc, X, W, offsets, H, G=None, U=None, ws=None):
+    """H: rows x d_hidden = act(G) * U with G and U the products of the rows of X with both halves of their group's weight.  G, U: kept for
+    the backward pass, matrices of one leading dimension or (GATED_HELD_MX8) 8-bit buffers."""
+    lib, dt = load_library(), _grouped_type(desc)
+    x, ldx = _matrix(X, dt, (desc.rows, desc.d_in))
+    h, ldh = _matrix(H, dt, (desc.rows, desc.d_hidden))
+    _check(lib.poetx_gated_fwd(ctypes.byref(desc), x, ldx, _gated_weight(lib, desc, W), _vector(offsets, desc.groups + 1), h, ldh, *_held(lib, desc, G, U),
+                               *_scratch(ws), _stream()), "poetx_gated_fwd")
+
+
+def poetx_gated_bwd(desc, dH, G, U, offsets, dG, dU, H=None):
+    """dG, dU and, if given, H again from dH and what poetx_gated_fwd kept."""
+    lib, dt, shape = load_library(), _grouped_type(desc), (desc.rows, desc.d_hidden)
+    dh, lddh = _matrix(dH, dt, shape)
+    h, ldh = (None, 0) if H is None else _matrix(H, dt, shape)
+    _check(lib.poetx_gated_bwd(ctypes.byref(desc), dh, lddh, *_held(lib, desc, G, U), _vector(offsets, desc.groups + 1), *_pair(desc, dG, dU), h, ldh, _stream()),
+           "poetx_gated_bwd")
+
+
+def poetx_gated_bwd_recompute(desc, dH, X, W, offsets, dG, dU, H=None, ws=None):
+    """The same where nothing was kept: G and U are made again from X."""
+    lib, dt, shape = load_library(), _grouped_type(desc), (desc.rows, desc.d_hidden)
+    dh, lddh = _matrix(dH, dt, shape)
+    x, ldx = _matrix(X, dt, (desc.rows, desc.d_in))
+    h, ldh = (None, 0) if H is None else _matrix(H, dt, shape)
+    _check(lib.poetx_gated_bwd_recompute(ctypes.byref(desc), dh, lddh, x, ldx, _gated_weight(lib, desc, W), _vector(offsets, desc.groups + 1), *_pair(desc, dG, dU),
+                                         h, ldh, *_scratch(ws), _stream()), "poetx_gated_bwd_recompute")
 
 
 def poetx_group_order_workspace_bytes(n: int, groups: int) -> int:

@@ -75,6 +75,24 @@ __device__ __forceinline__ u32x4 load_branched(const T* row, int c, int cols, bo
   return v;
 }
 
+// eight elements of a row from column c on, zeros from column cols on
+__device__ __forceinline__ void load8(const uint16_t* row, int c, int cols, float (&v)[8]) {
+  const u32x4 x = load_branched(row, c, cols, true);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __builtin_bit_cast(float, x[i] << 16);
+    v[2 * i + 1] = __builtin_bit_cast(float, x[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void load8(const float* row, int c, int cols, float (&v)[8]) {
+  const u32x4 x = load_branched(row, c, cols, true), y = load_branched(row, c + 4, cols, true);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] = __builtin_bit_cast(float, (uint32_t)x[i]);
+    v[4 + i] = __builtin_bit_cast(float, (uint32_t)y[i]);
+  }
+}
+
 // v without its first n elements, zeros behind them (all zeros from n = 8 on)
 __device__ __forceinline__ u32x4 drop_first(const u32x4& v, int n) {
   typedef unsigned long long u64;

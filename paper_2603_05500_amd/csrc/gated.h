@@ -1,0 +1,68 @@
+// The gated feed-forward block: what its kernels share.
+//   G = X Wg^T, U = X Wu^T, H = act(G) U;   dG = dH U act'(G), dU = dH act(G)
+// act(g) = g s(z), s the logistic function, z = g (silu) or 2 sqrt(2 / pi) (g + 0.044715 g^3) (gelu in its tanh form, as (1 + tanh(z / 2)) / 2 = s(z)); so
+// act'(g) = s (1 + g z'(g) (1 - s)).
+#pragma once
+
+#include "edge_gemm.h"
+#include "grouped.h"
+#include "mx8.h"
+
+namespace poetx {
+namespace gated {
+
+// z = g (c1 + c3 g^2): both activations by the same instructions
+struct Act {
+  float c1, c3;
+};
+inline Act act_of(int activation) { return activation == POETX_GATED_GELU ? Act{1.5957691216057308f, 0.0713548162726002f} : Act{1.f, 0.f}; }
+
+// Its value and derivative.  Beyond 1e18 z keeps its sign (and no zero meets an infinity); beyond 1000 the derivative is 0 or 1 whatever g is, and 1 - s or s is zero.  NaN stays
+// NaN.  exp and the reciprocal are the hardware's, a unit in the last place each; z log2(e) rounded costs e^-z |z| 2^-24 of itself.
+__device__ __forceinline__ void act_both(Act k, float g, float& a, float& da) {
+  const float lo = g < -1e18f ? -1e18f : g, c = lo > 1e18f ? 1e18f : lo;
+  const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * (c * fmaf(k.c3, c * c, k.c1))));
+  const float t = __builtin_amdgcn_fmed3f(g, -1000.f, 1000.f);
+  a = lo * s;
+  da = s * fmaf(t * fmaf(3.f * k.c3, t * t, k.c1), 1.f - s, 1.f);
+}
+__device__ __forceinline__ float act_value(Act k, float g) {
+  float a, da;
+  act_both(k, g, a, da);
+  return a;
+}
+
+// What a call makes of G and U
+enum Mode { FWD, HOLD, HOLD_MX8, BWD };
+struct Out {
+  void* H;            // BWD: may be null
+  void* G;            // HOLD: G and U; BWD: dG and dU; HOLD_MX8: buffers
+  void* U;
+  const void* dH;     // BWD
+  i64 ldh, ldgu, lddh;
+  Act act;
+};
+struct Call {
+  const void* X;
+  const void* W;      // dense: groups x 2n x m, gate then up
+  i64 ldx;
+  const int32_t* offsets;
+  i64 rows;
+  int m, n, groups;
+  Mode mode;
+  Out out;
+};
+
+// Where G and U come from: matrices of the type, 8-bit buffers, or fp32 sums of parts of the contraction, [split][rows][2n]
+enum Source { SAME, MX8, SUMS };
+struct In {
+  const void* G;
+  const void* U;
+  i64 ld;
+  int splits;         // SUMS
+};
+// the rows that some group has, one pass over G and U (gated_rows.hip)
+void rows_launch(int dtype, Source src, const In& in, const int32_t* offsets, int groups, i64 rows, int n, Mode mode, const Out& out, hipStream_t st);
+
+}  // namespace gated
+}  // namespace poetx

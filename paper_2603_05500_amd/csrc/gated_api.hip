@@ -1,0 +1,156 @@
+// C-ABI entry points of the gated feed-forward block: argument checks and kernel dispatch.
+#include "api_checks.h"
+#include "gated.h"
+
+using namespace poetx;
+
+namespace {
+
+int check_desc(const poetx_gated_desc* d) {
+  if (!d || d->d_in <= 0 || d->d_hidden <= 0 || d->groups <= 0 || d->rows < 0 || !dtype_ok(d->dtype)) return POETX_ERR_INVALID_ARG;
+  if ((d->flags & ~(POETX_GATED_W_MX4 | POETX_GATED_HELD_MX8)) != 0 || (d->activation != POETX_GATED_SILU && d->activation != POETX_GATED_GELU)) return POETX_ERR_INVALID_ARG;
+  if ((d->flags & POETX_GATED_W_MX4) && d->dtype != POETX_BF16) return POETX_ERR_UNSUPPORTED;
+  const i64 out = 2 * (i64)d->d_hidden, wide = d->d_in > out ? d->d_in : out;
+  if (wide >= (1 << 24) || d->rows >= (1ll << 30) || d->groups * out >= (1ll << 31) || d->rows * wide >= kMostElements || d->groups * out * d->d_in >= kMostElements)
+    return POETX_ERR_UNSUPPORTED;
+  return POETX_OK;
+}
+
+size_t weight_bytes(const poetx_gated_desc* d) {
+  const i64 rows = 2 * (i64)d->groups * d->d_hidden;
+  return d->flags & POETX_GATED_W_MX4 ? mx4::bytes(rows, d->d_in) : (size_t)rows * d->d_in * esize(d->dtype);
+}
+
+// A tensor of a call: `bytes` from its first element to its last one's end.
+struct Area {
+  const void* p;
+  size_t bytes;
+};
+bool apart(const Area* outs, int no, const Area* ins, int ni) {
+  for (int i = 0; i < no; ++i) {
+    if (!outs[i].p) continue;
+    for (int j = 0; j < ni; ++j)
+      if (ins[j].p && overlap(outs[i].p, outs[i].bytes, ins[j].p, ins[j].bytes)) return false;
+  }
+  return true;
+}
+// Do two matrices of one leading dimension share an element?  They may lie between each other's rows.
+bool pair_apart(const void* a, const void* b, i64 rows, i64 cols, i64 ld, size_t es) {
+  if (!overlap(a, span(rows, cols, ld, es), b, span(rows, cols, ld, es))) return true;
+  const i64 pitch = ld * (i64)es, d = (i64)((uintptr_t)b - (uintptr_t)a) % pitch, off = d < 0 ? d + pitch : d;
+  return off >= cols * (i64)es && pitch - off >= cols * (i64)es;
+}
+
+bool ld_fits(i64 rows, i64 ld) { return rows == 0 || ld < kMostElements / rows; }
+
+// What the 4-bit weight's values take of the workspace; sums of the products follow.
+size_t operand_bytes(const poetx_gated_desc* d) { return d->flags & POETX_GATED_W_MX4 ? align256((size_t)d->groups * 2 * d->d_hidden * d->d_in * 2) : 0; }
+
+grouped::Call product_of(const poetx_gated_desc* d, const void* X, i64 ldx, const void* W, const int32_t* offsets) {
+  return grouped::Call{X, nullptr, W, nullptr, ldx, 0, 2 * (i64)d->d_hidden, offsets, d->rows, d->d_in, 2 * d->d_hidden, d->groups, 0};
+}
+grouped::Plan plan_of(const poetx_gated_desc* d, const grouped::Call& c) {
+  const grouped::Plan p = grouped::plan(d->dtype, grouped::FWD, c, grouped::stream_supported(d->dtype, grouped::FWD, c), ~(size_t)0);
+  return p;
+}
+size_t sums_bytes(const poetx_gated_desc* d) {
+  const grouped::Plan p = plan_of(d, product_of(d, nullptr, d->d_in, nullptr, nullptr));
+  return align256((size_t)p.splits * d->rows * 2 * d->d_hidden * sizeof(float));
+}
+size_t workspace_bytes(const poetx_gated_desc* d) { return d->rows == 0 ? 0 : operand_bytes(d) + sums_bytes(d); }
+
+void products(const poetx_gated_desc* d, const void* X, i64 ldx, const void* W, const int32_t* offsets, gated::Mode mode, const gated::Out& out, void* ws, hipStream_t st) {
+  if (d->flags & POETX_GATED_W_MX4) {
+    StageTimer tm(POETX_STAGE_DEQUANT, st);
+    mx4_dequantize_groups_launch(W, d->groups, 2 * d->d_hidden, d->d_in, offsets, d->rows, ws, st);
+    W = ws;
+  }
+  StageTimer tm(POETX_STAGE_DENSE, st);
+  grouped::Call c = product_of(d, X, ldx, W, offsets);
+  c.out = (char*)ws + operand_bytes(d);
+  const grouped::Plan p = plan_of(d, c);
+  if (p.kernel >= grouped::STREAM_256) grouped::stream_sums(d->dtype, p, c, c.out, st);
+  else grouped::edge_sums(d->dtype, p.kernel, c, st);
+  gated::rows_launch(d->dtype, gated::SUMS, gated::In{c.out, nullptr, 0, p.splits}, offsets, d->groups, d->rows, d->d_hidden, mode, out, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t poetx_gated_workspace_bytes(const poetx_gated_desc* desc) { return check_desc(desc) == POETX_OK ? workspace_bytes(desc) : 0; }
+
+int poetx_gated_fwd(const poetx_gated_desc* d, const void* X, int64_t ldx, const void* W, const int32_t* offsets, void* H, int64_t ldh, void* G, void* U,
+                    int64_t ldgu, void* ws, size_t ws_bytes, void* stream) {
+  const int rc = check_desc(d);
+  if (rc != POETX_OK) return rc;
+  if (!W || !offsets || !G != !U || (d->rows > 0 && (!X || !H))) return POETX_ERR_INVALID_ARG;
+  const bool mx8 = G && (d->flags & POETX_GATED_HELD_MX8);
+  const i64 rows = d->rows, n = d->d_hidden;
+  if (ldx < d->d_in || ldh < n || (G && !mx8 && ldgu < n)) return POETX_ERR_BAD_SHAPE;
+  if (!ld_fits(rows, ldx) || !ld_fits(rows, ldh) || (G && !mx8 && !ld_fits(rows, ldgu))) return POETX_ERR_UNSUPPORTED;
+  const size_t es = esize(d->dtype), kept = rows == 0 ? 0 : mx8 ? mx8::bytes(rows, (int)n) : span(rows, n, ldgu, es);
+  if (((d->flags & POETX_GATED_W_MX4) && ((uintptr_t)W & 15)) || (mx8 && (((uintptr_t)G | (uintptr_t)U) & 15))) return POETX_ERR_INVALID_ARG;
+  const Area outs[] = {{H, span(rows, n, ldh, es)}, {G, kept}, {U, kept}};
+  const Area ins[] = {{X, span(rows, d->d_in, ldx, es)}, {W, weight_bytes(d)}, {offsets, 4 * ((size_t)d->groups + 1)}};
+  if (!apart(outs, 3, ins, 3) || !apart(outs, 1, outs + 1, 2) || (G && rows > 0 && (mx8 ? overlap(G, kept, U, kept) : !pair_apart(G, U, rows, n, ldgu, es))))
+    return POETX_ERR_INVALID_ARG;
+  if (rows == 0) return POETX_OK;
+  const size_t need = workspace_bytes(d);
+  if (need > 0) {
+    if (!ws || ((uintptr_t)ws & 15) || ws_bytes < need) return POETX_ERR_WORKSPACE;
+    const Area scratch[] = {{ws, need}};
+    if (!apart(scratch, 1, ins, 3) || !apart(scratch, 1, outs, 3)) return POETX_ERR_INVALID_ARG;
+  }
+  const gated::Out out{H, G, U, nullptr, ldh, ldgu, 0, gated::act_of(d->activation)};
+  products(d, X, ldx, W, offsets, !G ? gated::FWD : mx8 ? gated::HOLD_MX8 : gated::HOLD, out, ws, (hipStream_t)stream);
+  return launch_status();
+}
+
+int poetx_gated_bwd(const poetx_gated_desc* d, const void* dH, int64_t lddh, const void* G, const void* U, int64_t ldgu, const int32_t* offsets, void* dG, void* dU,
+                    int64_t lddgu, void* H, int64_t ldh, void* stream) {
+  const int rc = check_desc(d);
+  if (rc != POETX_OK) return rc;
+  const i64 rows = d->rows, n = d->d_hidden;
+  if (!offsets || (rows > 0 && (!dH || !G || !U || !dG || !dU))) return POETX_ERR_INVALID_ARG;
+  const bool mx8 = d->flags & POETX_GATED_HELD_MX8;
+  if (lddh < n || (!mx8 && ldgu < n) || lddgu < n || (H && ldh < n)) return POETX_ERR_BAD_SHAPE;
+  if (!ld_fits(rows, lddh) || (!mx8 && !ld_fits(rows, ldgu)) || !ld_fits(rows, lddgu) || (H && !ld_fits(rows, ldh))) return POETX_ERR_UNSUPPORTED;
+  if (mx8 && (((uintptr_t)G | (uintptr_t)U) & 15)) return POETX_ERR_INVALID_ARG;
+  const size_t es = esize(d->dtype), kept = rows == 0 ? 0 : mx8 ? mx8::bytes(rows, (int)n) : span(rows, n, ldgu, es), grads = span(rows, n, lddgu, es);
+  const Area outs[] = {{H, H ? span(rows, n, ldh, es) : 0}, {dG, grads}, {dU, grads}};
+  const Area ins[] = {{dH, span(rows, n, lddh, es)}, {G, kept}, {U, kept}, {offsets, 4 * ((size_t)d->groups + 1)}};
+  if (!apart(outs, 3, ins, 4) || !apart(outs, 1, outs + 1, 2) || (rows > 0 && !pair_apart(dG, dU, rows, n, lddgu, es))) return POETX_ERR_INVALID_ARG;
+  if (rows == 0) return POETX_OK;
+  StageTimer tm(POETX_STAGE_LAYOUT, (hipStream_t)stream);
+  const gated::Out out{H, dG, dU, dH, ldh, lddgu, lddh, gated::act_of(d->activation)};
+  gated::rows_launch(d->dtype, mx8 ? gated::MX8 : gated::SAME, gated::In{G, U, ldgu, 1}, offsets, d->groups, rows, d->d_hidden, gated::BWD, out, (hipStream_t)stream);
+  return launch_status();
+}
+
+int poetx_gated_bwd_recompute(const poetx_gated_desc* d, const void* dH, int64_t lddh, const void* X, int64_t ldx, const void* W, const int32_t* offsets, void* dG,
+                              void* dU, int64_t lddgu, void* H, int64_t ldh, void* ws, size_t ws_bytes, void* stream) {
+  const int rc = check_desc(d);
+  if (rc != POETX_OK) return rc;
+  const i64 rows = d->rows, n = d->d_hidden;
+  if (!W || !offsets || (rows > 0 && (!dH || !X || !dG || !dU))) return POETX_ERR_INVALID_ARG;
+  if (lddh < n || ldx < d->d_in || lddgu < n || (H && ldh < n)) return POETX_ERR_BAD_SHAPE;
+  if (!ld_fits(rows, lddh) || !ld_fits(rows, ldx) || !ld_fits(rows, lddgu) || (H && !ld_fits(rows, ldh))) return POETX_ERR_UNSUPPORTED;
+  if ((d->flags & POETX_GATED_W_MX4) && ((uintptr_t)W & 15)) return POETX_ERR_INVALID_ARG;
+  const size_t es = esize(d->dtype), grads = span(rows, n, lddgu, es);
+  const Area outs[] = {{H, H ? span(rows, n, ldh, es) : 0}, {dG, grads}, {dU, grads}};
+  const Area ins[] = {{dH, span(rows, n, lddh, es)}, {X, span(rows, d->d_in, ldx, es)}, {W, weight_bytes(d)}, {offsets, 4 * ((size_t)d->groups + 1)}};
+  if (!apart(outs, 3, ins, 4) || !apart(outs, 1, outs + 1, 2) || (rows > 0 && !pair_apart(dG, dU, rows, n, lddgu, es))) return POETX_ERR_INVALID_ARG;
+  if (rows == 0) return POETX_OK;
+  const size_t need = workspace_bytes(d);
+  if (need > 0) {
+    if (!ws || ((uintptr_t)ws & 15) || ws_bytes < need) return POETX_ERR_WORKSPACE;
+    const Area scratch[] = {{ws, need}};
+    if (!apart(scratch, 1, ins, 4) || !apart(scratch, 1, outs, 3)) return POETX_ERR_INVALID_ARG;
+  }
+  const gated::Out out{H, dG, dU, dH, ldh, lddgu, lddh, gated::act_of(d->activation)};
+  products(d, X, ldx, W, offsets, gated::BWD, out, ws, (hipStream_t)stream);
+  return launch_status();
+}
+
+}  // extern "C"

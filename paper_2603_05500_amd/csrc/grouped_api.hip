@@ -1,32 +1,16 @@
-// C-ABI entry points of 4-bit buffers, grouped products and the order of groups: argument checks and kernel dispatch.
+// C-ABI entry points of 4-bit and 8-bit buffers, grouped products and the order of groups: argument checks and kernel dispatch.
+#include "api_checks.h"
 #include "grouped.h"
-#include "mx4.h"
+#include "mx8.h"
 
 using namespace poetx;
 
 namespace {
 
-inline bool dtype_ok(int dtype) { return dtype == POETX_F32 || dtype == POETX_BF16; }
-inline size_t esize(int dtype) { return dtype == POETX_F32 ? 4 : 2; }
-// Do a and b, `na` and `nb` bytes from each, share any?  Nothing overlaps nothing.
-inline bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-  const char *x = (const char*)a, *y = (const char*)b;
-  return na > 0 && nb > 0 && x < y + nb && y < x + na;
-}
-// Bytes from the first element of a rows x cols matrix to its last one's end.
-inline size_t span(i64 rows, i64 cols, i64 ld, size_t es) { return rows > 0 ? (size_t)((rows - 1) * ld + cols) * es : 0; }
-constexpr i64 kMostElements = 1ll << 40;
-
-int check_matrix(const void* p, int dtype, i64 rows, int cols, i64 ld) {
-  if (!p || rows <= 0 || cols <= 0 || !dtype_ok(dtype)) return POETX_ERR_INVALID_ARG;
-  if (ld < cols) return POETX_ERR_BAD_SHAPE;
-  if (rows >= (1ll << 40) || ld >= kMostElements / rows) return POETX_ERR_UNSUPPORTED;
-  return POETX_OK;
-}
-
 int check_desc(const poetx_grouped_desc* d) {
   if (!d || d->d_in <= 0 || d->d_out <= 0 || d->groups <= 0 || d->rows < 0 || !dtype_ok(d->dtype) || d->reserved != 0) return POETX_ERR_INVALID_ARG;
-  if ((d->flags & ~(POETX_GROUPED_W_MX4 | POETX_GROUPED_X_MX4)) != 0) return POETX_ERR_INVALID_ARG;
+  if ((d->flags & ~(POETX_GROUPED_W_MX4 | POETX_GROUPED_X_MX4 | POETX_GROUPED_X_MX8)) != 0) return POETX_ERR_INVALID_ARG;
+  if ((d->flags & POETX_GROUPED_X_MX4) && (d->flags & POETX_GROUPED_X_MX8)) return POETX_ERR_INVALID_ARG;
   if ((d->flags & POETX_GROUPED_X_MX4) && !(d->flags & POETX_GROUPED_W_MX4)) return POETX_ERR_INVALID_ARG;
   if ((d->flags & POETX_GROUPED_W_MX4) && d->dtype != POETX_BF16) return POETX_ERR_UNSUPPORTED;
   const i64 wide = d->d_in > d->d_out ? d->d_in : d->d_out;
@@ -70,7 +54,9 @@ size_t operand_bytes(const poetx_grouped_desc* d) {
   const size_t codes = align256(grouped::codes_workspace_bytes(d)), values = dequantised_bytes(d) + rounded_bytes(d);
   return codes > values ? codes : values;
 }
-size_t workspace_bytes(const poetx_grouped_desc* d) { return d->rows == 0 ? 0 : operand_bytes(d) + parts_bytes(d); }
+// 8-bit X, as values
+size_t held_bytes(const poetx_grouped_desc* d) { return align256((size_t)d->rows * d->d_in * esize(d->dtype)); }
+size_t workspace_bytes(const poetx_grouped_desc* d) { return d->rows == 0 ? 0 : d->flags & POETX_GROUPED_X_MX8 ? held_bytes(d) : operand_bytes(d) + parts_bytes(d); }
 
 // A 4-bit weight's values, made in the workspace, for the products that do not decode it themselves.
 const void* dense_weight(const poetx_grouped_desc* d, const void* W, const int32_t* offsets, void* ws, hipStream_t st) {
@@ -99,6 +85,7 @@ int check_rows_call(const poetx_grouped_desc* d, const void* in, i64 ld_in, int 
                     int d_o, bool needs_ws, const void* ws, size_t ws_bytes) {
   const int rc = check_desc(d);
   if (rc != POETX_OK) return rc;
+  if (d->flags & POETX_GROUPED_X_MX8) return POETX_ERR_UNSUPPORTED;
   if (!W || !offsets || (d->rows > 0 && (!in || !out))) return POETX_ERR_INVALID_ARG;
   if (ld_in < d_i || ld_out < d_o) return POETX_ERR_BAD_SHAPE;
   if (d->rows > 0 && (ld_in >= kMostElements / d->rows || ld_out >= kMostElements / d->rows)) return POETX_ERR_UNSUPPORTED;
@@ -196,19 +183,51 @@ int poetx_grouped_bwd_input(const poetx_grouped_desc* d, const void* dZ, int64_t
 
 int poetx_grouped_bwd_weight(const poetx_grouped_desc* d, const void* X, int64_t ldx, const void* dZ, int64_t lddz, const int32_t* offsets, float* dW,
                              int32_t accumulate, void* ws, size_t ws_bytes, void* stream) {
-  (void)ws, (void)ws_bytes;
   const int rc = check_desc(d);
   if (rc != POETX_OK) return rc;
   if (!offsets || !dW || (d->rows > 0 && (!X || !dZ))) return POETX_ERR_INVALID_ARG;
   if (d->flags & POETX_GROUPED_W_MX4) return POETX_ERR_UNSUPPORTED;
+  const bool mx8 = d->flags & POETX_GROUPED_X_MX8;
+  if (mx8) ldx = d->d_in;      // of its values
   if (ldx < d->d_in || lddz < d->d_out) return POETX_ERR_BAD_SHAPE;
   if (d->rows > 0 && (ldx >= kMostElements / d->rows || lddz >= kMostElements / d->rows)) return POETX_ERR_UNSUPPORTED;
   const size_t es = esize(d->dtype), ob = (size_t)d->groups * d->d_out * d->d_in * sizeof(float);
-  if (overlap(dW, ob, X, span(d->rows, d->d_in, ldx, es)) || overlap(dW, ob, dZ, span(d->rows, d->d_out, lddz, es)) ||
-      overlap(dW, ob, offsets, 4 * ((size_t)d->groups + 1)))
-    return POETX_ERR_INVALID_ARG;
-  product(d, grouped::WEIGHT, grouped::Call{X, dZ, nullptr, dW, ldx, lddz, d->d_in, offsets, d->rows, d->d_in, d->d_out, d->groups, accumulate != 0}, nullptr, 0,
-          (hipStream_t)stream);
+  const size_t xb = mx8 && d->rows > 0 ? mx8::bytes(d->rows, d->d_in) : span(d->rows, d->d_in, ldx, es), zb = span(d->rows, d->d_out, lddz, es);
+  if (mx8 && ((uintptr_t)X & 15)) return POETX_ERR_INVALID_ARG;
+  if (overlap(dW, ob, X, xb) || overlap(dW, ob, dZ, zb) || overlap(dW, ob, offsets, 4 * ((size_t)d->groups + 1))) return POETX_ERR_INVALID_ARG;
+  hipStream_t st = (hipStream_t)stream;
+  if (mx8 && d->rows > 0) {
+    if (!enough(d, ws, ws_bytes)) return POETX_ERR_WORKSPACE;
+    const size_t wb = workspace_bytes(d);
+    if (overlap(ws, wb, X, xb) || overlap(ws, wb, dZ, zb) || overlap(ws, wb, dW, ob)) return POETX_ERR_INVALID_ARG;
+    StageTimer tm(POETX_STAGE_DEQUANT, st);
+    mx8_dequantize_launch(X, d->rows, d->d_in, d->dtype, ws, d->d_in, st, offsets, d->groups);
+    X = ws;
+  }
+  product(d, grouped::WEIGHT, grouped::Call{X, dZ, nullptr, dW, ldx, lddz, d->d_in, offsets, d->rows, d->d_in, d->d_out, d->groups, accumulate != 0}, nullptr, 0, st);
+  return launch_status();
+}
+
+size_t poetx_mx8_bytes(int64_t rows, int32_t cols) {
+  if (rows <= 0 || cols <= 0 || rows >= kMostElements / cols) return 0;
+  return mx8::bytes(rows, cols);
+}
+
+int poetx_mx8_quantize(const void* X, int32_t dtype, int64_t rows, int32_t cols, int64_t ld, void* Q, void* stream) {
+  const int rc = check_matrix(X, dtype, rows, cols, ld);
+  if (rc != POETX_OK) return rc;
+  if (!Q || ((uintptr_t)Q & 15) || overlap(X, span(rows, cols, ld, esize(dtype)), Q, mx8::bytes(rows, cols))) return POETX_ERR_INVALID_ARG;
+  StageTimer tm(POETX_STAGE_DEQUANT, (hipStream_t)stream);
+  mx8_quantize_launch(dtype, X, rows, cols, ld, Q, (hipStream_t)stream);
+  return launch_status();
+}
+
+int poetx_mx8_dequantize(const void* Q, int64_t rows, int32_t cols, int32_t dtype, void* out, int64_t ld, void* stream) {
+  const int rc = check_matrix(out, dtype, rows, cols, ld);
+  if (rc != POETX_OK) return rc;
+  if (!Q || ((uintptr_t)Q & 15) || overlap(out, span(rows, cols, ld, esize(dtype)), Q, mx8::bytes(rows, cols))) return POETX_ERR_INVALID_ARG;
+  StageTimer tm(POETX_STAGE_DEQUANT, (hipStream_t)stream);
+  mx8_dequantize_launch(Q, rows, cols, dtype, out, ld, (hipStream_t)stream);
   return launch_status();
 }
 

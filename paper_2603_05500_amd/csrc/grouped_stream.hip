@@ -178,6 +178,24 @@ void stream_launch(int dtype, Dir dir, const Plan& p, const Call& c, void* scrat
   if (p.splits > 1) add_parts(dtype, a.C, p.splits, a.N, c, st);
 }
 
+void stream_sums(int dtype, const Plan& p, const Call& c, void* sums, hipStream_t st) {
+  const int es = dtype == POETX_F32 ? 4 : 2;
+  StreamArgs a = {};
+  a.offsets = c.offsets;
+  a.rows = (int)c.rows;
+  a.groups = c.groups;
+  a.C = sums;
+  a.A = (const char*)c.in;
+  a.lda = (int)(es * c.ld_in);
+  a.B = (const char*)c.w;
+  a.ldb = es * c.m;
+  a.K = c.m;
+  a.N = a.ldc = c.n;
+  a.splits = p.splits;
+  if (dtype == POETX_BF16) return go<FWD, Parts128>(a, st);
+  p.kernel == SINGLE_128 ? go<FWD, Single128>(a, st) : go<FWD, Single64>(a, st);
+}
+
 // ---- both operands in four bits ---------------------------------------------------------------------
 bool codes_supported(const poetx_grouped_desc* d, const void* Z, i64 ldz) {
   return d->groups <= Codes256::GROUPS && d->d_out % 8 == 0 && ldz % 8 == 0 && ldz * 512 < (1ll << 31) && aligned16(Z) && (i64)mx4::units(d->d_in) * 64 * 256 < (1ll << 31) &&

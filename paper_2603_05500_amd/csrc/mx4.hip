@@ -15,23 +15,6 @@ using edge::u32x4;
 
 constexpr int UPL = 2;      // units per sixteen lanes, their loads in flight together
 
-__device__ __forceinline__ void load8(const uint16_t* row, int c, int cols, float (&v)[8]) {
-  const u32x4 x = edge::load_branched(row, c, cols, true);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __builtin_bit_cast(float, x[i] << 16);
-    v[2 * i + 1] = __builtin_bit_cast(float, x[i] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void load8(const float* row, int c, int cols, float (&v)[8]) {
-  const u32x4 x = edge::load_branched(row, c, cols, true), y = edge::load_branched(row, c + 4, cols, true);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[i] = __builtin_bit_cast(float, (uint32_t)x[i]);
-    v[4 + i] = __builtin_bit_cast(float, (uint32_t)y[i]);
-  }
-}
-
 // Eight elements of a lane, sixteen lanes a unit -> the lane's codes and, in every lane, the unit's four scale bytes.
 __device__ __forceinline__ uint32_t quantise_unit(const float (&v)[8], int lane, uint32_t& word) {
   uint32_t top = 0;
@@ -70,7 +53,7 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const T* __restrict__
     const i64 u = first + 16 * p;
     const bool on = u >= u0 && u < u1;
     const i64 row = on ? u / upr : 0;
-    load8(X + row * ld, on ? (int)(u - row * upr) * mx4::UNIT + 8 * lane : cols, cols, v[p]);
+    edge::load8(X + row * ld, on ? (int)(u - row * upr) * mx4::UNIT + 8 * lane : cols, cols, v[p]);
   }
 #pragma unroll
   for (int p = 0; p < UPL; ++p) {
@@ -162,7 +145,7 @@ __global__ __launch_bounds__(256) void mx4_operands_kernel(OperandArgs a, int bl
       const i64 row = r0 + local + 16 * s + (tid >> 4);
 #pragma unroll
       for (int p = 0; p < UPL; ++p)
-        load8(a.X + (row < r1 ? row : 0) * a.ld, row < r1 && u0 + p < a.units ? (u0 + p) * mx4::UNIT + 8 * l16 : a.cols, a.cols, v[s][p]);
+        edge::load8(a.X + (row < r1 ? row : 0) * a.ld, row < r1 && u0 + p < a.units ? (u0 + p) * mx4::UNIT + 8 * l16 : a.cols, a.cols, v[s][p]);
     }
 #pragma unroll
     for (int s = 0; s < 4; ++s) {

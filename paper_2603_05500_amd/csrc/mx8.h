@@ -1,0 +1,64 @@
+// The 8-bit microscaled format on the device: where a buffer's parts lie, and its conversions.
+#pragma once
+
+#include "mx4.h"
+
+namespace poetx {
+namespace mx8 {
+
+using mx4::UNIT;
+using mx4::units;
+__host__ __device__ inline size_t scale_offset(i64 rows, int cols) { return align256((size_t)rows * units(cols) * UNIT); }
+inline size_t bytes(i64 rows, int cols) { return scale_offset(rows, cols) + (size_t)rows * units(cols) * 4; }
+struct View {
+  uint8_t* codes;
+  uint32_t* scales;      // a word per unit
+};
+__host__ __device__ inline View view(const void* Q, i64 rows, int cols) { return View{(uint8_t*)Q, (uint32_t*)((uint8_t*)Q + scale_offset(rows, cols))}; }
+
+// Scale byte of a block whose largest magnitude has these fp32 bits: its exponent field, which is 0 for what is below 2^-126 and 255 for infinities and NaN.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t amax_bits) { return amax_bits >> 23; }
+
+// x 2^(133 - scale) to the nearest whole number, ties to even, at most 127.  Values of 2^-133 have no reciprocal in fp32: the exponent is added, not multiplied.
+__device__ __forceinline__ int to_code(float x, uint32_t scale) {
+  return (int)__builtin_amdgcn_fmed3f(__builtin_rintf(__builtin_amdgcn_ldexpf(x, 133 - (int)scale)), -127.f, 127.f);
+}
+// Four of them, the first in the low byte.  All are 0 in a block that is not finite.
+__device__ __forceinline__ uint32_t to_codes4(float a, float b, float c, float d, uint32_t scale) {
+  const uint32_t w = (to_code(a, scale) & 255) | (to_code(b, scale) & 255) << 8 | (to_code(c, scale) & 255) << 16 | (uint32_t)to_code(d, scale) << 24;
+  return scale == 255 ? 0 : w;
+}
+// code E of four
+template <int E>
+__device__ __forceinline__ float value(uint32_t codes, uint32_t scale) {
+  const float v = __builtin_amdgcn_ldexpf((float)((int)(codes << (24 - 8 * E)) >> 24), (int)scale - 133);
+  return scale == 255 ? __builtin_nanf("") : v;
+}
+__device__ __forceinline__ void values8(uint32_t lo, uint32_t hi, uint32_t scale, float (&v)[8]) {
+  v[0] = value<0>(lo, scale), v[1] = value<1>(lo, scale), v[2] = value<2>(lo, scale), v[3] = value<3>(lo, scale);
+  v[4] = value<0>(hi, scale), v[5] = value<1>(hi, scale), v[6] = value<2>(hi, scale), v[7] = value<3>(hi, scale);
+}
+
+// Eight elements of a lane, sixteen lanes a unit -> the lane's codes and, in every lane, the unit's four scale bytes.
+__device__ __forceinline__ void quantise_unit(const float (&v)[8], int lane16, uint32_t (&codes)[2], uint32_t& word) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t a = __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu;
+    top = a > top ? a : top;
+  }
+#pragma unroll
+  for (int s = 1; s < 4; s *= 2) {
+    const uint32_t o = __shfl_xor(top, s);
+    top = o > top ? o : top;
+  }
+  const uint32_t sb = scale_byte(top);
+  codes[0] = to_codes4(v[0], v[1], v[2], v[3], sb);
+  codes[1] = to_codes4(v[4], v[5], v[6], v[7], sb);
+  word = sb << (8 * (lane16 >> 2));
+  word |= __shfl_xor(word, 4);
+  word |= __shfl_xor(word, 8);
+}
+
+}  // namespace mx8
+}  // namespace poetx

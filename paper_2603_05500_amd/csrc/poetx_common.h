@@ -79,7 +79,7 @@ __host__ __device__ constexpr bool tile_inside(int start, int width, int extent)
 static_assert(!tile_inside(0x7fffff80, 128, 0x7ffffffb) && tile_inside(0x7fffff00, 128, 0x7ffffffb) && tile_inside(0, 128, 128) && !tile_inside(0, 128, 127),
               "the last tile of 2^31 - 5 columns is no whole one");
 
-inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+__host__ __device__ inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Convert the status of the launches enqueued so far into a poetx_status.
 inline int launch_status() { return hipGetLastError() == hipSuccess ? POETX_OK : POETX_ERR_HIP; }

@@ -182,6 +182,11 @@ void mx4_dequantize_launch(const void* Q, i64 rows, int cols, int dtype, void* o
 // the bf16 values [groups][n][cols] of the groups that have rows
 void mx4_dequantize_groups_launch(const void* Q, int groups, int n, int cols, const int32_t* offsets, i64 rows, void* out, hipStream_t st);
 
+// ---- 8-bit buffers (mx8.hip; layout: mx8.h) -----------------------------------------------------
+void mx8_quantize_launch(int dtype, const void* X, i64 rows, int cols, i64 ld, void* Q, hipStream_t st);
+// offsets: only the rows that one of `groups` groups has
+void mx8_dequantize_launch(const void* Q, i64 rows, int cols, int dtype, void* out, i64 ld, hipStream_t st, const int32_t* offsets = nullptr, int groups = 0);
+
 // ---- rows in the order of their groups (group_order.hip) ---------------------------------------
 size_t group_order_workspace_bytes(i64 n, int groups);
 void group_order_launch(const int32_t* ids, i64 n, int groups, int32_t* offsets, int32_t* order, void* ws, hipStream_t st);
