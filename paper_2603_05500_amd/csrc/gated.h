@@ -61,6 +61,9 @@ struct In {
   i64 ld;
   int splits;         // SUMS
 };
+// whole 16-byte vectors (gated_stream.hip); k: of plan() for a forward of 2n columns
+bool stream_supported(int dtype, const Call& c);
+void stream_launch(int dtype, grouped::Kernel k, const Call& c, hipStream_t st);
 // the rows that some group has, one pass over G and U (gated_rows.hip)
 void rows_launch(int dtype, Source src, const In& in, const int32_t* offsets, int groups, i64 rows, int n, Mode mode, const Out& out, hipStream_t st);
 

@@ -69,6 +69,8 @@ void products(const poetx_gated_desc* d, const void* X, i64 ldx, const void* W, 
   grouped::Call c = product_of(d, X, ldx, W, offsets);
   c.out = (char*)ws + operand_bytes(d);
   const grouped::Plan p = plan_of(d, c);
+  const gated::Call q{X, W, ldx, offsets, d->rows, d->d_in, d->d_hidden, d->groups, mode, out};
+  if (p.kernel >= grouped::STREAM_256 && p.splits == 1 && gated::stream_supported(d->dtype, q)) return gated::stream_launch(d->dtype, p.kernel, q, st);
   if (p.kernel >= grouped::STREAM_256) grouped::stream_sums(d->dtype, p, c, c.out, st);
   else grouped::edge_sums(d->dtype, p.kernel, c, st);
   gated::rows_launch(d->dtype, gated::SUMS, gated::In{c.out, nullptr, 0, p.splits}, offsets, d->groups, d->rows, d->d_hidden, mode, out, st);

@@ -1,0 +1,70 @@
+// The gated block on the streaming kernel: both projections, the activation and the product in one launch, and the backward pass that makes G and U again.
+#include "grouped_stream.h"
+
+namespace poetx {
+namespace gated {
+namespace {
+
+using grouped::BF16;
+using grouped::F32;
+using grouped::StreamArgs;
+using grouped::StreamTile;
+
+constexpr int kCUs = 256;
+
+template <class C>
+void go(const StreamArgs& a0, hipStream_t st) {
+  auto kern = grouped::grouped_stream_kernel<grouped::FWD, C>;
+  static const bool configured = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS_BYTES) == hipSuccess;
+  (void)configured;
+  StreamArgs a = a0;
+  const int cols = C::GATED == HOLD_MX8 ? mx8::units(a.N) * mx8::UNIT : a.N;      // codes past the last column are zeros
+  a.tiles_n = ceil_div(cols, C::BN / 2);
+  hipLaunchKernelGGL(kern, dim3(kCUs * C::PER_CU), dim3(256), C::LDS_BYTES, st, a);
+}
+
+template <Mode MODE>
+void pick(grouped::Kernel k, const StreamArgs& a, hipStream_t st) {
+  if (k == grouped::SINGLE_128) go<StreamTile<128, 128, 4, F32, 2, false, MODE>>(a, st);
+  else if (k == grouped::SINGLE_64) {
+    if constexpr (MODE == HOLD_MX8) go<StreamTile<128, 128, 4, F32, 2, false, MODE>>(a, st);      // a wave's columns have to be whole blocks
+    else go<StreamTile<64, 64, 8, F32, 2, false, MODE>>(a, st);
+  } else if (k == grouped::STREAM_256) go<StreamTile<256, 256, 4, BF16, 1, false, MODE>>(a, st);
+  else if (k == grouped::STREAM_256x128) go<StreamTile<256, 128, 6, BF16, 1, false, MODE>>(a, st);
+  else go<StreamTile<128, 128, 8, BF16, 1, false, MODE>>(a, st);
+}
+
+}  // namespace
+
+bool stream_supported(int dtype, const Call& c) {
+  const int es = dtype == POETX_F32 ? 4 : 2, v = 16 / es;
+  const i64 wide = (1ll << 31) / (es * 256);      // a tile's rows span less than 2^31 bytes, and so do a group's weights
+  auto fits = [&](const void* p, i64 ld) { return ((uintptr_t)p & 15) == 0 && ld % v == 0 && ld < wide; };
+  const bool hold = c.mode == HOLD || c.mode == BWD;
+  return c.groups <= 256 && c.m % v == 0 && c.n % v == 0 && fits(c.X, c.ldx) && ((uintptr_t)c.W & 15) == 0 && (2 * (i64)c.n + 256) * c.m * es < (1ll << 31) &&
+         (!c.out.H || fits(c.out.H, c.out.ldh)) && (!hold || (fits(c.out.G, c.out.ldgu) && fits(c.out.U, c.out.ldgu))) && (c.mode != BWD || fits(c.out.dH, c.out.lddh)) &&
+         (c.mode != HOLD_MX8 || c.n < wide);
+}
+
+void stream_launch(int dtype, grouped::Kernel k, const Call& c, hipStream_t st) {
+  const int es = dtype == POETX_F32 ? 4 : 2;
+  StreamArgs a = {};
+  a.A = (const char*)c.X;
+  a.lda = (int)(es * c.ldx);
+  a.B = (const char*)c.W;
+  a.ldb = es * c.m;
+  a.K = c.m;
+  a.N = c.n;
+  a.offsets = c.offsets;
+  a.rows = (int)c.rows;
+  a.groups = c.groups;
+  a.splits = 1;
+  a.block = c.out;
+  if (c.mode == FWD) pick<FWD>(k, a, st);
+  else if (c.mode == HOLD) pick<HOLD>(k, a, st);
+  else if (c.mode == HOLD_MX8) pick<HOLD_MX8>(k, a, st);
+  else pick<BWD>(k, a, st);
+}
+
+}  // namespace gated
+}  // namespace poetx

@@ -21,9 +21,8 @@
 #pragma once
 #include <utility>
 
-#include "grouped.h"
+#include "gated.h"
 #include "mfma_dense_kernel.h"
-#include "mx4.h"
 
 namespace poetx {
 namespace grouped {
@@ -35,18 +34,21 @@ using mx4::u32x4;
 enum Elem { BF16, F32, CODES };
 
 // PARTS: fp32 sums of a range of the contraction go to `parts`, to be added up by another launch (bf16; fp32 needs no kernel of its own).
-template <int BM_, int BN_, int NS_, Elem ELEM_, int PER_CU_ = 1, bool PARTS_ = false>
+// GATED: a gated block's forward or the recomputing half of its backward pass, as gated::Mode says; NOT_GATED otherwise.
+constexpr int NOT_GATED = -1;
+template <int BM_, int BN_, int NS_, Elem ELEM_, int PER_CU_ = 1, bool PARTS_ = false, int GATED_ = NOT_GATED>
 struct StreamTile {
   static constexpr int BM = BM_, BN = BN_, NS = NS_, NW = 4, PER_CU = PER_CU_;
   static constexpr Elem ELEM = ELEM_;
   static constexpr bool PARTS = PARTS_;
+  static constexpr int GATED = GATED_;
   static constexpr bool FP4 = ELEM == CODES;
   static constexpr int DEPTH = FP4 ? 128 : ELEM == F32 ? 16 : 32;      // elements of a stage
   static constexpr int SETS = 4, GROUPS = 64 * SETS;      // groups per lane, in all
   static constexpr int A_BYTES = BM * 64, B_BYTES = BN * 64, S_BYTES = FP4 ? (BM + BN) * 4 : 0, STAGE_BYTES = A_BYTES + B_BYTES + S_BYTES;
   static constexpr int TM = BM / 32, TN = BN / 32, MF = TM * TN * (ELEM == F32 ? 4 : 1);      // MFMAs of a stage; fp32: 4 of depth per MFMA
   static constexpr int RS = MF / (TM + TN) < 3 ? MF / (TM + TN) : 3;
-  static constexpr int OUT_BYTES = ELEM == F32 || PARTS ? 0 : TN / 4 * 2048;
+  static constexpr int OUT_BYTES = ELEM == F32 || PARTS ? 0 : GATED == NOT_GATED ? TN / 4 * 2048 : TN * 256 * (GATED == gated::HOLD || GATED == gated::BWD ? 3 : 1);
   static constexpr int LDS_BYTES = NS * STAGE_BYTES + NW * OUT_BYTES;
   static constexpr int IPWA = A_BYTES / 1024 / NW, IPWB = B_BYTES / 1024 / NW, IPWS = FP4 ? (BM + BN) / 256 : 0;
   static constexpr int LPT = IPWA + IPWB + IPWS;
@@ -70,6 +72,7 @@ struct StreamArgs {
   int tiles_n;            // column tiles
   int accumulate;
   int splits;             // FWD, INPUT: ranges of the contraction, whose sums go to [split][rows][N] at C; 1: the result does
+  gated::Out block;       // GATED: what is made of a tile; N: d_hidden, tiles_n: of so many columns (HOLD_MX8: rounded up to whole units)
 };
 
 // 16 (4) bytes per lane from base + voff straight into LDS at lds + 16 (4) * lane; zeros from the descriptor's end on.  Between M0's write and its use there has to be
@@ -125,14 +128,198 @@ __device__ __forceinline__ void mfma_fp4(floatx4& c, const u32x4& a, const u32x4
 // c += a b on 16 x 16 x 4 fp32
 __device__ __forceinline__ void mfma_fp32(floatx4& c, uint32_t a, uint32_t b) { asm volatile("v_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b)); }
 
+// ---- what a gated block makes of a wave's piece of a tile, rows r0 on of a group that ends with r1, columns j0 on --------------
+// Register a, c of a lane: row 16 a + (lane & 15), columns 4 (lane >> 4) .. + 3 of piece c / 2, of G where c is even and of U where it is odd.
+template <class C>
+__device__ __forceinline__ void gated_tile(const StreamArgs& g, floatx4 (&acc)[C::TM][C::TN], int r0, int r1, int j0, int wave, int lane, char* stg) {
+  constexpr gated::Mode MODE = (gated::Mode)C::GATED;
+  constexpr bool FP32 = C::ELEM == F32, PAIR = MODE == gated::HOLD || MODE == gated::BWD;      // PAIR: G and U, or dG and dU, as matrices
+  constexpr int P = C::TN / 2, ES = FP32 ? 4 : 2, AT_ONCE = P < 2 ? P : 2;      // pieces of 16 columns
+  const gated::Out& o = g.block;
+  asm volatile("" : "+v"(lane));      // what follows from it is worked out anew for each tile: kept from tile to tile it took registers that the products need
+  const int li = lane & 15, q4 = lane >> 4, top = (wave >> 1) * (C::BM / 2), left = (wave & 1) * (C::BN / 4);      // the wave's piece in the tile
+  const int row0 = r0 + top, rows = r1 - row0, cols = g.N - j0 - left;      // of the piece; either may be none
+  // Descriptors that move down 16 rows at a time, so that a lane's offsets are the same for every a.
+  struct Matrix {
+    uint64_t at;
+    i64 left, step;
+    __device__ __forceinline__ Matrix(const void* p, i64 before, i64 bytes, i64 down) : at((uint64_t)p + before), left(bytes), step(down) {}
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t here() const { return make_rsrc((void*)at, left); }
+    __device__ __forceinline__ void next() {
+      at += step, left -= step;
+      asm volatile("" : "+s"(at), "+s"(left));
+    }
+  };
+  auto matrix = [&](const void* p, i64 ld) __attribute__((always_inline)) {
+    return Matrix(p, ((i64)row0 * ld + j0 + left) * ES, ((i64)(rows - 1) * ld + cols) * ES, 16 * ld * ES);
+  };
+  Matrix mh = matrix(o.H, o.ldh), mg = matrix(o.G, o.ldgu), mu = matrix(o.U, o.ldgu), md = matrix(o.dH, o.lddh);
+  const bool with_h = MODE != gated::BWD || o.H;
+  // HOLD_MX8: rows of codes and scales
+  const int units = mx8::units(g.N), pitch = units * mx8::UNIT;
+  const mx8::View vg = mx8::view(o.G, g.rows, g.N), vu = mx8::view(o.U, g.rows, g.N);
+  auto codes = [&](const void* p) __attribute__((always_inline)) { return Matrix(p, (i64)row0 * pitch + j0 + left, (i64)rows * pitch - j0 - left, 16 * pitch); };
+  auto scales = [&](const void* p) __attribute__((always_inline)) { return Matrix(p, (i64)row0 * units * 4 + (j0 + left) / 32, (i64)rows * units * 4 - (j0 + left) / 32, 64 * units); };
+  Matrix cg = codes(vg.codes), cu = codes(vu.codes), sg = scales(vg.scales), su = scales(vu.scales);
+
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  typedef std::conditional_t<FP32, u32x4, u32x2> Four;
+  Four dh[2][MODE == gated::BWD ? P : 1];
+  auto fetch = [&](int a) __attribute__((always_inline)) {      // dH of 16 rows, ahead of their turn
+    const auto rd = md.here();
+    md.next();
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int col = 16 * p + 4 * q4, v = col < cols ? (li * (int)o.lddh + col) * ES : kNowhere;
+      if constexpr (FP32) dh[a & 1][p] = __builtin_amdgcn_raw_buffer_load_b128(rd, v, 0, 0);
+      else dh[a & 1][p] = __builtin_amdgcn_raw_buffer_load_b64(rd, v, 0, 0);
+    }
+  };
+  // bf16: 16 rows of a matrix at a time through LDS, an area each, so that every instruction writes whole lines (P = 4) or halves of them
+  constexpr int AREA = 32 * 16 * P, CHUNKS = 2 * P;      // bytes; 16-byte chunks of a row
+  auto place = [](int r, int ch) __attribute__((always_inline)) { return r * (16 * CHUNKS) + 16 * (ch ^ (P == 4 ? (r >> 1) & 7 : (r >> 2) & 3)); };
+  auto put = [&](int k, int p, const float (&z)[AT_ONCE][4], const Matrix& m, i64 ld) __attribute__((always_inline)) {
+    if constexpr (FP32) {
+      const auto r = m.here();
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) {
+        const int col = 16 * (p + i) + 4 * q4;
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, floatx4{z[i][0], z[i][1], z[i][2], z[i][3]}), r, col < cols ? (li * (int)ld + col) * 4 : kNowhere, 0, 0);
+      }
+    } else {
+      uint32_t w[4];
+      dense::pack_pair(floatx4{z[0][0], z[0][1], z[0][2], z[0][3]}, floatx4{z[1][0], z[1][1], z[1][2], z[1][3]}, w);
+      *reinterpret_cast<u32x4*>(stg + k * AREA + place(li, (p + (q4 & 1)) * 2 + (q4 >> 1))) = u32x4{w[0], w[1], w[2], w[3]};
+    }
+  };
+  auto get = [&](int k, const Matrix& m, i64 ld) __attribute__((always_inline)) {
+    if constexpr (!FP32) {
+      const auto rsrc = m.here();
+#pragma unroll
+      for (int i = 0; i < P / 2; ++i) {
+        const int r = lane / CHUNKS + (64 / CHUNKS) * i, ch = lane % CHUNKS, col = 8 * ch;
+        const u32x4 w = *reinterpret_cast<const u32x4*>(stg + k * AREA + place(r, ch));
+        __builtin_amdgcn_raw_buffer_store_b128(w, rsrc, col < cols ? (r * (int)ld + col) * 2 : kNowhere, 0, 0);
+      }
+    }
+  };
+  // codes and the scale of a block of 32 columns (two pieces) of each row; columns past the last are no part of it and have codes of zero
+  auto quantise = [&](const float (&z)[AT_ONCE][4], int p, uint32_t& d0, uint32_t& d1, uint32_t& sb) __attribute__((always_inline)) {
+    const bool in0 = 16 * p + 4 * q4 < cols, in1 = 16 * p + 16 + 4 * q4 < cols;
+    uint32_t m = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t s0 = in0 ? __builtin_bit_cast(uint32_t, z[0][e]) & 0x7fffffffu : 0, s1 = in1 ? __builtin_bit_cast(uint32_t, z[AT_ONCE - 1][e]) & 0x7fffffffu : 0;
+      m = s0 > m ? s0 : m;
+      m = s1 > m ? s1 : m;
+    }
+    const auto t = __builtin_amdgcn_permlane16_swap(m, m, false, false);      // over the four groups of 16 lanes
+    m = t[0] > t[1] ? t[0] : t[1];
+    const auto f = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+    m = f[0] > f[1] ? f[0] : f[1];
+    sb = mx8::scale_byte(m);
+    d0 = in0 ? mx8::to_codes4(z[0][0], z[0][1], z[0][2], z[0][3], sb) : 0;
+    d1 = in1 ? mx8::to_codes4(z[AT_ONCE - 1][0], z[AT_ONCE - 1][1], z[AT_ONCE - 1][2], z[AT_ONCE - 1][3], sb) : 0;
+  };
+  // A group of 16 lanes gives its four columns of every piece for all columns of one (P = 4; P = 2: half of one).
+  auto store_codes = [&](const uint32_t (&d)[P], const uint32_t (&sb)[(P + 1) / 2], Matrix& mc, Matrix& ms) __attribute__((always_inline)) {
+    const auto rc = mc.here(), rs = ms.here();
+    if constexpr (P >= 2) {
+      const auto t0 = __builtin_amdgcn_permlane16_swap(d[0], d[1], false, false);
+      if constexpr (P == 4) {
+        const auto t1 = __builtin_amdgcn_permlane16_swap(d[2], d[3], false, false);
+        const auto e = __builtin_amdgcn_permlane32_swap(t0[0], t1[0], false, false), f = __builtin_amdgcn_permlane32_swap(t0[1], t1[1], false, false);
+        __builtin_amdgcn_raw_buffer_store_b128(u32x4{e[0], f[0], e[1], f[1]}, rc, li * pitch + 16 * q4, 0, 0);
+      } else {
+        __builtin_amdgcn_raw_buffer_store_b64(u32x2{t0[0], t0[1]}, rc, li * pitch + 16 * (q4 & 1) + 8 * (q4 >> 1), 0, 0);
+      }
+      const int where = q4 == 0 ? li * units * 4 : kNowhere;
+      if constexpr (P == 4) __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(sb[0] | sb[1] << 8), rs, where, 0, 0);
+      else __builtin_amdgcn_raw_buffer_store_b8((uint8_t)sb[0], rs, where, 0, 0);
+    }
+    mc.next(), ms.next();
+  };
+
+  if constexpr (MODE == gated::BWD) fetch(0);
+#pragma unroll
+  for (int a = 0; a < C::TM; ++a) {
+    if constexpr (MODE == gated::BWD) {
+      if (a + 1 < C::TM) fetch(a + 1);
+    }
+    uint32_t dg[P], du[P], bg[(P + 1) / 2], bu[(P + 1) / 2];
+#pragma unroll
+    for (int p = 0; p < P; p += AT_ONCE) {
+      float x[AT_ONCE][4], y[AT_ONCE][4], h[AT_ONCE][4];
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) {
+        floatx4 &ag = acc[a][2 * (p + i)], &au = acc[a][2 * (p + i) + 1];
+        asm volatile("" : "+a"(ag), "+a"(au));      // read here and no sooner: the compiler copied accumulators ahead of their turn, and up to 180 registers of a lane through memory
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[i][e] = ag[e], y[i][e] = au[e];
+        ag = au = floatx4{0.f, 0.f, 0.f, 0.f};
+      }
+      if constexpr (MODE == gated::HOLD) {
+        put(1, p, x, mg, o.ldgu);
+        put(2, p, y, mu, o.ldgu);
+      }
+      if constexpr (MODE == gated::HOLD_MX8) {
+        static_assert(MODE != gated::HOLD_MX8 || P % 2 == 0, "whole blocks of 32");
+        quantise(x, p, dg[p], dg[p + 1], bg[p / 2]);
+        quantise(y, p, du[p], du[p + 1], bu[p / 2]);
+      }
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (MODE == gated::BWD) {
+            float d, v, s;
+            if constexpr (FP32) d = __builtin_bit_cast(float, (uint32_t)dh[a & 1][p + i][e]);
+            else d = __builtin_bit_cast(float, e & 1 ? dh[a & 1][p + i][e >> 1] & 0xffff0000u : dh[a & 1][p + i][e >> 1] << 16);
+            gated::act_both(o.act, x[i][e], v, s);
+            h[i][e] = v * y[i][e];
+            x[i][e] = d * y[i][e] * s;
+            y[i][e] = d * v;
+          } else {
+            h[i][e] = gated::act_value(o.act, x[i][e]) * y[i][e];
+          }
+        }
+      if constexpr (MODE == gated::BWD) {
+        put(1, p, x, mg, o.ldgu);
+        put(2, p, y, mu, o.ldgu);
+      }
+      if (with_h) put(0, p, h, mh, o.ldh);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (!FP32) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // this wave's own writes; the areas are private to it
+      if (with_h) get(0, mh, o.ldh);
+      if constexpr (PAIR) {
+        get(1, mg, o.ldgu);
+        get(2, mu, o.ldgu);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // read back before the areas are rewritten
+    }
+    mh.next();
+    if constexpr (PAIR) mg.next(), mu.next();
+    if constexpr (MODE == gated::HOLD_MX8) {
+      store_codes(dg, bg, cg, sg);
+      store_codes(du, bu, cu, su);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
 // f(0), f(1), .. as constants
 template <int... I, class F>
 __device__ __forceinline__ void in_turn(std::integer_sequence<int, I...>, const F& f) {
   (f(std::integral_constant<int, I>{}), ...);
 }
 
+// GATED: columns of B come in pieces of 16, gate and up in turn, the tile's columns of H being half as many: a lane then holds G and U of the same four elements of a row.
 template <Dir DIR, class C>
 __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
+  constexpr bool GATED = C::GATED != NOT_GATED;
+  static_assert(!GATED || (DIR == FWD && C::ELEM != CODES), "a gated block's products");
   constexpr bool FP4 = C::FP4, FP32 = C::ELEM == F32, A_K = DIR != WEIGHT, B_K = DIR == FWD;
   // WIDE: rows come 64 deep, whole 128-byte lines.  Two stages are a unit, which arrives in two halves of its rows, one per stage; as it is needed as a whole, and its
   // place is free, with its first stage, the last half is in flight a stage less, and the ring has to be deep.  As in the dense product, 64-byte pieces would ask for every line twice.
@@ -140,6 +327,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   constexpr int DEPTH = C::DEPTH, ES = FP32 ? 4 : 2;      // bytes of an element (not of a code)
   static_assert(!FP4 || DIR == FWD, "codes are contracted along their rows");
   constexpr int BM = C::BM, BN = C::BN, NS = C::NS, STAGE_BYTES = C::STAGE_BYTES, A_BYTES = C::A_BYTES;
+  constexpr int BW = GATED ? BN / 2 : BN;      // rows of a weight, columns of the result
   constexpr int IPWA = C::IPWA, IPWB = C::IPWB, IPWS = C::IPWS, LPT = C::LPT, TM = C::TM, TN = C::TN, MF = C::MF, RS = C::RS, DS = C::DS;
   constexpr int GROUP = dense::GROUP;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -212,7 +400,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
     const int first_m = (u / per_group) * GROUP;
     const int gsz = (tiles_m - first_m) < GROUP ? (tiles_m - first_m) : GROUP;
     const int rt = first_m + (u % per_group) % gsz;
-    w.j0 = ((u % per_group) / gsz) * BN;
+    w.j0 = ((u % per_group) / gsz) * BW;
     w.i0 = rt * BM;
     w.first = w.r0 = w.r1 = 0;
     if (DIR == WEIGHT) {
@@ -251,14 +439,15 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   uint32_t voffA[IPWA], voffB[FP4 ? 1 : IPWB], voffS[IPWS ? IPWS : 1];      // FP4: both operands' rows are as long, and the tile square
   // Rows along the output: where chunk c of row k lies.  bf16: as the transposing loads like it; fp32: a fragment's four rows 4 q + e, q = 0 .. 3, in four different 64 bytes.
   auto strided_chunk = [&](int c, int k) __attribute__((always_inline)) { return FP32 ? c ^ (4 * ((k >> 2) & 3)) : dense::kx16_chunk(c, k); };
-  auto slot_offset = [&](int slot, bool kmajor, int width, int ld) __attribute__((always_inline)) {
+  auto paired = [&](int r) __attribute__((always_inline)) { return (r >> 5) * 16 + (r & 15) + (r & 16 ? g.N : 0); };      // GATED: the weight's row that is row r of the tile
+  auto slot_offset = [&](int slot, bool kmajor, int width, int ld, bool pairs = false) __attribute__((always_inline)) {
     if (WIDE) {
       const int r = slot >> 3, c = (slot & 7) ^ ((r >> 1) & 7);
-      return (uint32_t)(r * ld + c * 16);
+      return (uint32_t)((pairs ? paired(r) : r) * ld + c * 16);
     }
     if (kmajor) {
       const int r = slot >> 2, c = dense::xk16_chunk(slot & 3, r);
-      return (uint32_t)(r * ld + c * 16);
+      return (uint32_t)((pairs ? paired(r) : r) * ld + c * 16);
     }
     const int k = slot / (width * ES / 16), c = strided_chunk(slot % (width * ES / 16), k);
     return (uint32_t)(k * ld + c * 16);
@@ -266,7 +455,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
 #pragma unroll
   for (int s = 0; s < IPWA; ++s) voffA[s] = slot_offset((wave * IPWA + s) * 64 + lane, A_K, BM, g.lda);
 #pragma unroll
-  for (int s = 0; s < (FP4 ? 0 : IPWB); ++s) voffB[s] = slot_offset((wave * IPWB + s) * 64 + lane, B_K, BN, g.ldb);
+  for (int s = 0; s < (FP4 ? 0 : IPWB); ++s) voffB[s] = slot_offset((wave * IPWB + s) * 64 + lane, B_K, BN, g.ldb, GATED);
   // scales: the first two waves bring A's, the others B's
   const bool scales_a = wave < 2;
 #pragma unroll
@@ -294,7 +483,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   int iti = -1, ikt = 0, iKT = 0, islot = 0;
   const LeftA stepA = A_K ? 64 : DEPTH * (LeftA)g.lda;
   const LeftB stepB = B_K ? 64 : DEPTH * (LeftB)g.ldb;
-  const int halfA = WIDE ? BM / 2 * g.lda : 0, halfB = WIDE ? BN / 2 * g.ldb : 0;
+  const int halfA = WIDE ? BM / 2 * g.lda : 0, halfB = WIDE ? BW / 2 * g.ldb : 0;
   auto next_tile = [&]() __attribute__((always_inline)) {
     Where w;
     do {
@@ -309,7 +498,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
     if (iti < n_my) {
       k0 = w.k0;
       k1 = w.k1;
-      if (DIR == FWD) hb = g.N - w.j0 < BN ? g.N - w.j0 : BN;      // rows of W in the tile
+      if (DIR == FWD) hb = g.N - w.j0 < BW ? g.N - w.j0 : BW;      // rows of W in the tile (GATED: of up, and of gate some lines above; none at all leaves those of up before them)
       if (DIR == WEIGHT) {
         const i64 len = w.r1 - w.r0;
         na.at = (uint64_t)(g.A + (i64)w.r0 * g.lda + ES * w.i0);
@@ -322,9 +511,9 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
         na.at = (uint64_t)(g.A + (i64)w.r0 * g.lda);
         na.left = (ha - 1) * (LeftA)g.lda + row;
         if (DIR == FWD) {
-          const i64 first = (i64)w.gr * g.N + w.j0;
+          const i64 first = (i64)w.gr * (GATED ? 2 * g.N : g.N) + w.j0;
           nb.at = (uint64_t)(g.B + first * g.ldb);
-          nb.left = (hb - 1) * (LeftB)g.ldb + row;
+          nb.left = ((GATED ? g.N : 0) + hb - 1) * (LeftB)g.ldb + row;
           nsa = (uint64_t)(g.SA + mx4::position(w.first, w.gr) + (w.r0 - w.first));      // a word per row
           nsb = (uint64_t)(g.SB + (i64)w.gr * ((g.N + 63) / 64 * 64) + w.j0);
         } else {
@@ -528,7 +717,9 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
       }
       const Where w = locate(ti);
       // Stores go through a descriptor as well: rows past the group's end (of dW) lie behind it, and a lane whose columns do not exist gets an offset that does.
-      if constexpr (DIR == WEIGHT || FP32 || C::PARTS) {
+      if constexpr (GATED) {
+        gated_tile<C>(g, acc, w.r0, w.r1, w.j0, wave, lane, lds + NS * STAGE_BYTES + wave * C::OUT_BYTES);
+      } else if constexpr (DIR == WEIGHT || FP32 || C::PARTS) {
         // a lane's four columns of a row
         const int row = wm * (BM / 2) + li, col = wn * (BN / 2) + 4 * q4, rows = DIR == WEIGHT ? g.M - w.i0 : w.r1 - w.r0, cols = g.N - w.j0;
         const i64 first = DIR == WEIGHT ? ((i64)w.gr * g.M + w.i0) * g.ldc : ((i64)w.split * g.rows + w.r0) * g.ldc;
