@@ -35,7 +35,7 @@ struct Op {
   int rows, cols;        // valid extents
   int rows_side;         // != 0: rows (cols) also end at the side of the batch's block
   int cols_side;
-  i64 cs;                // strided operands (template flag): distance of neighbouring columns, rows then being ld apart as ever
+  i64 cs;                // strided operands (template flag): distance of neighbouring columns, rows then being ld apart as ever; paired ones: of an odd row from the even one before it
 };
 
 struct Args {
@@ -207,7 +207,8 @@ struct Shape {
 // 32s with 1 - 7 tokens 25 % less time, fp32 ones 7 %).  A choice between WHOLE and BRANCHED inside one kernel costs the short launches that are
 // not whole up to 5 % (the code), so it is made outside; us, BRANCHED / WHOLE: gradients of 1024 features, b = 64, 512 tokens 4.28 / 3.77; bf16 1024 x 1024 x 512 8.4 / 7.5 and,
 // backward, 9.2 / 7.8; fp32 256 x 256 x 512 6.4 / 6.0.
-enum Load { BRANCHED, STRIDED, MASKED, WHOLE };
+// PAIRED: branched; B (K major) has rows of two matrices in turn, rows 2 i and 2 i + 1 being cs apart and pairs ld.
+enum Load { BRANCHED, STRIDED, MASKED, WHOLE, PAIRED };
 
 // Epi: __device__ void operator()(int batch, int split, int row, int col, const float (&v)[8]) -- eight
 // consecutive columns of one output row, indices inside the batch; it does its own masking.
@@ -259,6 +260,14 @@ __device__ __forceinline__ void edge_product(const Args& g, const Epi& epi, int 
     const int rr = LOAD == WHOLE || r < s.rows ? r : 0;
     return (s.pm ? (i64)s.pm[rr] : (i64)rr) * s.ld;
   };
+  auto row_at_b = [&](int r) {
+    if constexpr (LOAD == PAIRED) {
+      const int rr = r < sb.rows ? r : 0;
+      return (i64)(rr >> 1) * sb.ld + (rr & 1) * g.B.cs;
+    } else {
+      return row_at(sb, r);
+    }
+  };
   auto rowno_a = [&](int s, int kt) { return (A_K ? i0 : kt * BK) + (s * NTH + tid) / VPRA; };
   auto rowno_b = [&](int s, int kt) { return (B_K ? j0 : kt * BK) + (s * NTH + tid) / VPRB; };
   auto col_a = [&](int s, int kt) { return (A_K ? kt * BK : i0) + ((s * NTH + tid) % VPRA) * V; };
@@ -270,7 +279,7 @@ __device__ __forceinline__ void edge_product(const Args& g, const Epi& epi, int 
     }
     if (!B_K || first) {
 #pragma unroll
-      for (int s = 0; s < NVB; ++s) rowB[s] = row_at(sb, rowno_b(s, kt));
+      for (int s = 0; s < NVB; ++s) rowB[s] = row_at_b(rowno_b(s, kt));
     }
   };
   const int whole_b = tile_inside(j0, BN, sb.cols) ? sb.rows / BK : 0;   // MASKED: stages up to here are whole and need no mask

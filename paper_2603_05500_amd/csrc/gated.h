@@ -61,9 +61,12 @@ struct In {
   i64 ld;
   int splits;         // SUMS
 };
+// a handful of rows per group, where grouped::few_supported() says so for 2n columns (grouped_few.hip): any sizes, strides and alignments; four: W is a 4-bit buffer
+void few_launch(int dtype, bool four, const Call& c, hipStream_t st);
 // whole 16-byte vectors (gated_stream.hip); k: of plan() for a forward of 2n columns
 bool stream_supported(int dtype, const Call& c);
 void stream_launch(int dtype, grouped::Kernel k, const Call& c, hipStream_t st);
+void edge_launch(int dtype, grouped::Kernel k, const Call& c, hipStream_t st);      // any shape (gated_edge.hip)
 // the rows that some group has, one pass over G and U (gated_rows.hip)
 void rows_launch(int dtype, Source src, const In& in, const int32_t* offsets, int groups, i64 rows, int n, Mode mode, const Out& out, hipStream_t st);
 

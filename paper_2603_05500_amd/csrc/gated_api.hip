@@ -46,34 +46,43 @@ bool ld_fits(i64 rows, i64 ld) { return rows == 0 || ld < kMostElements / rows; 
 // What the 4-bit weight's values take of the workspace; sums of the products follow.
 size_t operand_bytes(const poetx_gated_desc* d) { return d->flags & POETX_GATED_W_MX4 ? align256((size_t)d->groups * 2 * d->d_hidden * d->d_in * 2) : 0; }
 
+// G | U as one product of 2n columns: what the choice of kernels goes by
 grouped::Call product_of(const poetx_gated_desc* d, const void* X, i64 ldx, const void* W, const int32_t* offsets) {
   return grouped::Call{X, nullptr, W, nullptr, ldx, 0, 2 * (i64)d->d_hidden, offsets, d->rows, d->d_in, 2 * d->d_hidden, d->groups, 0};
 }
-grouped::Plan plan_of(const poetx_gated_desc* d, const grouped::Call& c) {
-  const grouped::Plan p = grouped::plan(d->dtype, grouped::FWD, c, grouped::stream_supported(d->dtype, grouped::FWD, c), ~(size_t)0);
-  return p;
+bool few(const poetx_gated_desc* d) {
+  return grouped::few_supported(d->dtype, grouped::FWD, d->rows, d->d_in, 2 * d->d_hidden, d->groups, d->flags & POETX_GATED_W_MX4 ? grouped::VALUES_MX4 : grouped::DENSE_WEIGHT);
 }
+// fp32 sums of contractions that are split among workgroups, where the tensors allow the streaming kernels
 size_t sums_bytes(const poetx_gated_desc* d) {
-  const grouped::Plan p = plan_of(d, product_of(d, nullptr, d->d_in, nullptr, nullptr));
-  return align256((size_t)p.splits * d->rows * 2 * d->d_hidden * sizeof(float));
+  if (few(d)) return 0;
+  const grouped::Call c = product_of(d, nullptr, d->d_in, nullptr, nullptr);
+  return grouped::stream_supported(d->dtype, grouped::FWD, c) ? align256(grouped::plan(d->dtype, grouped::FWD, c, true, ~(size_t)0).parts) : 0;
 }
-size_t workspace_bytes(const poetx_gated_desc* d) { return d->rows == 0 ? 0 : operand_bytes(d) + sums_bytes(d); }
+size_t workspace_bytes(const poetx_gated_desc* d) { return d->rows == 0 || few(d) ? 0 : operand_bytes(d) + sums_bytes(d); }
 
 void products(const poetx_gated_desc* d, const void* X, i64 ldx, const void* W, const int32_t* offsets, gated::Mode mode, const gated::Out& out, void* ws, hipStream_t st) {
-  if (d->flags & POETX_GATED_W_MX4) {
+  gated::Call q{X, W, ldx, offsets, d->rows, d->d_in, d->d_hidden, d->groups, mode, out};
+  const bool four = d->flags & POETX_GATED_W_MX4;
+  if (few(d)) {
+    StageTimer tm(POETX_STAGE_DENSE, st);
+    return gated::few_launch(d->dtype, four, q, st);
+  }
+  if (four) {
     StageTimer tm(POETX_STAGE_DEQUANT, st);
     mx4_dequantize_groups_launch(W, d->groups, 2 * d->d_hidden, d->d_in, offsets, d->rows, ws, st);
-    W = ws;
+    q.W = W = ws;
   }
   StageTimer tm(POETX_STAGE_DENSE, st);
-  grouped::Call c = product_of(d, X, ldx, W, offsets);
-  c.out = (char*)ws + operand_bytes(d);
-  const grouped::Plan p = plan_of(d, c);
-  const gated::Call q{X, W, ldx, offsets, d->rows, d->d_in, d->d_hidden, d->groups, mode, out};
-  if (p.kernel >= grouped::STREAM_256 && p.splits == 1 && gated::stream_supported(d->dtype, q)) return gated::stream_launch(d->dtype, p.kernel, q, st);
-  if (p.kernel >= grouped::STREAM_256) grouped::stream_sums(d->dtype, p, c, c.out, st);
-  else grouped::edge_sums(d->dtype, p.kernel, c, st);
-  gated::rows_launch(d->dtype, gated::SUMS, gated::In{c.out, nullptr, 0, p.splits}, offsets, d->groups, d->rows, d->d_hidden, mode, out, st);
+  const grouped::Call c = product_of(d, X, ldx, W, offsets);
+  const bool streams = gated::stream_supported(d->dtype, q);
+  const size_t scratch = sums_bytes(d);
+  const grouped::Plan p = grouped::plan(d->dtype, grouped::FWD, c, streams, scratch);
+  if (p.kernel < grouped::STREAM_256) return gated::edge_launch(d->dtype, p.kernel, q, st);
+  if (p.splits == 1) return gated::stream_launch(d->dtype, p.kernel, q, st);
+  void* sums = (char*)ws + operand_bytes(d);
+  grouped::stream_sums(d->dtype, p, c, sums, st);
+  gated::rows_launch(d->dtype, gated::SUMS, gated::In{sums, nullptr, 0, p.splits}, offsets, d->groups, d->rows, d->d_hidden, mode, out, st);
 }
 
 }  // namespace

@@ -41,7 +41,8 @@ bool stream_supported(int dtype, const Call& c) {
   const i64 wide = (1ll << 31) / (es * 256);      // a tile's rows span less than 2^31 bytes, and so do a group's weights
   auto fits = [&](const void* p, i64 ld) { return ((uintptr_t)p & 15) == 0 && ld % v == 0 && ld < wide; };
   const bool hold = c.mode == HOLD || c.mode == BWD;
-  return c.groups <= 256 && c.m % v == 0 && c.n % v == 0 && fits(c.X, c.ldx) && ((uintptr_t)c.W & 15) == 0 && (2 * (i64)c.n + 256) * c.m * es < (1ll << 31) &&
+  return c.groups <= 256 && c.m % v == 0 && c.n % v == 0 && fits(c.X, c.ldx) && ((uintptr_t)c.W & 15) == 0 && c.m < wide / 2 && 2 * (i64)c.n < wide &&
+         (2 * (i64)c.n + 256) * c.m * es < (1ll << 31) &&
          (!c.out.H || fits(c.out.H, c.out.ldh)) && (!hold || (fits(c.out.G, c.out.ldgu) && fits(c.out.U, c.out.ldgu))) && (c.mode != BWD || fits(c.out.dH, c.out.lddh)) &&
          (c.mode != HOLD_MX8 || c.n < wide);
 }

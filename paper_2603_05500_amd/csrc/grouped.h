@@ -144,8 +144,7 @@ bool stream_supported(int dtype, Dir dir, const Call& c);
 void stream_launch(int dtype, Dir dir, const Plan& p, const Call& c, void* scratch, hipStream_t st);
 // fp32 sums of a contraction's ranges, [split][rows][cols], added in order into c.out
 void add_parts(int dtype, const void* parts, int splits, int cols, const Call& c, hipStream_t st);
-// Z = X W^T in fp32, as `splits` sums of ranges of the contraction, [split][rows][n] (any leading dimension of the edge kernels', whose contractions are whole)
-void edge_sums(int dtype, Kernel k, const Call& c, hipStream_t st);
+// Z = X W^T as fp32 sums of the plan's ranges of the contraction, [split][rows][n]
 void stream_sums(int dtype, const Plan& p, const Call& c, void* sums, hipStream_t st);
 // Z = X W^T with X rounded to four bits on the way, W a 4-bit buffer
 bool codes_supported(const poetx_grouped_desc* d, const void* Z, i64 ldz);

@@ -94,9 +94,5 @@ void edge_launch(int dtype, Dir dir, Kernel k, const Call& c, hipStream_t st) {
   else f ? launch_dir<float, float, WEIGHT, false>(k, c, st) : launch_dir<uint16_t, float, WEIGHT, false>(k, c, st);
 }
 
-void edge_sums(int dtype, Kernel k, const Call& c, hipStream_t st) {
-  dtype == POETX_F32 ? launch_dir<float, float, FWD, false>(k, c, st) : launch_dir<uint16_t, float, FWD, false>(k, c, st);
-}
-
 }  // namespace grouped
 }  // namespace poetx

@@ -9,9 +9,8 @@
 //   VALUES  32 codes with their scale, decoded in registers: four MFMAs of depth 32, in which the four groups of 16 lanes hold four different blocks of 32
 //           (the order of a contraction is free as long as both operands keep it)
 //   CODES   32 codes, and 32 of X: one scaled MFMA of depth 128
-#include "edge_gemm.h"
-#include "grouped.h"
-#include "mx4.h"
+// A gated block's weight rows come in turn from gate and up, so that a tile has G and U of half as many columns of H.
+#include "gated.h"
 
 namespace poetx {
 namespace grouped {
@@ -35,16 +34,72 @@ struct FewArgs {
   const int32_t* offsets;
   i64 rows;
   int m, n, groups, units, tiles_n;
+  gated::Out block;         // GATED (n: d_hidden)
 };
 
-template <int RT, int NT, int NW, Kind KIND, int U>
+constexpr int NOT_GATED = -1;
+
+// What a gated block makes of G and U of a tile, `part` being sums of NW waves [16 NT rows][8 RT pairs].  HOLD_MX8: RT = 4, the 32 columns of a block.
+template <int RT, int NT, int NW, int MODE, class T>
+__device__ __forceinline__ void gated_out(const FewArgs& a, const RowTile& t, int rows, int h0, const float (&part)[NW][RT * NT * 256]) {
+  const gated::Out& o = a.block;
+  for (int i = threadIdx.x; i < RT * NT * 128; i += 64 * NW) {
+    const int row = i / (8 * RT), col = h0 + i % (8 * RT);
+    float g = 0.f, u = 0.f;
+#pragma unroll
+    for (int z = 0; z < NW; ++z) g += part[z][2 * i], u += part[z][2 * i + 1];
+    const bool on = row < rows && col < a.n;
+    const i64 at = t.r0 + row;
+    if constexpr (MODE == gated::HOLD_MX8) {
+      static_assert(MODE != gated::HOLD_MX8 || RT == 4, "a block of 32 columns to half a wave");
+      auto keep = [&](float v, const void* Q) {
+        uint32_t m = on ? __builtin_bit_cast(uint32_t, v) & 0x7fffffffu : 0;
+#pragma unroll
+        for (int s = 1; s < 32; s *= 2) {
+          const uint32_t other = __shfl_xor(m, s);
+          m = other > m ? other : m;
+        }
+        const uint32_t sb = mx8::scale_byte(m);
+        if (row >= rows) return;
+        const mx8::View q = mx8::view(Q, a.rows, a.n);
+        const i64 unit = at * mx8::units(a.n) + col / mx8::UNIT;
+        q.codes[unit * mx8::UNIT + col % mx8::UNIT] = (uint8_t)(on && sb != 255 ? mx8::to_code(v, sb) : 0);
+        if (i % 32 == 0) ((uint8_t*)q.scales)[unit * 4 + col % mx8::UNIT / 32] = (uint8_t)sb;
+      };
+      keep(g, o.G);
+      keep(u, o.U);
+    }
+    if (!on) continue;
+    auto put = [&](void* p, i64 ld, float v) {
+      if constexpr (sizeof(T) == 4) ((float*)p)[at * ld + col] = v;
+      else ((uint16_t*)p)[at * ld + col] = (uint16_t)mm::pack2_bf16(v, 0.f);
+    };
+    if constexpr (MODE == gated::HOLD) {
+      put(o.G, o.ldgu, g);
+      put(o.U, o.ldgu, u);
+    }
+    float v, d;
+    gated::act_both(o.act, g, v, d);
+    if constexpr (MODE == gated::BWD) {
+      float dh;
+      if constexpr (sizeof(T) == 4) dh = ((const float*)o.dH)[at * o.lddh + col];
+      else dh = bf16_bits_to_float(((const uint16_t*)o.dH)[at * o.lddh + col]);
+      put(o.G, o.ldgu, dh * u * d);
+      put(o.U, o.ldgu, dh * v);
+      if (!o.H) continue;
+    }
+    put(o.H, o.ldh, v * u);
+  }
+}
+
+template <int RT, int NT, int NW, Kind KIND, int U, int MODE>
 __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(FewArgs a, int first) {
   __shared__ float part[NW][RT * NT * 256];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int x = lane & 15, q = lane >> 4;
   const int bx = first + (int)blockIdx.x;
-  const int rt_no = bx / a.tiles_n, n0 = bx % a.tiles_n * (16 * RT);
+  const int rt_no = bx / a.tiles_n, n0 = bx % a.tiles_n * (MODE == NOT_GATED ? 16 * RT : 8 * RT);
   RowTile t;
   if (a.groups == 1) {
     const Range r = own_range(a.offsets, 0, a.rows);
@@ -60,8 +115,13 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(FewArgs a, int fir
   i64 wrow[RT];
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    const int row = n0 + 16 * r + x;
-    wrow[r] = (i64)t.g * a.n + (row < a.n ? row : a.n - 1);
+    if constexpr (MODE == NOT_GATED) {
+      const int row = n0 + 16 * r + x;
+      wrow[r] = (i64)t.g * a.n + (row < a.n ? row : a.n - 1);
+    } else {
+      const int row = n0 + 8 * r + (x >> 1);
+      wrow[r] = ((i64)t.g * 2 + (x & 1)) * a.n + (row < a.n ? row : a.n - 1);
+    }
   }
   i64 xrow[NT];
 #pragma unroll
@@ -203,6 +263,7 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(FewArgs a, int fir
 #pragma unroll
       for (int e = 0; e < 4; ++e) part[wave][((16 * c + x) * RT + r) * 16 + 4 * q + e] = acc[r][c][e];
   __syncthreads();
+  if constexpr (MODE != NOT_GATED) return gated_out<RT, NT, NW, MODE, std::conditional_t<KIND == SINGLE, float, uint16_t>>(a, t, rows, n0, part);
   for (int i = tid; i < RT * NT * 256; i += 64 * NW) {
     const int row = i / (16 * RT), col = n0 + i % (16 * RT);
     float y = 0.f;
@@ -216,12 +277,12 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(FewArgs a, int fir
   }
 }
 
-template <int RT, int NT, int NW, Kind KIND, int U>
+template <int RT, int NT, int NW, Kind KIND, int U, int MODE = NOT_GATED>
 void go(FewArgs a, hipStream_t st) {
-  a.tiles_n = ceil_div(a.n, 16 * RT);
+  a.tiles_n = MODE == NOT_GATED ? ceil_div(a.n, 16 * RT) : MODE == gated::HOLD_MX8 ? mx8::units(a.n) * 4 : ceil_div(a.n, 8 * RT);      // HOLD_MX8: codes past the last column are zeros
   const i64 total = (a.groups == 1 ? (a.rows + 16 * NT - 1) / (16 * NT) : most_row_tiles(a.rows, a.groups, 16 * NT)) * a.tiles_n;
   launch_in_rows(total, [&](int first, unsigned count) {
-    hipLaunchKernelGGL((grouped_few_kernel<RT, NT, NW, KIND, U>), dim3(count), dim3(64 * NW), 0, st, a, first);
+    hipLaunchKernelGGL((grouped_few_kernel<RT, NT, NW, KIND, U, MODE>), dim3(count), dim3(64 * NW), 0, st, a, first);
   });
 }
 
@@ -247,6 +308,31 @@ void pick(const FewArgs& a, hipStream_t st) {
   else if (mean <= 16) go<4, 1, 8, KIND, 4>(a, st);
   else if (mean <= 32 || tiles < 512 * 16) go<4, 2, 4, KIND, 1>(a, st);
   else go<4, 4, 4, KIND, 1>(a, st);
+}
+
+// a gated block: of twice as many weight rows
+template <Kind KIND, int MODE>
+void pick_gated(const FewArgs& a, hipStream_t st) {
+  const i64 live = a.rows < a.groups ? a.rows : a.groups, mean = (a.rows + live - 1) / live, tiles = small_tiles(a.rows, a.groups, 2 * a.n);
+  if constexpr (MODE != gated::HOLD_MX8) {
+    if (tiles <= (KIND == SINGLE ? 1024 : 768)) return go<1, 1, 4, KIND, KIND == SINGLE ? 1 : 4, MODE>(a, st);
+  }
+  if constexpr (KIND == SINGLE) {
+    if constexpr (MODE == gated::HOLD_MX8) return go<4, 1, 4, KIND, 1, MODE>(a, st);
+    else return go<2, 2, 4, KIND, 1, MODE>(a, st);
+  } else if constexpr (KIND == DENSE) {
+    if constexpr (MODE != gated::HOLD_MX8) {
+      if (tiles <= 1024 && mean <= 8) return go<1, 1, 4, KIND, 4, MODE>(a, st);
+    }
+    return go<4, 1, 4, KIND, 2, MODE>(a, st);
+  } else {
+    if constexpr (MODE != gated::HOLD_MX8) {
+      if (mean <= 8) return go<2, 1, 4, KIND, 4, MODE>(a, st);
+    }
+    if (mean <= 16) return go<4, 1, 8, KIND, 4, MODE>(a, st);
+    if (mean <= 32 || tiles < 512 * 16) return go<4, 2, 4, KIND, 1, MODE>(a, st);
+    go<4, 4, 4, KIND, 1, MODE>(a, st);
+  }
 }
 
 }  // namespace
@@ -285,4 +371,29 @@ void few_codes(const poetx_grouped_desc* d, const void* Xq, const void* Wq, cons
 }
 
 }  // namespace grouped
+
+namespace gated {
+
+// `four`: W is a 4-bit buffer
+void few_launch(int dtype, bool four, const Call& c, hipStream_t st) {
+  using namespace grouped;
+  FewArgs a{c.X, nullptr, c.W, nullptr, nullptr, c.ldx, 0, c.offsets, c.rows, c.m, c.n, c.groups, (c.m + 127) / 128, 0, c.out};
+  auto typed = [&](auto MODE_) {
+    constexpr int MODE = decltype(MODE_)::value;
+    if (four) {
+      const mx4::View w = mx4::view(c.W, 2 * (i64)c.groups * c.n, c.m);
+      a.W = w.codes;
+      a.ws = w.scales;
+      pick_gated<VALUES, MODE>(a, st);
+    } else {
+      dtype == POETX_F32 ? pick_gated<SINGLE, MODE>(a, st) : pick_gated<DENSE, MODE>(a, st);
+    }
+  };
+  if (c.mode == FWD) typed(std::integral_constant<int, FWD>{});
+  else if (c.mode == HOLD) typed(std::integral_constant<int, HOLD>{});
+  else if (c.mode == HOLD_MX8) typed(std::integral_constant<int, HOLD_MX8>{});
+  else typed(std::integral_constant<int, BWD>{});
+}
+
+}  // namespace gated
 }  // namespace poetx

@@ -62,9 +62,10 @@ def test_gated_forward_arguments(clib):  # noqa: F811
     four, both = px.GATED_W_MX4, px.GATED_W_MX4 | px.GATED_HELD_MX8
     assert fwd(flags=four, W=at(W, 8)) == 1
     assert fwd(flags=both, G=at(G, 8)) == fwd(flags=both, U=at(U, 4)) == fwd(flags=both, U=at(G, 512 * 100)) == 1
-    need = px.poetx_gated_workspace_bytes(_desc(flags=four))
-    assert need > 0 and fwd(flags=four, ws=None) == fwd(flags=four, n=need - 1) == fwd(flags=four, ws=at(ws, 8)) == 5
-    assert fwd(flags=four, ws=X) == fwd(flags=four, ws=H) == fwd(flags=four, ws=at(G, 16)) == 1
+    many = _desc(flags=four, rows=4096)      # more rows than the kernels for a handful take
+    need = px.poetx_gated_workspace_bytes(many)
+    assert need > 0 and fwd(d=many, ws=None) == fwd(d=many, n=need - 1) == fwd(d=many, ws=at(ws, 8)) == 5
+    assert fwd(d=many, ws=X) == fwd(d=many, ws=H) == fwd(d=many, ws=at(G, 16)) == 1
     # no rows: nothing to do, nothing looked at
     assert fwd(d=_desc(rows=0), X=None, H=None, G=None, U=None, ws=None, n=0) == 0
 
@@ -90,8 +91,9 @@ def test_gated_backward_arguments(clib):  # noqa: F811
     assert again(X=None) == again(W=None) == 1 and again(ldx=255) == 2
     assert again(dG=X) == again(H=W) == 1
     four = px.GATED_W_MX4
-    need = px.poetx_gated_workspace_bytes(_desc(flags=four))
-    assert again(flags=four, ws=None) == again(flags=four, n=need - 1) == 5 and again(flags=four, ws=dH) == again(flags=four, ws=dU) == 1
+    need = px.poetx_gated_workspace_bytes(_desc(flags=four, rows=4096))
+    assert again(flags=four, rows=4096, ws=None) == again(flags=four, rows=4096, n=need - 1) == 5
+    assert again(flags=four, rows=4096, ws=dH) == again(flags=four, rows=4096, ws=dU) == 1
     assert bwd(rows=0, dH=None, G=None, U=None, dG=None, dU=None, H=None) == 0
     assert again(rows=0, dH=None, X=None, dG=None, dU=None, H=None, ws=None, n=0) == 0
 
