@@ -63,7 +63,7 @@ __device__ __forceinline__ void gated_out(const FewArgs& a, const RowTile& t, in
         if (row >= rows) return;
         const mx8::View q = mx8::view(Q, a.rows, a.n);
         const i64 unit = at * mx8::units(a.n) + col / mx8::UNIT;
-        q.codes[unit * mx8::UNIT + col % mx8::UNIT] = (uint8_t)(on && sb != 255 ? mx8::to_code(v, sb) : 0);
+        q.codes[unit * mx8::UNIT + col % mx8::UNIT] = (uint8_t)(on && sb != 255 ? mx8::to_code(v, sb) & 255 : 0);
         if (i % 32 == 0) ((uint8_t*)q.scales)[unit * 4 + col % mx8::UNIT / 32] = (uint8_t)sb;
       };
       keep(g, o.G);

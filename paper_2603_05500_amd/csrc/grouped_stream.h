@@ -206,13 +206,9 @@ __device__ __forceinline__ void gated_tile(const StreamArgs& g, floatx4 (&acc)[C
   // codes and the scale of a block of 32 columns (two pieces) of each row; columns past the last are no part of it and have codes of zero
   auto quantise = [&](const float (&z)[AT_ONCE][4], int p, uint32_t& d0, uint32_t& d1, uint32_t& sb) __attribute__((always_inline)) {
     const bool in0 = 16 * p + 4 * q4 < cols, in1 = 16 * p + 16 + 4 * q4 < cols;
-    uint32_t m = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t s0 = in0 ? __builtin_bit_cast(uint32_t, z[0][e]) & 0x7fffffffu : 0, s1 = in1 ? __builtin_bit_cast(uint32_t, z[AT_ONCE - 1][e]) & 0x7fffffffu : 0;
-      m = s0 > m ? s0 : m;
-      m = s1 > m ? s1 : m;
-    }
+    const uint32_t m0 = in0 ? mx8::largest4(z[0][0], z[0][1], z[0][2], z[0][3]) : 0;
+    const uint32_t m1 = in1 ? mx8::largest4(z[AT_ONCE - 1][0], z[AT_ONCE - 1][1], z[AT_ONCE - 1][2], z[AT_ONCE - 1][3]) : 0;
+    uint32_t m = m0 > m1 ? m0 : m1;
     const auto t = __builtin_amdgcn_permlane16_swap(m, m, false, false);      // over the four groups of 16 lanes
     m = t[0] > t[1] ? t[0] : t[1];
     const auto f = __builtin_amdgcn_permlane32_swap(m, m, false, false);
@@ -323,7 +319,10 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   constexpr bool FP4 = C::FP4, FP32 = C::ELEM == F32, A_K = DIR != WEIGHT, B_K = DIR == FWD;
   // WIDE: rows come 64 deep, whole 128-byte lines.  Two stages are a unit, which arrives in two halves of its rows, one per stage; as it is needed as a whole, and its
   // place is free, with its first stage, the last half is in flight a stage less, and the ring has to be deep.  As in the dense product, 64-byte pieces would ask for every line twice.
-  constexpr bool WIDE = A_K && B_K && C::ELEM == BF16 && C::NS >= 6;
+  constexpr bool BEHIND = A_K && B_K && C::ELEM == BF16 && C::NS >= 6;
+  // WHOLE_UNITS: the same where the ring has two units only: one of them arrives, both halves of its rows, while the second stage of the other is multiplied, whose place it takes.
+  constexpr bool WHOLE_UNITS = GATED && A_K && B_K && C::ELEM == BF16 && C::NS == 4;
+  constexpr bool WIDE = BEHIND || WHOLE_UNITS;
   constexpr int DEPTH = C::DEPTH, ES = FP32 ? 4 : 2;      // bytes of an element (not of a code)
   static_assert(!FP4 || DIR == FWD, "codes are contracted along their rows");
   constexpr int BM = C::BM, BN = C::BN, NS = C::NS, STAGE_BYTES = C::STAGE_BYTES, A_BYTES = C::A_BYTES;
@@ -662,7 +661,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
 
   start_tile();
 #pragma unroll 1
-  for (int t = 0; t < NS - (WIDE ? 1 : 0); ++t) {
+  for (int t = 0; t < NS - (BEHIND ? 1 : 0); ++t) {
 #pragma unroll
     for (int i = 0; i < 6; ++i) next_b(i);
 #pragma unroll
@@ -672,7 +671,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
     issue_advance();
     tile_advance();
   }
-  mm::wait_vmcnt_and_barrier<(WIDE ? NS - 3 : NS - 1) * LPT>();
+  mm::wait_vmcnt_and_barrier<(BEHIND ? NS - 3 : WHOLE_UNITS ? NS - 2 : NS - 1) * LPT>();
   Frags F, Gf;
   int cslot = 0;
 #pragma unroll
@@ -684,7 +683,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
     auto multiply = [&](const Frags& X, Frags& Y, auto ODD) __attribute__((always_inline)) {      // ODD: the stage in X is the second of a unit
       constexpr bool odd = decltype(ODD)::value;
       // Every wave holds this stage in registers and the next one has landed (WIDE: with the other half of its unit).  Stages up to kt + NS - 1 are issued, WIDE one less.
-      mm::wait_all_reads_and_barrier<(WIDE ? odd ? NS - 4 : NS - 3 : NS - 2) * LPT>();
+      mm::wait_all_reads_and_barrier<(BEHIND ? odd ? NS - 4 : NS - 3 : WHOLE_UNITS ? odd ? 0 : NS - 2 : NS - 2) * LPT>();
       const int nslot = cslot + 1 == NS ? 0 : cslot + 1;
       in_turn(std::make_integer_sequence<int, MF>{}, [&](auto I) __attribute__((always_inline)) {
         constexpr int i = decltype(I)::value, a = i % TM, b = i / TM % TN;
@@ -692,10 +691,14 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
         else if constexpr (FP32) mfma_fp32(acc[a][b], X.b[b][i / (TM * TN)], X.a[a][i / (TM * TN)]);
         else dense::mfma16(acc[a][b], __builtin_bit_cast(bf16x8, X.b[b]), __builtin_bit_cast(bf16x8, X.a[a]));
         if constexpr (i % RS == 0 && i / RS < TM + TN) load_piece(Y, nslot, i / RS, !odd);
-        if constexpr (i % DS == W * DS / 4 && i / DS < LPT) issue(i / DS);
-        if constexpr (i < 6) next_b(i);
-        if constexpr (i >= IPWA * DS && i < IPWA * DS + 4) next_a(i - IPWA * DS);
-        if constexpr (i == MF - 1) issue_advance();
+        // WHOLE_UNITS: two stages' loads in the time of one
+        constexpr int span = WHOLE_UNITS ? MF / 2 : MF, every = WHOLE_UNITS ? DS / 2 : DS, at = i % span;
+        if constexpr (!WHOLE_UNITS || odd) {
+          if constexpr (at % every == W * every / 4 && at / every < LPT) issue(at / every);
+          if constexpr (at < 6) next_b(at);
+          if constexpr (at >= IPWA * every && at < IPWA * every + 4) next_a(at - IPWA * every);
+          if constexpr (at == span - 1) issue_advance();
+        }
         __builtin_amdgcn_sched_barrier(0);
       });
       cslot = nslot;
@@ -704,9 +707,9 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
       const Where range = locate(ti);
       for (int kt = range.k0; kt < range.k1; kt += 2) {
         multiply(F, Gf, std::false_type{});
-        if (WIDE) tile_advance();
+        if (BEHIND) tile_advance();
         multiply(Gf, F, std::true_type{});
-        if (!WIDE) tile_advance();
+        if (!BEHIND) tile_advance();
       }
       if constexpr (FP32) {      // as settle() does
         asm volatile("s_nop 15\n\ts_nop 3");
