@@ -46,6 +46,7 @@ __device__ __forceinline__ float act_value(Act k, float g) {
 
 // What a call makes of G and U
 enum Mode { FWD, HOLD, HOLD_MX8, BWD };
+constexpr int NONE = -1;      // kernels that also make plain products: no block
 struct Out {
   void* H;            // BWD: may be null
   void* G;            // HOLD: G and U; BWD: dG and dU; HOLD_MX8: buffers
@@ -65,6 +66,53 @@ struct Call {
   Out out;
 };
 
+// Eight neighbouring columns of a row, from col on, in fp32 -> what the mode asks for.  g, u: G and U, changed; dh: dH (BWD).  HOLD_MX8: four lanes have the 32 columns of a block, all of
+// which are here; columns past the last have codes of zero.
+template <class T, Mode MODE>
+__device__ __forceinline__ void emit8(const Out& o, i64 rows, int n, i64 row, int col, bool on, float (&g)[8], float (&u)[8], const float (&dh)[8]) {
+  const int left = on ? n - col : 0;
+  if constexpr (MODE == HOLD_MX8) {
+    auto keep = [&](const float (&z)[8], const void* Q) __attribute__((always_inline)) {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = e < left ? z[e] : 0.f;
+      uint32_t codes[2], sb;
+      mx8::quantise8(v, codes, sb);
+      if (!on) return;
+      typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+      const mx8::View q = mx8::view(Q, rows, n);
+      const i64 unit = row * mx8::units(n) + col / mx8::UNIT;
+      *reinterpret_cast<u32x2*>(q.codes + unit * mx8::UNIT + col % mx8::UNIT) = u32x2{codes[0], codes[1]};
+      if (col % 32 == 0) ((uint8_t*)q.scales)[unit * 4 + col % mx8::UNIT / 32] = (uint8_t)sb;
+    };
+    keep(g, o.G);
+    keep(u, o.U);
+  }
+  if (left <= 0) return;
+  if constexpr (MODE == HOLD) {
+    edge::store8((T*)o.G + row * o.ldgu + col, g, left);
+    edge::store8((T*)o.U + row * o.ldgu + col, u, left);
+  }
+  float h[8];
+  if constexpr (MODE == BWD) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float v, d;
+      act_both(o.act, g[e], v, d);
+      h[e] = v * u[e];
+      g[e] = dh[e] * u[e] * d;
+      u[e] = dh[e] * v;
+    }
+    edge::store8((T*)o.G + row * o.ldgu + col, g, left);
+    edge::store8((T*)o.U + row * o.ldgu + col, u, left);
+    if (!o.H) return;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = act_value(o.act, g[e]) * u[e];
+  }
+  edge::store8((T*)o.H + row * o.ldh + col, h, left);
+}
+
 // Where G and U come from: matrices of the type, 8-bit buffers, or fp32 sums of parts of the contraction, [split][rows][2n]
 enum Source { SAME, MX8, SUMS };
 struct In {
@@ -75,6 +123,11 @@ struct In {
 };
 // a handful of rows per group, where grouped::few_supported() says so for 2n columns (grouped_few.hip): any sizes, strides and alignments; four: W is a 4-bit buffer
 void few_launch(int dtype, bool four, const Call& c, hipStream_t st);
+// W a 4-bit buffer, decoded on the way, and whole 16-byte vectors (grouped_values.hip).  False where another way is the better one: few_launch() if `few`, otherwise the weight written out
+// first.  sums: the workspace for parts of the contraction, sums_bytes of it; scratch: what the other way has for its own
+bool values_supported(const Call& c);
+bool values_launch(const Call& c, bool few, void* sums, size_t sums_bytes, size_t scratch, hipStream_t st);
+size_t values_parts_bytes(int m, int n, int groups, i64 rows, bool few, size_t scratch);
 // whole 16-byte vectors (gated_stream.hip); k: of plan() for a forward of 2n columns
 bool stream_supported(int dtype, const Call& c);
 void stream_launch(int dtype, grouped::Kernel k, const Call& c, hipStream_t st);

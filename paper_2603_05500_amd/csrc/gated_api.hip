@@ -43,30 +43,51 @@ bool pair_apart(const void* a, const void* b, i64 rows, i64 cols, i64 ld, size_t
 
 bool ld_fits(i64 rows, i64 ld) { return rows == 0 || ld < kMostElements / rows; }
 
-// What the 4-bit weight's values take of the workspace; sums of the products follow.
-size_t operand_bytes(const poetx_gated_desc* d) { return d->flags & POETX_GATED_W_MX4 ? align256((size_t)d->groups * 2 * d->d_hidden * d->d_in * 2) : 0; }
-
 // G | U as one product of 2n columns: what the choice of kernels goes by
 grouped::Call product_of(const poetx_gated_desc* d, const void* X, i64 ldx, const void* W, const int32_t* offsets) {
   return grouped::Call{X, nullptr, W, nullptr, ldx, 0, 2 * (i64)d->d_hidden, offsets, d->rows, d->d_in, 2 * d->d_hidden, d->groups, 0};
 }
-bool few(const poetx_gated_desc* d) {
-  return grouped::few_supported(d->dtype, grouped::FWD, d->rows, d->d_in, 2 * d->d_hidden, d->groups, d->flags & POETX_GATED_W_MX4 ? grouped::VALUES_MX4 : grouped::DENSE_WEIGHT);
-}
+bool few(const poetx_gated_desc* d, grouped::Weight w) { return grouped::few_supported(d->dtype, grouped::FWD, d->rows, d->d_in, 2 * d->d_hidden, d->groups, w); }
 // fp32 sums of contractions that are split among workgroups, where the tensors allow the streaming kernels
-size_t sums_bytes(const poetx_gated_desc* d) {
-  if (few(d)) return 0;
+size_t stream_sums_bytes(const poetx_gated_desc* d) {
   const grouped::Call c = product_of(d, nullptr, d->d_in, nullptr, nullptr);
   return grouped::stream_supported(d->dtype, grouped::FWD, c) ? align256(grouped::plan(d->dtype, grouped::FWD, c, true, ~(size_t)0).parts) : 0;
 }
-size_t workspace_bytes(const poetx_gated_desc* d) { return d->rows == 0 || few(d) ? 0 : operand_bytes(d) + sums_bytes(d); }
+// The workspace: a 4-bit weight's values, where a call may need them (which of two kernels for a handful of rows takes one depends on its tensors), then sums.
+struct Scratch {
+  size_t weight, sums;
+};
+Scratch scratch_of(const poetx_gated_desc* d) {
+  Scratch s{0, 0};
+  if (d->rows == 0) return s;
+  if (!(d->flags & POETX_GATED_W_MX4)) {
+    s.sums = few(d, grouped::DENSE_WEIGHT) ? 0 : stream_sums_bytes(d);
+    return s;
+  }
+  const bool streamed = few(d, grouped::VALUES_STREAMED_MX4);
+  if (!streamed || !few(d, grouped::VALUES_MX4)) {
+    s.weight = align256((size_t)d->groups * 2 * d->d_hidden * d->d_in * 2);
+    s.sums = stream_sums_bytes(d);
+  }
+  const size_t v = align256(gated::values_parts_bytes(d->d_in, d->d_hidden, d->groups, d->rows, streamed, s.sums));
+  s.sums = v > s.sums ? v : s.sums;
+  return s;
+}
+size_t workspace_bytes(const poetx_gated_desc* d) {
+  const Scratch s = scratch_of(d);
+  return s.weight + s.sums;
+}
 
 void products(const poetx_gated_desc* d, const void* X, i64 ldx, const void* W, const int32_t* offsets, gated::Mode mode, const gated::Out& out, void* ws, hipStream_t st) {
   gated::Call q{X, W, ldx, offsets, d->rows, d->d_in, d->d_hidden, d->groups, mode, out};
-  const bool four = d->flags & POETX_GATED_W_MX4;
-  if (few(d)) {
+  const bool four = d->flags & POETX_GATED_W_MX4, streamed = four && gated::values_supported(q);
+  const bool handful = few(d, !four ? grouped::DENSE_WEIGHT : streamed ? grouped::VALUES_STREAMED_MX4 : grouped::VALUES_MX4);
+  const Scratch s = scratch_of(d);
+  void* sums = (char*)ws + s.weight;
+  {
     StageTimer tm(POETX_STAGE_DENSE, st);
-    return gated::few_launch(d->dtype, four, q, st);
+    if (streamed && gated::values_launch(q, handful, sums, s.sums, s.sums, st)) return;
+    if (handful) return gated::few_launch(d->dtype, four, q, st);
   }
   if (four) {
     StageTimer tm(POETX_STAGE_DEQUANT, st);
@@ -75,12 +96,9 @@ void products(const poetx_gated_desc* d, const void* X, i64 ldx, const void* W, 
   }
   StageTimer tm(POETX_STAGE_DENSE, st);
   const grouped::Call c = product_of(d, X, ldx, W, offsets);
-  const bool streams = gated::stream_supported(d->dtype, q);
-  const size_t scratch = sums_bytes(d);
-  const grouped::Plan p = grouped::plan(d->dtype, grouped::FWD, c, streams, scratch);
+  const grouped::Plan p = grouped::plan(d->dtype, grouped::FWD, c, gated::stream_supported(d->dtype, q), s.sums);
   if (p.kernel < grouped::STREAM_256) return gated::edge_launch(d->dtype, p.kernel, q, st);
   if (p.splits == 1) return gated::stream_launch(d->dtype, p.kernel, q, st);
-  void* sums = (char*)ws + operand_bytes(d);
   grouped::stream_sums(d->dtype, p, c, sums, st);
   gated::rows_launch(d->dtype, gated::SUMS, gated::In{sums, nullptr, 0, p.splits}, offsets, d->groups, d->rows, d->d_hidden, mode, out, st);
 }

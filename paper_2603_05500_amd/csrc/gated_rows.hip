@@ -25,7 +25,7 @@ __global__ __launch_bounds__(256) void gated_rows_kernel(RowsArgs a, int block0)
   const int lane = threadIdx.x & 15;
   const i64 first = (i64)(block0 + (int)blockIdx.x) * (16 * UPL) + (threadIdx.x >> 4);
   const i64 r0 = grouped::offset_at(a.offsets, 0, a.rows), r1 = grouped::furthest_end(a.offsets, a.groups, a.rows);
-  const mx8::View qg = mx8::view(SRC == MX8 ? a.in.G : a.out.G, a.rows, a.n), qu = mx8::view(SRC == MX8 ? a.in.U : a.out.U, a.rows, a.n);
+  const mx8::View qg = mx8::view(a.in.G, a.rows, a.n), qu = mx8::view(a.in.U, a.rows, a.n);      // MX8
   float g[UPL][8], u[UPL][8], dh[UPL][8];
 #pragma unroll
   for (int p = 0; p < UPL; ++p) {
@@ -60,45 +60,7 @@ __global__ __launch_bounds__(256) void gated_rows_kernel(RowsArgs a, int block0)
 #pragma unroll
   for (int p = 0; p < UPL; ++p) {
     const i64 unit = first + 16 * p, row = unit / a.upr;
-    const bool on = row >= r0 && row < r1;
-    const int col = (int)(unit - row * a.upr) * mx8::UNIT + 8 * lane;
-    if constexpr (MODE == HOLD_MX8) {      // the lanes of a block work together; elements past the end are zeros
-      uint32_t c[2], word;
-      mx8::quantise_unit(g[p], lane, c, word);
-      if (on) {
-        *reinterpret_cast<u32x2*>(qg.codes + unit * mx8::UNIT + 8 * lane) = u32x2{c[0], c[1]};
-        if (lane == 0) qg.scales[unit] = word;
-      }
-      mx8::quantise_unit(u[p], lane, c, word);
-      if (on) {
-        *reinterpret_cast<u32x2*>(qu.codes + unit * mx8::UNIT + 8 * lane) = u32x2{c[0], c[1]};
-        if (lane == 0) qu.scales[unit] = word;
-      }
-    }
-    const int left = a.n - col;
-    if (!on || left <= 0) continue;
-    if constexpr (MODE == HOLD) {
-      edge::store8((T*)a.out.G + row * a.out.ldgu + col, g[p], left);
-      edge::store8((T*)a.out.U + row * a.out.ldgu + col, u[p], left);
-    }
-    float h[8];
-    if constexpr (MODE == BWD) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float v, d;
-        act_both(a.out.act, g[p][e], v, d);
-        h[e] = v * u[p][e];
-        g[p][e] = dh[p][e] * u[p][e] * d;
-        u[p][e] = dh[p][e] * v;
-      }
-      edge::store8((T*)a.out.G + row * a.out.ldgu + col, g[p], left);
-      edge::store8((T*)a.out.U + row * a.out.ldgu + col, u[p], left);
-      if (!a.out.H) continue;
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) h[e] = act_value(a.out.act, g[p][e]) * u[p][e];
-    }
-    edge::store8((T*)a.out.H + row * a.out.ldh + col, h, left);
+    emit8<T, MODE>(a.out, a.rows, a.n, row, (int)(unit - row * a.upr) * mx8::UNIT + 8 * lane, row >= r0 && row < r1, g[p], u[p], dh[p]);
   }
 }
 

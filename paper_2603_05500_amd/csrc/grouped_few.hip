@@ -37,7 +37,7 @@ struct FewArgs {
   gated::Out block;         // GATED (n: d_hidden)
 };
 
-constexpr int NOT_GATED = -1;
+constexpr int NOT_GATED = gated::NONE;
 
 // What a gated block makes of G and U of a tile, `part` being sums of NW waves [16 NT rows][8 RT pairs].  HOLD_MX8: RT = 4, the 32 columns of a block.
 template <int RT, int NT, int NW, int MODE, class T>

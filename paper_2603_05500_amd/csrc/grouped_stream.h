@@ -35,7 +35,7 @@ enum Elem { BF16, F32, CODES };
 
 // PARTS: fp32 sums of a range of the contraction go to `parts`, to be added up by another launch (bf16; fp32 needs no kernel of its own).
 // GATED: a gated block's forward or the recomputing half of its backward pass, as gated::Mode says; NOT_GATED otherwise.
-constexpr int NOT_GATED = -1;
+constexpr int NOT_GATED = gated::NONE;
 template <int BM_, int BN_, int NS_, Elem ELEM_, int PER_CU_ = 1, bool PARTS_ = false, int GATED_ = NOT_GATED>
 struct StreamTile {
   static constexpr int BM = BM_, BN = BN_, NS = NS_, NW = 4, PER_CU = PER_CU_;

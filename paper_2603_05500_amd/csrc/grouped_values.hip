@@ -26,14 +26,18 @@ struct ValuesArgs {
   int m, n, groups, units, tiles_n;
   int splits;      // PARTS: ranges of the contraction, whose fp32 sums go to parts, [split][rows][n]
   float* parts;
+  gated::Out block;      // MODE: of a gated block (n: d_hidden)
 };
 
-template <int BM, int BN, int NS, bool PARTS>
+// MODE: a gated block, a tile's first half of columns being gate's and its second half up's of as many columns of H.
+template <int BM, int BN, int NS, bool PARTS, int MODE>
 __global__ __launch_bounds__(256) void grouped_values_kernel(ValuesArgs g, int first) {
   constexpr int A_BYTES = BM * 256, B_BYTES = BN * 64, STAGE_BYTES = A_BYTES + B_BYTES + BN * 4;
   constexpr int IPWA = BM / 16, IPWB = BN / 64, LPU = IPWA + IPWB + 1, TM = BM / 32, TN = BN / 32, MF = TM * TN;
+  constexpr bool GATED = MODE != NOT_GATED;
+  constexpr int BW = GATED ? BN / 2 : BN;
   constexpr int OUT_LD = BN + 8;      // elements of a row of the tile on its way out: 16-byte chunks of 8 rows in different banks
-  typedef typename std::conditional<PARTS, float, uint16_t>::type Out;
+  typedef typename std::conditional<PARTS || GATED, float, uint16_t>::type Out;
   static_assert(BN <= 256 && IPWA % 2 == 0 && (NS - 1) * LPU < 64 && NS >= 3 && BM * OUT_LD * (int)sizeof(Out) <= NS * STAGE_BYTES, "values tile");
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int tiles = count_row_tiles(g.offsets, g.groups, g.rows, BM) * g.tiles_n, total = PARTS ? tiles * g.splits : tiles;
@@ -43,9 +47,11 @@ __global__ __launch_bounds__(256) void grouped_values_kernel(ValuesArgs g, int f
   const int split = PARTS ? id / tiles : 0, u0 = PARTS ? g.units * split / g.splits : 0, u1 = PARTS ? g.units * (split + 1) / g.splits : g.units;
   id -= split * tiles;
   const RowTile t = find_row_tile(g.offsets, g.groups, g.rows, BM, id / g.tiles_n);
-  const int n0 = id % g.tiles_n * BN;
+  const int n0 = id % g.tiles_n * BW;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1, q4 = lane >> 4, li = lane & 15;
-  const int rows = t.r1 - t.r0 < BM ? t.r1 - t.r0 : BM, cols = g.n - n0 < BN ? g.n - n0 : BN;
+  const int rows = t.r1 - t.r0 < BM ? t.r1 - t.r0 : BM, cols = g.n - n0 < BW ? g.n - n0 : BW;
+  auto weight_row = [&](int r) __attribute__((always_inline)) { return GATED && r >= BW ? g.n - BW + r : r; };      // from the tile's first one
+  const int wrows = GATED ? g.n + cols : cols;      // that the descriptors reach over
 
   // ---- loads: X a row's 16 chunks in the order chunk ^ row % 8, so that 8 rows' same chunk lies in different banks
   const int lda = 2 * (int)g.ldx, ldb = g.units * 64;
@@ -61,14 +67,14 @@ __global__ __launch_bounds__(256) void grouped_values_kernel(ValuesArgs g, int f
 #pragma unroll
   for (int i = 0; i < IPWB; ++i) {
     const int slot = (wave * IPWB + i) * 64 + lane, r = slot >> 2;
-    voffB[i] = (uint32_t)(r * ldb + 16 * dense::xk16_chunk(slot & 3, r));
+    voffB[i] = (uint32_t)(weight_row(r) * ldb + 16 * dense::xk16_chunk(slot & 3, r));
   }
   const int srow = (wave * 64) % BN;      // BN < 256: some waves bring the same scales
-  const uint32_t voffS = (uint32_t)((srow + lane) * g.units * 4);
-  const i64 wrow = (i64)t.g * g.n + n0;
+  const uint32_t voffS = (uint32_t)(weight_row(srow + lane) * g.units * 4);
+  const i64 wrow = (i64)t.g * (GATED ? 2 * g.n : g.n) + n0;
   // an operand's descriptor at the unit in issue, and the bytes from there on
   u32x4 ra{}, rb{}, rs{};
-  int left_a = uniform((rows - 1) * lda + 2 * g.m - 256 * u0), left_b = uniform(cols * ldb - 64 * u0), left_s = uniform((cols * g.units - u0) * 4);
+  int left_a = uniform((rows - 1) * lda + 2 * g.m - 256 * u0), left_b = uniform(wrows * ldb - 64 * u0), left_s = uniform((wrows * g.units - u0) * 4);
   auto start = [&](u32x4& r, const void* at, int left) __attribute__((always_inline)) {
     r = u32x4{(uint32_t)uniform((int)(uint64_t)at), (uint32_t)uniform((int)((uint64_t)at >> 32)) & 0xffffu, (uint32_t)left, 0x00020000u};
   };
@@ -195,10 +201,27 @@ __global__ __launch_bounds__(256) void grouped_values_kernel(ValuesArgs g, int f
     for (int b = 0; b < TN; ++b) {
       typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
       Out* at = out + (wm * (BM / 2) + a * 16 + li) * OUT_LD + wn * (BN / 2) + b * 16 + 4 * q4;
-      if constexpr (PARTS) *reinterpret_cast<floatx4*>(at) = acc[a][b];
+      if constexpr (PARTS || GATED) *reinterpret_cast<floatx4*>(at) = acc[a][b];
       else *reinterpret_cast<u32x2*>(at) = u32x2{mm::pack2_bf16(acc[a][b][0], acc[a][b][1]), mm::pack2_bf16(acc[a][b][2], acc[a][b][3])};
     }
   __syncthreads();
+  if constexpr (GATED) {
+    for (int i = tid; i < BM * BW / 8; i += 256) {
+      const int row = i / (BW / 8), col = i % (BW / 8) * 8;
+      const bool on = row < rows;
+      float G[8], U[8], dh[8] = {};
+      const float* at = (const float*)out + row * OUT_LD + col;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const floatx4 x = *reinterpret_cast<const floatx4*>(at + 4 * h), y = *reinterpret_cast<const floatx4*>(at + BW + 4 * h);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) G[4 * h + e] = x[e], U[4 * h + e] = y[e];
+      }
+      if constexpr (MODE == gated::BWD) edge::load8((const uint16_t*)g.block.dH + (on ? t.r0 + row : t.r0) * g.block.lddh, on ? n0 + col : g.n, g.n, dh);
+      gated::emit8<uint16_t, (gated::Mode)MODE>(g.block, g.rows, g.n, t.r0 + row, n0 + col, on, G, U, dh);
+    }
+    return;
+  }
   constexpr int V = 16 / sizeof(Out);
   for (int i = tid; i < BM * BN / V; i += 256) {
     const int row = i / (BN / V), col = i % (BN / V) * V;
@@ -207,13 +230,13 @@ __global__ __launch_bounds__(256) void grouped_values_kernel(ValuesArgs g, int f
   }
 }
 
-template <int BM, int BN, int NS, bool PARTS = false>
+template <int BM, int BN, int NS, bool PARTS = false, int MODE = NOT_GATED>
 void go(ValuesArgs a, hipStream_t st) {
   constexpr int BYTES = NS * (BM * 256 + BN * 68);
-  auto kern = grouped_values_kernel<BM, BN, NS, PARTS>;
+  auto kern = grouped_values_kernel<BM, BN, NS, PARTS, MODE>;
   static const bool configured = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, BYTES) == hipSuccess;
   (void)configured;
-  a.tiles_n = ceil_div(a.n, BN);
+  a.tiles_n = MODE == NOT_GATED ? ceil_div(a.n, BN) : ceil_div(MODE == gated::HOLD_MX8 ? mx8::units(a.n) * mx8::UNIT : a.n, BN / 2);      // HOLD_MX8: codes past the last column are zeros
   launch_in_rows((a.groups == 1 ? (a.rows + BM - 1) / BM : most_row_tiles(a.rows, a.groups, BM)) * a.tiles_n * (PARTS ? a.splits : 1),
                  [&](int first, unsigned count) { hipLaunchKernelGGL(kern, dim3(count), dim3(256), BYTES, st, a, first); });
 }
@@ -230,8 +253,13 @@ bool values_supported(const poetx_grouped_desc* d, const void* X, i64 ldx, const
 // 2 to 3 % more time than the best would.  us, 64 x 128 / 128 x 128 / 128 x 256 / values: 14336 x 4096, 128 rows 22.6 / 29 / 46 / 66, 512 rows 71 / 61 / 52 / 88; 2048 x 5632, 1999 rows
 // 52 / 44 / 66 / 69 (three weights in turn; 128 x 128 41 to 43 with the one in the caches); 64 experts of 1376 x 2048 with 128 rows each 65 / 69 / 81 / 162.  64 x 128 four stages deep, one workgroup per CU: 23.7, 85, 60, 86.
 // Whole / in ranges / few rows: 1152 x 12032, 219 rows 51 / 20 / 41, 832 x 7232, 223 rows 33 / 16 / 25.
-bool values_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, bool few, bool whole, void* ws, size_t ws_bytes, size_t scratch,
-                   hipStream_t st) {
+namespace {
+
+struct ValuesPlan {
+  bool better;       // than the other way
+  int tile, ranges;
+};
+ValuesPlan values_plan(const poetx_grouped_desc* d, const Call& c, bool few, bool whole, size_t ws_bytes, size_t scratch) {
   struct Tile {
     int h, w;
     double rest, unit;      // us: of a launch; of a unit of a round of 256 tiles
@@ -256,18 +284,28 @@ bool values_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const vo
       if (us < least) least = us, best = i, ranges = splits;
     }
   }
-  const Call c{X, nullptr, Wq, Z, ldx, 0, ldz, offsets, d->rows, d->d_in, d->d_out, d->groups, 0};
   const double written = 2.5 + (double)(d->rows < d->groups ? d->rows : d->groups) * d->d_out * d->d_in * 2.53 / 5.5e6;
-  if (few ? least >= few_values_us(d) : whole && least >= written + plan(POETX_BF16, FWD, c, stream_supported(POETX_BF16, FWD, c), scratch).us) return false;
+  const bool other = few ? least >= few_values_us(d) : whole && least >= written + plan(POETX_BF16, FWD, c, stream_supported(POETX_BF16, FWD, c), scratch).us;
+  return ValuesPlan{!other, best, ranges};
+}
+void parts_launch(int tile, const ValuesArgs& a, hipStream_t st) { tile == 0 ? go<64, 128, 3, true>(a, st) : go<128, 128, 3, true>(a, st); }
+
+}  // namespace
+
+bool values_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const void* Wq, const int32_t* offsets, void* Z, i64 ldz, bool few, bool whole, void* ws, size_t ws_bytes, size_t scratch,
+                   hipStream_t st) {
+  const Call c{X, nullptr, Wq, Z, ldx, 0, ldz, offsets, d->rows, d->d_in, d->d_out, d->groups, 0};
+  const ValuesPlan p = values_plan(d, c, few, whole, ws_bytes, scratch);
+  if (!p.better) return false;
   StageTimer tm(POETX_STAGE_DENSE, st);
   const mx4::View w = mx4::view(Wq, (i64)d->groups * d->d_out, d->d_in);
-  const ValuesArgs a{(const uint16_t*)X, ldx, w.codes, w.scales, (uint16_t*)Z, ldz, offsets, d->rows, d->d_in, d->d_out, d->groups, units, 0, ranges, (float*)ws};
-  if (ranges > 1) {
-    best == 0 ? go<64, 128, 3, true>(a, st) : go<128, 128, 3, true>(a, st);
-    add_parts(POETX_BF16, ws, ranges, d->d_out, c, st);
-  } else if (best == 0) {
+  const ValuesArgs a{(const uint16_t*)X, ldx, w.codes, w.scales, (uint16_t*)Z, ldz, offsets, d->rows, d->d_in, d->d_out, d->groups, mx4::units(d->d_in), 0, p.ranges, (float*)ws, {}};
+  if (p.ranges > 1) {
+    parts_launch(p.tile, a, st);
+    add_parts(POETX_BF16, ws, p.ranges, d->d_out, c, st);
+  } else if (p.tile == 0) {
     go<64, 128, 3>(a, st);
-  } else if (best == 1) {
+  } else if (p.tile == 1) {
     go<128, 128, 3>(a, st);
   } else {
     go<128, 256, 3>(a, st);
@@ -276,4 +314,52 @@ bool values_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const vo
 }
 
 }  // namespace grouped
+
+namespace gated {
+namespace {
+
+poetx_grouped_desc twice(int m, int n, int groups, i64 rows) { return poetx_grouped_desc{m, 2 * n, groups, POETX_BF16, rows, POETX_GROUPED_W_MX4, 0}; }
+grouped::Call product_of(const void* X, i64 ldx, const void* W, const int32_t* offsets, i64 rows, int m, int n, int groups) {
+  return grouped::Call{X, nullptr, W, nullptr, ldx, 0, 2 * (i64)n, offsets, rows, m, 2 * n, groups, 0};
+}
+
+}  // namespace
+
+bool values_supported(const Call& c) {
+  return c.m % 8 == 0 && c.n % 8 == 0 && c.ldx % 8 == 0 && ((uintptr_t)c.X & 15) == 0 && c.ldx < (1 << 22) && c.m < (1 << 22) &&
+         ((i64)c.n + 256) * mx4::units(c.m) * 64 < (1ll << 31);
+}
+size_t values_parts_bytes(int m, int n, int groups, i64 rows, bool few, size_t scratch) {
+  const poetx_grouped_desc d = twice(m, n, groups, rows);
+  const grouped::ValuesPlan p = grouped::values_plan(&d, product_of(nullptr, m, nullptr, nullptr, rows, m, n, groups), few, true, ~(size_t)0, scratch);
+  return p.better && p.ranges > 1 ? (size_t)p.ranges * rows * 2 * n * sizeof(float) : 0;
+}
+// The choice is that of a product of 2n columns: the tiles, the contraction and the bytes of the weight are the same.
+bool values_launch(const Call& c, bool few, void* sums, size_t sums_bytes, size_t scratch, hipStream_t st) {
+  using grouped::go;
+  const poetx_grouped_desc d = twice(c.m, c.n, c.groups, c.rows);
+  const grouped::ValuesPlan p = grouped::values_plan(&d, product_of(c.X, c.ldx, c.W, c.offsets, c.rows, c.m, c.n, c.groups), few, true, sums_bytes, scratch);
+  if (!p.better) return false;
+  const mx4::View w = mx4::view(c.W, 2 * (i64)c.groups * c.n, c.m);
+  grouped::ValuesArgs a{(const uint16_t*)c.X, c.ldx, w.codes, w.scales, nullptr, 0, c.offsets, c.rows, c.m, c.n, c.groups, mx4::units(c.m), 0, p.ranges, (float*)sums, c.out};
+  if (p.ranges > 1) {
+    a.n = 2 * c.n;
+    grouped::parts_launch(p.tile, a, st);
+    rows_launch(POETX_BF16, SUMS, In{sums, nullptr, 0, p.ranges}, c.offsets, c.groups, c.rows, c.n, c.mode, c.out, st);
+    return true;
+  }
+  auto tiled = [&](auto MODE_) {
+    constexpr int MODE = decltype(MODE_)::value;
+    if (p.tile == 0) go<64, 128, 3, false, MODE>(a, st);
+    else if (p.tile == 1) go<128, 128, 3, false, MODE>(a, st);
+    else go<128, 256, 3, false, MODE>(a, st);
+  };
+  if (c.mode == FWD) tiled(std::integral_constant<int, FWD>{});
+  else if (c.mode == HOLD) tiled(std::integral_constant<int, HOLD>{});
+  else if (c.mode == HOLD_MX8) tiled(std::integral_constant<int, HOLD_MX8>{});
+  else tiled(std::integral_constant<int, BWD>{});
+  return true;
+}
+
+}  // namespace gated
 }  // namespace poetx

@@ -53,8 +53,8 @@ __device__ __forceinline__ void values8(uint32_t lo, uint32_t hi, uint32_t scale
   v[4] = value<0>(hi, scale), v[5] = value<1>(hi, scale), v[6] = value<2>(hi, scale), v[7] = value<3>(hi, scale);
 }
 
-// Eight elements of a lane, sixteen lanes a unit -> the lane's codes and, in every lane, the unit's four scale bytes.
-__device__ __forceinline__ void quantise_unit(const float (&v)[8], int lane16, uint32_t (&codes)[2], uint32_t& word) {
+// Eight elements of a lane, four lanes a block -> the lane's codes and the block's scale byte.
+__device__ __forceinline__ void quantise8(const float (&v)[8], uint32_t (&codes)[2], uint32_t& sb) {
   const uint32_t t0 = largest4(v[0], v[1], v[2], v[3]), t1 = largest4(v[4], v[5], v[6], v[7]);
   uint32_t top = t0 > t1 ? t0 : t1;
 #pragma unroll
@@ -62,9 +62,14 @@ __device__ __forceinline__ void quantise_unit(const float (&v)[8], int lane16, u
     const uint32_t o = __shfl_xor(top, s);
     top = o > top ? o : top;
   }
-  const uint32_t sb = scale_byte(top);
+  sb = scale_byte(top);
   codes[0] = to_codes4(v[0], v[1], v[2], v[3], sb);
   codes[1] = to_codes4(v[4], v[5], v[6], v[7], sb);
+}
+// The same of sixteen lanes, a unit -> in every lane, the unit's four scale bytes.
+__device__ __forceinline__ void quantise_unit(const float (&v)[8], int lane16, uint32_t (&codes)[2], uint32_t& word) {
+  uint32_t sb;
+  quantise8(v, codes, sb);
   word = sb << (8 * (lane16 >> 2));
   word |= __shfl_xor(word, 4);
   word |= __shfl_xor(word, 8);
