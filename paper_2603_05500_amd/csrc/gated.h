@@ -123,12 +123,12 @@ struct In {
 };
 // a handful of rows per group, where grouped::few_supported() says so for 2n columns (grouped_few.hip): any sizes, strides and alignments; four: W is a 4-bit buffer
 void few_launch(int dtype, bool four, const Call& c, hipStream_t st);
-// W a 4-bit buffer, decoded on the way, and whole 16-byte vectors (grouped_values.hip).  False where another way is the better one: few_launch() if `few`, otherwise the weight written out
+// W a 4-bit buffer, decoded on the way, and X of whole 16-byte vectors (grouped_values.hip).  False where another way is the better one: few_launch() if `few`, otherwise the weight written out
 // first.  sums: the workspace for parts of the contraction, sums_bytes of it; scratch: what the other way has for its own
 bool values_supported(const Call& c);
 bool values_launch(const Call& c, bool few, void* sums, size_t sums_bytes, size_t scratch, hipStream_t st);
 size_t values_parts_bytes(int m, int n, int groups, i64 rows, bool few, size_t scratch);
-// whole 16-byte vectors (gated_stream.hip); k: of plan() for a forward of 2n columns
+// X and W of whole 16-byte vectors (gated_stream.hip); k: of plan() for a forward of 2n columns
 bool stream_supported(int dtype, const Call& c);
 void stream_launch(int dtype, grouped::Kernel k, const Call& c, hipStream_t st);
 void edge_launch(int dtype, grouped::Kernel k, const Call& c, hipStream_t st);      // any shape (gated_edge.hip)

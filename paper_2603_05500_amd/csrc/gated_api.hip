@@ -51,7 +51,8 @@ bool few(const poetx_gated_desc* d, grouped::Weight w) { return grouped::few_sup
 // fp32 sums of contractions that are split among workgroups, where the tensors allow the streaming kernels
 size_t stream_sums_bytes(const poetx_gated_desc* d) {
   const grouped::Call c = product_of(d, nullptr, d->d_in, nullptr, nullptr);
-  return grouped::stream_supported(d->dtype, grouped::FWD, c) ? align256(grouped::plan(d->dtype, grouped::FWD, c, true, ~(size_t)0).parts) : 0;
+  const gated::Call q{nullptr, nullptr, d->d_in, nullptr, d->rows, d->d_in, d->d_hidden, d->groups, gated::FWD, {}};
+  return d->d_hidden % 2 == 0 && gated::stream_supported(d->dtype, q) ? align256(grouped::plan(d->dtype, grouped::FWD, c, true, ~(size_t)0).parts) : 0;
 }
 // The workspace: a 4-bit weight's values, where a call may need them (which of two kernels for a handful of rows takes one depends on its tensors), then sums.
 struct Scratch {
@@ -96,7 +97,7 @@ void products(const poetx_gated_desc* d, const void* X, i64 ldx, const void* W, 
   }
   StageTimer tm(POETX_STAGE_DENSE, st);
   const grouped::Call c = product_of(d, X, ldx, W, offsets);
-  const grouped::Plan p = grouped::plan(d->dtype, grouped::FWD, c, gated::stream_supported(d->dtype, q), s.sums);
+  const grouped::Plan p = grouped::plan(d->dtype, grouped::FWD, c, gated::stream_supported(d->dtype, q), d->d_hidden % 2 == 0 ? s.sums : 0);      // sums are stored in whole vectors
   if (p.kernel < grouped::STREAM_256) return gated::edge_launch(d->dtype, p.kernel, q, st);
   if (p.splits == 1) return gated::stream_launch(d->dtype, p.kernel, q, st);
   grouped::stream_sums(d->dtype, p, c, sums, st);

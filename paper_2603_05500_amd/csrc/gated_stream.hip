@@ -33,18 +33,20 @@ void pick(grouped::Kernel k, const StreamArgs& a, hipStream_t st) {
   else if (k == grouped::STREAM_256x128) go<StreamTile<256, 128, 6, BF16, 1, false, MODE>>(a, st);
   else go<StreamTile<128, 128, 8, BF16, 1, false, MODE>>(a, st);
 }
+template <Mode MODE>
+void pick_narrow(grouped::Kernel k, const StreamArgs& a, hipStream_t st) {
+  if (k == grouped::SINGLE_128 || k == grouped::SINGLE_64) go<StreamTile<128, 128, 4, F32, 2, false, MODE, true>>(a, st);
+  else if (k == grouped::STREAM_256 || k == grouped::STREAM_256x128) go<StreamTile<256, 128, 6, BF16, 1, false, MODE, true>>(a, st);
+  else go<StreamTile<128, 128, 8, BF16, 1, false, MODE, true>>(a, st);
+}
 
 }  // namespace
 
 bool stream_supported(int dtype, const Call& c) {
   const int es = dtype == POETX_F32 ? 4 : 2, v = 16 / es;
   const i64 wide = (1ll << 31) / (es * 256);      // a tile's rows span less than 2^31 bytes, and so do a group's weights
-  auto fits = [&](const void* p, i64 ld) { return ((uintptr_t)p & 15) == 0 && ld % v == 0 && ld < wide; };
-  const bool hold = c.mode == HOLD || c.mode == BWD;
-  return c.groups <= 256 && c.m % v == 0 && c.n % v == 0 && fits(c.X, c.ldx) && ((uintptr_t)c.W & 15) == 0 && c.m < wide / 2 && 2 * (i64)c.n < wide &&
-         (2 * (i64)c.n + 256) * c.m * es < (1ll << 31) &&
-         (!c.out.H || fits(c.out.H, c.out.ldh)) && (!hold || (fits(c.out.G, c.out.ldgu) && fits(c.out.U, c.out.ldgu))) && (c.mode != BWD || fits(c.out.dH, c.out.lddh)) &&
-         (c.mode != HOLD_MX8 || c.n < wide);
+  return c.groups <= 256 && c.m % v == 0 && c.ldx % v == 0 && (((uintptr_t)c.X | (uintptr_t)c.W) & 15) == 0 && c.ldx < wide && c.m < wide / 2 && 2 * (i64)c.n < wide &&
+         (2 * (i64)c.n + 256) * c.m * es < (1ll << 31) && c.out.ldh < wide && c.out.ldgu < wide && c.out.lddh < wide;
 }
 
 void stream_launch(int dtype, grouped::Kernel k, const Call& c, hipStream_t st) {
@@ -61,10 +63,19 @@ void stream_launch(int dtype, grouped::Kernel k, const Call& c, hipStream_t st) 
   a.groups = c.groups;
   a.splits = 1;
   a.block = c.out;
-  if (c.mode == FWD) pick<FWD>(k, a, st);
-  else if (c.mode == HOLD) pick<HOLD>(k, a, st);
-  else if (c.mode == HOLD_MX8) pick<HOLD_MX8>(k, a, st);
-  else pick<BWD>(k, a, st);
+  const int v = 16 / es;
+  auto whole = [&](const void* p, i64 ld) { return ((uintptr_t)p & 15) == 0 && ld % v == 0; };
+  const bool pair = c.mode == HOLD || c.mode == BWD;
+  const bool wide = c.n % v == 0 && whole(c.out.H, c.out.H ? c.out.ldh : 0) && (!pair || (whole(c.out.G, c.out.ldgu) && whole(c.out.U, c.out.ldgu))) &&
+                    (c.mode != BWD || whole(c.out.dH, c.out.lddh));
+  auto mode = [&](auto MODE_) {
+    constexpr Mode MODE = decltype(MODE_)::value;
+    wide ? pick<MODE>(k, a, st) : pick_narrow<MODE>(k, a, st);
+  };
+  if (c.mode == FWD) mode(std::integral_constant<Mode, FWD>{});
+  else if (c.mode == HOLD) mode(std::integral_constant<Mode, HOLD>{});
+  else if (c.mode == HOLD_MX8) mode(std::integral_constant<Mode, HOLD_MX8>{});
+  else mode(std::integral_constant<Mode, BWD>{});
 }
 
 }  // namespace gated

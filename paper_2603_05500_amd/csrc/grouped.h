@@ -20,6 +20,7 @@ struct Call {
   i64 rows;
   int m, n, groups;
   int accumulate;
+  int row_in = 0, row_in2 = 0;      // WEIGHT on the streams: elements that may be read of a row of in, in2, where that is more than m, n
 };
 
 // First row and end of a group.  Offsets are taken inside the tensor.  Where rows are computed none is taken below those before it: whatever they say, groups then share
@@ -141,6 +142,7 @@ double tiles_of(Dir dir, i64 rows, int m, int n, int groups, int h, int w);
 void edge_launch(int dtype, Dir dir, Kernel k, const Call& c, hipStream_t st);      // any shape (grouped_edge.hip)
 // whole 16-byte vectors (grouped_stream.hip)
 bool stream_supported(int dtype, Dir dir, const Call& c);
+bool weight_stream_supported(int dtype, const Call& c);      // of operands in rows of whole vectors, whatever m and n, with scratch for what is not; c.out 16-byte aligned
 void stream_launch(int dtype, Dir dir, const Plan& p, const Call& c, void* scratch, hipStream_t st);
 // fp32 sums of a contraction's ranges, [split][rows][cols], added in order into c.out
 void add_parts(int dtype, const void* parts, int splits, int cols, const Call& c, hipStream_t st);

@@ -54,9 +54,43 @@ size_t operand_bytes(const poetx_grouped_desc* d) {
   const size_t codes = align256(grouped::codes_workspace_bytes(d)), values = dequantised_bytes(d) + rounded_bytes(d);
   return codes > values ? codes : values;
 }
-// 8-bit X, as values
-size_t held_bytes(const poetx_grouped_desc* d) { return align256((size_t)d->rows * d->d_in * esize(d->dtype)); }
-size_t workspace_bytes(const poetx_grouped_desc* d) { return d->rows == 0 ? 0 : d->flags & POETX_GROUPED_X_MX8 ? held_bytes(d) : operand_bytes(d) + parts_bytes(d); }
+// Weight gradient of an 8-bit X.  The workspace: X's values, in rows of whole vectors; dZ again in such rows, where its own have another length; then fp32 sums of a contraction that is
+// split among workgroups, or of gradients whose rows are no whole vectors.
+struct Held {
+  i64 ldx, lddz;      // lddz: 0 where dZ is taken as it is
+  size_t x, dz, sums;
+};
+grouped::Call held_call(const poetx_grouped_desc* d, const Held& h) {
+  grouped::Call c = {};
+  c.rows = d->rows;
+  c.m = d->d_in;
+  c.n = d->d_out;
+  c.groups = d->groups;
+  c.ld_in = h.ldx;
+  c.ld_in2 = h.lddz;
+  c.ld_out = d->d_in;
+  c.row_in = (int)h.ldx;
+  c.row_in2 = (int)h.lddz;
+  return c;
+}
+Held held_of(const poetx_grouped_desc* d) {
+  const size_t es = esize(d->dtype);
+  const i64 v = 16 / (i64)es;
+  Held h;
+  h.ldx = (d->d_in + v - 1) / v * v;
+  h.lddz = d->d_out % v ? (d->d_out + v - 1) / v * v : 0;
+  h.x = align256((size_t)d->rows * h.ldx * es);
+  h.dz = align256((size_t)d->rows * h.lddz * es);
+  const grouped::Call c = held_call(d, h);
+  h.sums = grouped::weight_stream_supported(d->dtype, c) ? align256(grouped::plan(d->dtype, grouped::WEIGHT, c, true, ~(size_t)0).parts) : 0;
+  return h;
+}
+size_t workspace_bytes(const poetx_grouped_desc* d) {
+  if (d->rows == 0) return 0;
+  if (!(d->flags & POETX_GROUPED_X_MX8)) return operand_bytes(d) + parts_bytes(d);
+  const Held h = held_of(d);
+  return h.x + h.dz + h.sums;
+}
 
 // A 4-bit weight's values, made in the workspace, for the products that do not decode it themselves.
 const void* dense_weight(const poetx_grouped_desc* d, const void* W, const int32_t* offsets, void* ws, hipStream_t st) {
@@ -200,9 +234,30 @@ int poetx_grouped_bwd_weight(const poetx_grouped_desc* d, const void* X, int64_t
     if (!enough(d, ws, ws_bytes)) return POETX_ERR_WORKSPACE;
     const size_t wb = workspace_bytes(d);
     if (overlap(ws, wb, X, xb) || overlap(ws, wb, dZ, zb) || overlap(ws, wb, dW, ob)) return POETX_ERR_INVALID_ARG;
-    StageTimer tm(POETX_STAGE_DEQUANT, st);
-    mx8_dequantize_launch(X, d->rows, d->d_in, d->dtype, ws, d->d_in, st, offsets, d->groups);
-    X = ws;
+    const Held h = held_of(d);
+    grouped::Call c = held_call(d, h);
+    c.in = ws;
+    c.in2 = dZ;
+    c.out = dW;
+    c.offsets = offsets;
+    c.accumulate = accumulate != 0;
+    const bool whole = ((uintptr_t)dZ & 15) == 0 && lddz % (16 / (i64)es) == 0;      // as its rows are, that is
+    {
+      StageTimer tm(POETX_STAGE_DEQUANT, st);
+      mx8_dequantize_launch(X, d->rows, d->d_in, d->dtype, ws, h.ldx, st, offsets, d->groups);
+      if (h.lddz) {
+        c.in2 = (char*)ws + h.x;
+        relay_rows_launch(d->dtype, dZ, d->rows, d->d_out, lddz, (char*)ws + h.x, h.lddz, st, offsets, d->groups);
+      } else {
+        c.ld_in2 = lddz;
+      }
+    }
+    StageTimer tm(POETX_STAGE_DENSE, st);
+    const bool streams = (h.lddz || whole) && grouped::weight_stream_supported(d->dtype, c) && ((uintptr_t)dW & 15) == 0;
+    const grouped::Plan p = grouped::plan(d->dtype, grouped::WEIGHT, c, streams, h.sums);
+    if (p.kernel >= grouped::STREAM_256) grouped::stream_launch(d->dtype, grouped::WEIGHT, p, c, (char*)ws + h.x + h.dz, st);
+    else grouped::edge_launch(d->dtype, grouped::WEIGHT, p.kernel, c, st);
+    return launch_status();
   }
   product(d, grouped::WEIGHT, grouped::Call{X, dZ, nullptr, dW, ldx, lddz, d->d_in, offsets, d->rows, d->d_in, d->d_out, d->groups, accumulate != 0}, nullptr, 0, st);
   return launch_status();

@@ -36,12 +36,14 @@ enum Elem { BF16, F32, CODES };
 // PARTS: fp32 sums of a range of the contraction go to `parts`, to be added up by another launch (bf16; fp32 needs no kernel of its own).
 // GATED: a gated block's forward or the recomputing half of its backward pass, as gated::Mode says; NOT_GATED otherwise.
 constexpr int NOT_GATED = gated::NONE;
-template <int BM_, int BN_, int NS_, Elem ELEM_, int PER_CU_ = 1, bool PARTS_ = false, int GATED_ = NOT_GATED>
+// NARROW: for any columns, strides and alignments of H, G, U and dH.  A switch inside the kernels cost those of whole vectors 2 to 5 %.
+template <int BM_, int BN_, int NS_, Elem ELEM_, int PER_CU_ = 1, bool PARTS_ = false, int GATED_ = NOT_GATED, bool NARROW_ = false>
 struct StreamTile {
   static constexpr int BM = BM_, BN = BN_, NS = NS_, NW = 4, PER_CU = PER_CU_;
   static constexpr Elem ELEM = ELEM_;
   static constexpr bool PARTS = PARTS_;
   static constexpr int GATED = GATED_;
+  static constexpr bool NARROW = NARROW_;
   static constexpr bool FP4 = ELEM == CODES;
   static constexpr int DEPTH = FP4 ? 128 : ELEM == F32 ? 16 : 32;      // elements of a stage
   static constexpr int SETS = 4, GROUPS = 64 * SETS;      // groups per lane, in all
@@ -69,9 +71,10 @@ struct StreamArgs {
   int rows, groups;
   int K;                  // FWD, INPUT: contraction, in elements (CODES: of whole units)
   int M, N;               // WEIGHT: rows of C (n); columns of C
+  int row_a, row_b;       // WEIGHT: elements that may be read of a row of A, of B (no less than M, N)
   int tiles_n;            // column tiles
   int accumulate;
-  int splits;             // FWD, INPUT: ranges of the contraction, whose sums go to [split][rows][N] at C; 1: the result does
+  int splits;             // ranges of the contraction, whose sums go to [split][rows][N] (WEIGHT: [split][group][M][N]) at C; 1: the result does
   gated::Out block;       // GATED: what is made of a tile; N: d_hidden, tiles_n: of so many columns (HOLD_MX8: rounded up to whole units)
 };
 
@@ -164,27 +167,60 @@ __device__ __forceinline__ void gated_tile(const StreamArgs& g, floatx4 (&acc)[C
 
   typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
   typedef std::conditional_t<FP32, u32x4, u32x2> Four;
+  typedef std::conditional_t<FP32, float, uint16_t> T;
+  typedef Four FourAt __attribute__((aligned(sizeof(T))));
   Four dh[2][MODE == gated::BWD ? P : 1];
   auto fetch = [&](int a) __attribute__((always_inline)) {      // dH of 16 rows, ahead of their turn
     const auto rd = md.here();
-    md.next();
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      const int col = 16 * p + 4 * q4, v = col < cols ? (li * (int)o.lddh + col) * ES : kNowhere;
-      if constexpr (FP32) dh[a & 1][p] = __builtin_amdgcn_raw_buffer_load_b128(rd, v, 0, 0);
-      else dh[a & 1][p] = __builtin_amdgcn_raw_buffer_load_b64(rd, v, 0, 0);
+      const int col = 16 * p + 4 * q4, at = (li * (int)o.lddh + col) * ES, v = col < cols ? at : kNowhere;
+      if constexpr (C::NARROW) {
+        const T* src = (const T*)md.at + (i64)li * o.lddh + col;
+        const int n = li < rows - 16 * a ? cols - col : 0;
+        Four f{};
+        if (n >= 4) {
+          f = *reinterpret_cast<const FourAt*>(src);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 3; ++i)
+            if (i < n) {
+              if constexpr (FP32) f[i] = __builtin_bit_cast(uint32_t, src[i]);
+              else f[i >> 1] |= (uint32_t)src[i] << (16 * (i & 1));
+            }
+        }
+        dh[a & 1][p] = f;
+      } else if constexpr (FP32) {
+        dh[a & 1][p] = __builtin_amdgcn_raw_buffer_load_b128(rd, v, 0, 0);
+      } else {
+        dh[a & 1][p] = __builtin_amdgcn_raw_buffer_load_b64(rd, v, 0, 0);
+      }
     }
+    md.next();
   };
   // bf16: 16 rows of a matrix at a time through LDS, an area each, so that every instruction writes whole lines (P = 4) or halves of them
   constexpr int AREA = 32 * 16 * P, CHUNKS = 2 * P;      // bytes; 16-byte chunks of a row
   auto place = [](int r, int ch) __attribute__((always_inline)) { return r * (16 * CHUNKS) + 16 * (ch ^ (P == 4 ? (r >> 1) & 7 : (r >> 2) & 3)); };
-  auto put = [&](int k, int p, const float (&z)[AT_ONCE][4], const Matrix& m, i64 ld) __attribute__((always_inline)) {
+  auto put = [&](int a, int k, int p, const float (&z)[AT_ONCE][4], const Matrix& m, i64 ld) __attribute__((always_inline)) {
     if constexpr (FP32) {
       const auto r = m.here();
 #pragma unroll
       for (int i = 0; i < AT_ONCE; ++i) {
         const int col = 16 * (p + i) + 4 * q4;
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, floatx4{z[i][0], z[i][1], z[i][2], z[i][3]}), r, col < cols ? (li * (int)ld + col) * 4 : kNowhere, 0, 0);
+        if constexpr (C::NARROW) {
+          float* to = (float*)m.at + (i64)li * ld + col;
+          const int n = li < rows - 16 * a ? cols - col : 0;
+          if (n >= 4) {
+            typedef floatx4 at4 __attribute__((aligned(4)));
+            *reinterpret_cast<at4*>(to) = floatx4{z[i][0], z[i][1], z[i][2], z[i][3]};
+          } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+              if (e < n) to[e] = z[i][e];
+          }
+        } else {
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, floatx4{z[i][0], z[i][1], z[i][2], z[i][3]}), r, col < cols ? (li * (int)ld + col) * 4 : kNowhere, 0, 0);
+        }
       }
     } else {
       uint32_t w[4];
@@ -192,14 +228,26 @@ __device__ __forceinline__ void gated_tile(const StreamArgs& g, floatx4 (&acc)[C
       *reinterpret_cast<u32x4*>(stg + k * AREA + place(li, (p + (q4 & 1)) * 2 + (q4 >> 1))) = u32x4{w[0], w[1], w[2], w[3]};
     }
   };
-  auto get = [&](int k, const Matrix& m, i64 ld) __attribute__((always_inline)) {
+  auto get = [&](int a, int k, const Matrix& m, i64 ld) __attribute__((always_inline)) {
     if constexpr (!FP32) {
       const auto rsrc = m.here();
 #pragma unroll
       for (int i = 0; i < P / 2; ++i) {
         const int r = lane / CHUNKS + (64 / CHUNKS) * i, ch = lane % CHUNKS, col = 8 * ch;
         const u32x4 w = *reinterpret_cast<const u32x4*>(stg + k * AREA + place(r, ch));
-        __builtin_amdgcn_raw_buffer_store_b128(w, rsrc, col < cols ? (r * (int)ld + col) * 2 : kNowhere, 0, 0);
+        if constexpr (C::NARROW) {
+          uint16_t* to = (uint16_t*)m.at + (i64)r * ld + col;
+          const int n = r < rows - 16 * a ? cols - col : 0;
+          if (n >= 8) {
+            *reinterpret_cast<edge::u32x4_a2*>(to) = w;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 7; ++e)
+              if (e < n) to[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+          }
+        } else {
+          __builtin_amdgcn_raw_buffer_store_b128(w, rsrc, col < cols ? (r * (int)ld + col) * 2 : kNowhere, 0, 0);
+        }
       }
     }
   };
@@ -255,11 +303,20 @@ __device__ __forceinline__ void gated_tile(const StreamArgs& g, floatx4 (&acc)[C
         ag = au = floatx4{0.f, 0.f, 0.f, 0.f};
       }
       if constexpr (MODE == gated::HOLD) {
-        put(1, p, x, mg, o.ldgu);
-        put(2, p, y, mu, o.ldgu);
+        put(a, 1, p, x, mg, o.ldgu);
+        put(a, 2, p, y, mu, o.ldgu);
       }
       if constexpr (MODE == gated::HOLD_MX8) {
         static_assert(MODE != gated::HOLD_MX8 || P % 2 == 0, "whole blocks of 32");
+        if constexpr (C::NARROW) {      // a lane's columns may end anywhere
+#pragma unroll
+          for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const bool in = 16 * (p + i) + 4 * q4 + e < cols;
+              x[i][e] = in ? x[i][e] : 0.f, y[i][e] = in ? y[i][e] : 0.f;
+            }
+        }
         quantise(x, p, dg[p], dg[p + 1], bg[p / 2]);
         quantise(y, p, du[p], du[p + 1], bu[p / 2]);
       }
@@ -280,18 +337,18 @@ __device__ __forceinline__ void gated_tile(const StreamArgs& g, floatx4 (&acc)[C
           }
         }
       if constexpr (MODE == gated::BWD) {
-        put(1, p, x, mg, o.ldgu);
-        put(2, p, y, mu, o.ldgu);
+        put(a, 1, p, x, mg, o.ldgu);
+        put(a, 2, p, y, mu, o.ldgu);
       }
-      if (with_h) put(0, p, h, mh, o.ldh);
+      if (with_h) put(a, 0, p, h, mh, o.ldh);
       __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (!FP32) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // this wave's own writes; the areas are private to it
-      if (with_h) get(0, mh, o.ldh);
+      if (with_h) get(a, 0, mh, o.ldh);
       if constexpr (PAIR) {
-        get(1, mg, o.ldgu);
-        get(2, mu, o.ldgu);
+        get(a, 1, mg, o.ldgu);
+        get(a, 2, mu, o.ldgu);
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // read back before the areas are rewritten
     }
@@ -359,7 +416,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
   }
   const int tiles_m = DIR == WEIGHT ? (g.M + BM - 1) / BM : row_tiles;      // WEIGHT: of one group
   const int per_weight = tiles_m * g.tiles_n;
-  const int T = per_weight * (DIR == WEIGHT ? g.groups : g.splits);
+  const int T = per_weight * (DIR == WEIGHT ? g.groups : 1) * g.splits;
   const int G = gridDim.x;
   // WEIGHT: a group's tiles take as long as it has rows.  Groups go by their size, the largest first, and workgroups through every other round backwards, so that their shares are
   // alike: 8192 rows, 15 of 16 groups of 1376 x 2048 that have 340 to 1200 of them each, 76 us as they come, 71 so.  Over many rounds shares are alike anyway (12 of 64 groups: 137, 139).
@@ -388,6 +445,10 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
     int u = ti * G + place(ti);
     w.gr = w.split = 0;
     if (DIR == WEIGHT) {
+      if (g.splits > 1) {
+        w.split = u / (per_weight * g.groups);
+        u -= w.split * (per_weight * g.groups);
+      }
       w.gr = u / per_weight;
       u -= w.gr * per_weight;
       if (by_size) w.gr = __builtin_ctzll(__ballot(tsum[0] == w.gr));
@@ -409,8 +470,13 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
           w.r0 = __builtin_amdgcn_readlane(tr0[q], w.gr & 63);
           w.r1 = __builtin_amdgcn_readlane(tr1[q], w.gr & 63);
         }
+      const int pairs = (w.r1 - w.r0 + 2 * DEPTH - 1) / (2 * DEPTH);
       w.k0 = 0;
-      w.k1 = (w.r1 - w.r0 + 2 * DEPTH - 1) / (2 * DEPTH) * 2;
+      w.k1 = pairs * 2;
+      if (g.splits > 1) {
+        w.k0 = pairs * w.split / g.splits * 2;
+        w.k1 = pairs * (w.split + 1) / g.splits * 2;
+      }
     } else {
       bool found = false;
 #pragma unroll
@@ -489,7 +555,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
       ++iti;
       if (iti >= n_my) break;
       w = locate(iti);
-    } while (DIR == WEIGHT && w.k1 == 0);
+    } while (DIR == WEIGHT && w.k1 == w.k0);
     Feed<LeftA> na{0, 0};      // nothing more: empty descriptors
     Feed<LeftB> nb{0, 0};
     int k0 = 0, k1 = 0x7fffffff, ha = 0, hb = 0;
@@ -501,9 +567,9 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
       if (DIR == WEIGHT) {
         const i64 len = w.r1 - w.r0;
         na.at = (uint64_t)(g.A + (i64)w.r0 * g.lda + ES * w.i0);
-        na.left = (len - 1) * (i64)g.lda + ES * (i64)(g.M - w.i0);
+        na.left = (len - 1) * (i64)g.lda + ES * (i64)(g.row_a - w.i0);
         nb.at = (uint64_t)(g.B + (i64)w.r0 * g.ldb + ES * w.j0);
-        nb.left = (len - 1) * (i64)g.ldb + ES * (i64)(g.N - w.j0);
+        nb.left = (len - 1) * (i64)g.ldb + ES * (i64)(g.row_b - w.j0);
       } else {
         ha = w.r1 - w.r0 < BM ? w.r1 - w.r0 : BM;
         const int row = FP4 ? g.K / 2 : ES * g.K;      // bytes of a row
@@ -521,9 +587,9 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
         }
       }
     }
-    if (DIR != WEIGHT) {
-      na.step(k0 * stepA);
-      nb.step(k0 * stepB);
+    na.step(k0 * stepA);
+    nb.step(k0 * stepB);
+    if (FP4) {
       nsa += (i64)k0 * g.sa_step;
       nsb += (i64)k0 * g.sb_step;
     }
@@ -725,7 +791,7 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
       } else if constexpr (DIR == WEIGHT || FP32 || C::PARTS) {
         // a lane's four columns of a row
         const int row = wm * (BM / 2) + li, col = wn * (BN / 2) + 4 * q4, rows = DIR == WEIGHT ? g.M - w.i0 : w.r1 - w.r0, cols = g.N - w.j0;
-        const i64 first = DIR == WEIGHT ? ((i64)w.gr * g.M + w.i0) * g.ldc : ((i64)w.split * g.rows + w.r0) * g.ldc;
+        const i64 first = DIR == WEIGHT ? (((i64)w.split * g.groups + w.gr) * g.M + w.i0) * g.ldc : ((i64)w.split * g.rows + w.r0) * g.ldc;
         const auto rc = make_rsrc((float*)g.C + first + w.j0, ((i64)(rows - 1) * g.ldc + cols) * 4);
         auto store = [&](auto ADD) __attribute__((always_inline)) {
 #pragma unroll

@@ -72,6 +72,25 @@ __global__ __launch_bounds__(256) void add_parts_kernel(const float* __restrict_
     *reinterpret_cast<u32x2*>(o) = u32x2{mm::pack2_bf16(sum[0], sum[1]), mm::pack2_bf16(sum[2], sum[3])};
   }
 }
+// The same of weight gradients, matrices of m columns one after the other; rows of the sums are whole vectors.
+__global__ __launch_bounds__(256) void add_weights_kernel(const floatx4* __restrict__ parts, int splits, i64 vectors, int m, float* __restrict__ out, int accumulate, int block0) {
+  const i64 i = (block0 + (i64)blockIdx.x) * 256 + threadIdx.x;
+  if (i >= vectors) return;
+  floatx4 sum = parts[i];
+  for (int s = 1; s < splits; ++s) sum += parts[i + s * vectors];
+  if (m % 4 == 0) {
+    floatx4* o = reinterpret_cast<floatx4*>(out) + i;
+    if (accumulate) sum += *o;
+    *o = sum;
+    return;
+  }
+  const int across = (m + 3) / 4;
+  const i64 row = i / across;
+  const int col = (int)(i - row * across) * 4;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (col + e < m) out[row * m + col + e] = accumulate ? out[row * m + col + e] + sum[e] : sum[e];
+}
 template <class T>
 void add(const float* parts, int splits, int cols, const Call& c, hipStream_t st) {
   const i64 waves = c.rows * ((cols + 255) / 256);
@@ -94,6 +113,13 @@ bool stream_supported(int dtype, Dir dir, const Call& c) {
   return c.groups <= Tile256::GROUPS && c.m % v == 0 && c.n % v == 0 && c.ld_in % v == 0 && c.ld_out % v == 0 && aligned16(c.in) && aligned16(c.out) &&
          c.ld_in < wide && c.ld_out < wide && c.m < wide / 2 &&
          (dir == WEIGHT ? c.ld_in2 % v == 0 && aligned16(c.in2) && c.ld_in2 < wide : aligned16(c.w));
+}
+
+bool weight_stream_supported(int dtype, const Call& c) {
+  const int es = dtype == POETX_F32 ? 4 : 2, v = 16 / es;
+  const i64 wide = (1ll << 31) / (es * 256);
+  return c.groups <= Tile256::GROUPS && c.ld_in % v == 0 && c.ld_in2 % v == 0 && (c.m % v == 0 || c.row_in >= (c.m + v - 1) / v * v) && (c.n % v == 0 || c.row_in2 >= (c.n + v - 1) / v * v) &&
+         c.ld_in < wide && c.ld_in2 < wide && c.ld_out < wide && c.m < wide / 2;
 }
 
 // The figures were fitted to 650 calls in bf16 and 700 in fp32 of random directions, sizes (64 to 14336; 64 to 4096), groups (1 to 128) and rows (1 to 32768; 8 to 8192), each
@@ -127,17 +153,20 @@ Plan plan(int dtype, Dir dir, const Call& c, bool streams, size_t scratch) {
     const double tiles = tiles_of(dir, c.rows, c.m, c.n, c.groups, r.h, r.w), stages = (double)(i64)((K + r.depth - 1) / r.depth);
     const double stage = r.stage * (dir == FWD && stream && r.kernel != STREAM_256 ? 0.9 : 1.0);      // bf16: whole lines; fp32: the fewest instructions beside the multiplications
     // few tiles: their contraction in ranges, whose fp32 sums are added by another launch (7.5 us with the wait between the two, and their way through the caches)
-    const bool splittable = dir != WEIGHT && (r.kernel == STREAM_128 || r.kernel >= SINGLE_128);
+    const bool splittable = dir == WEIGHT ? stream : r.kernel == STREAM_128 || r.kernel >= SINGLE_128;
     for (const int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
-      const size_t parts = splits > 1 ? (size_t)splits * c.rows * out_cols * sizeof(float) : 0;
+      // a weight gradient whose rows are no whole vectors goes by way of the scratch in any case
+      const bool through = splits > 1 || (stream && dir == WEIGHT && c.m % 4 != 0);
+      const size_t parts = through ? (size_t)splits * (dir == WEIGHT ? (i64)c.groups * c.n : c.rows) * ((out_cols + 3) / 4 * 4) * sizeof(float) : 0;
+      if (splits == 1 && parts > scratch) break;
       if (splits > 1 && (!splittable || parts > scratch || 4 * splits > stages || tiles * splits > 2 * r.at_once)) break;
       double us = tiles * splits / r.at_once;
       if (stream && !f) us = c.groups == 1 ? (double)(i64)(us + 0.999) : us + r.uneven;
       us = (us < 1 ? 1 : us) * (double)(i64)((stages + splits - 1) / splits) * stage;
       // a stream stores between multiplications; the others have several workgroups on a CU, but store less well
       const double stores = (f ? 1.5 : 1.35) * out_us;
-      us = r.rest + (stream ? us + out_us : us > stores ? us : stores);
-      if (splits > 1) us += 7.5 + 2 * parts / 8e6;
+      us = r.rest + (stream ? us + splits * out_us : us > stores ? us : stores);
+      if (through) us += 7.5 + (dir == WEIGHT ? parts / 8e6 + out_us : 2 * parts / 8e6);
       if (us < best.us) best = Plan{r.kernel, splits, parts, us};
     }
   }
@@ -162,7 +191,20 @@ void stream_launch(int dtype, Dir dir, const Plan& p, const Call& c, void* scrat
     a.ldb = (int)(es * c.ld_in);
     a.M = c.n;
     a.N = c.m;
-    return pick<WEIGHT>(k, a, st);
+    a.row_a = c.row_in2 > c.n ? c.row_in2 : c.n;
+    a.row_b = c.row_in > c.m ? c.row_in : c.m;
+    if (!p.parts) return pick<WEIGHT>(k, a, st);
+    const int ld = (c.m + 3) / 4 * 4;
+    a.C = scratch;
+    a.ldc = ld;
+    a.N = ld <= a.row_b ? ld : c.m;
+    a.accumulate = 0;
+    pick<WEIGHT>(k, a, st);
+    const i64 vectors = (i64)c.groups * c.n * (ld / 4);
+    launch_in_rows((vectors + 255) / 256, [&](int block0, unsigned count) {
+      hipLaunchKernelGGL(add_weights_kernel, dim3(count), dim3(256), 0, st, (const floatx4*)scratch, p.splits, vectors, c.m, (float*)c.out, c.accumulate, block0);
+    });
+    return;
   }
   a.A = (const char*)c.in;
   a.lda = (int)(es * c.ld_in);

@@ -326,19 +326,19 @@ grouped::Call product_of(const void* X, i64 ldx, const void* W, const int32_t* o
 }  // namespace
 
 bool values_supported(const Call& c) {
-  return c.m % 8 == 0 && c.n % 8 == 0 && c.ldx % 8 == 0 && ((uintptr_t)c.X & 15) == 0 && c.ldx < (1 << 22) && c.m < (1 << 22) &&
+  return c.m % 8 == 0 && c.ldx % 8 == 0 && ((uintptr_t)c.X & 15) == 0 && c.ldx < (1 << 22) && c.m < (1 << 22) &&
          ((i64)c.n + 256) * mx4::units(c.m) * 64 < (1ll << 31);
 }
 size_t values_parts_bytes(int m, int n, int groups, i64 rows, bool few, size_t scratch) {
   const poetx_grouped_desc d = twice(m, n, groups, rows);
-  const grouped::ValuesPlan p = grouped::values_plan(&d, product_of(nullptr, m, nullptr, nullptr, rows, m, n, groups), few, true, ~(size_t)0, scratch);
+  const grouped::ValuesPlan p = grouped::values_plan(&d, product_of(nullptr, m, nullptr, nullptr, rows, m, n, groups), few, true, n % 2 == 0 ? ~(size_t)0 : 0, scratch);      // sums are stored in whole vectors
   return p.better && p.ranges > 1 ? (size_t)p.ranges * rows * 2 * n * sizeof(float) : 0;
 }
 // The choice is that of a product of 2n columns: the tiles, the contraction and the bytes of the weight are the same.
 bool values_launch(const Call& c, bool few, void* sums, size_t sums_bytes, size_t scratch, hipStream_t st) {
   using grouped::go;
   const poetx_grouped_desc d = twice(c.m, c.n, c.groups, c.rows);
-  const grouped::ValuesPlan p = grouped::values_plan(&d, product_of(c.X, c.ldx, c.W, c.offsets, c.rows, c.m, c.n, c.groups), few, true, sums_bytes, scratch);
+  const grouped::ValuesPlan p = grouped::values_plan(&d, product_of(c.X, c.ldx, c.W, c.offsets, c.rows, c.m, c.n, c.groups), few, true, c.n % 2 == 0 ? sums_bytes : 0, scratch);
   if (!p.better) return false;
   const mx4::View w = mx4::view(c.W, 2 * (i64)c.groups * c.n, c.m);
   grouped::ValuesArgs a{(const uint16_t*)c.X, c.ldx, w.codes, w.scales, nullptr, 0, c.offsets, c.rows, c.m, c.n, c.groups, mx4::units(c.m), 0, p.ranges, (float*)sums, c.out};

@@ -68,7 +68,27 @@ __global__ __launch_bounds__(256) void mx8_dequantize_kernel(mx8::View q, int co
   }
 }
 
+// Rows of whole vectors from rows of any length and alignment: a vector a lane, zeros past the columns.
+template <class T>
+__global__ __launch_bounds__(256) void relay_rows_kernel(const T* __restrict__ X, i64 ld, int cols, i64 rows, T* __restrict__ out, i64 ldo, int block0, const int32_t* offsets, int groups) {
+  constexpr int V = 16 / sizeof(T);
+  const i64 across = ldo / V, i = (block0 + (i64)blockIdx.x) * 256 + threadIdx.x, row = i / across;
+  const int col = (int)(i - row * across) * V;
+  const i64 r0 = grouped::offset_at(offsets, 0, rows), r1 = grouped::furthest_end(offsets, groups, rows);
+  if (row < r0 || row >= r1) return;
+  *reinterpret_cast<edge::u32x4*>(out + row * ldo + col) = edge::load_branched(X + row * ld, col, cols, true);
+}
+
 }  // namespace
+
+void relay_rows_launch(int dtype, const void* X, i64 rows, int cols, i64 ld, void* out, i64 ldo, hipStream_t st, const int32_t* offsets, int groups) {
+  auto go = [&](auto* x, auto* o) {
+    launch_in_rows((rows * (ldo * (i64)sizeof(*o) / 16) + 255) / 256, [&](int block0, unsigned count) {
+      hipLaunchKernelGGL(relay_rows_kernel, dim3(count), dim3(256), 0, st, x, ld, cols, rows, o, ldo, block0, offsets, groups);
+    });
+  };
+  dtype == POETX_F32 ? go((const float*)X, (float*)out) : go((const uint16_t*)X, (uint16_t*)out);
+}
 
 void mx8_quantize_launch(int dtype, const void* X, i64 rows, int cols, i64 ld, void* Q, hipStream_t st) {
   const int upr = mx8::units(cols);

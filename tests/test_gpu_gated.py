@@ -346,6 +346,20 @@ def test_gated_mx4_strides(lib, pads, shift, before, extra):
     run_all([17, 0, 150, 3], 136, 200, "bf16", weight="mx4", pads=pads, shift=shift, before=before, extra=extra)
 
 
+# Enough tiles for the streams, and contractions for them to be split, of whole vectors and of others.
+LARGE = [
+    # counts, m, n, pads (of X, of the rest)
+    ([4096], 256, 2048, (0, 0)), ([4095], 264, 2047, (8, 3)), ([2048, 0, 2040], 136, 1030, (0, 0)), ([1000, 24], 320, 1280, (0, 8)), ([1023], 512, 1022, (0, 1)),
+    ([130] * 9, 192, 257, (0, 0)), ([700, 0, 333], 2048, 72, (0, 0)), ([515], 4096, 66, (0, 0)), ([300], 3336, 129, (0, 0)), ([90] * 24, 128, 384, (0, 0)),
+]
+
+
+@pytest.mark.parametrize("dtype,act,weight", [("bf16", "gelu", "dense"), ("bf16", "silu", "mx4"), ("f32", "silu", "dense")])
+@pytest.mark.parametrize("counts,m,n,pads", LARGE)
+def test_gated_large(lib, counts, m, n, pads, dtype, act, weight):
+    run_all(counts, m, n, dtype, act, weight, pads=pads, before=3, extra=5)
+
+
 @pytest.mark.parametrize("held", ["same", "mx8"])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("act", ["silu", "gelu"])
@@ -440,7 +454,9 @@ def test_gated_offsets_out_of_range(lib):
 # ------------------------------------------------------------------------------------ the weight gradient of 8-bit rows
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("counts,m,n,before,extra", [([1], 1, 1, 0, 0), ([0], 8, 8, 0, 0), ([3], 7, 5, 1, 2), ([5, 1, 0, 130, 64], 64, 96, 0, 3), ([300, 0, 1, 211], 256, 320, 0, 0),
-                                                     ([31, 33, 32], 100, 60, 40, 0), ([1] * 70, 64, 64, 0, 0), ([513], 1408, 264, 0, 130), ([128, 129], 136, 200, 8, 8)])
+                                                     ([31, 33, 32], 100, 60, 40, 0), ([1] * 70, 64, 64, 0, 0), ([513], 1408, 264, 0, 130), ([128, 129], 136, 200, 8, 8),
+                                                     ([4598], 384, 480, 0, 1), ([3000, 0, 2001], 257, 263, 5, 0), ([2500], 1030, 1001, 0, 0), ([700, 650], 1026, 1032, 1, 1),
+                                                     ([900] * 3, 1032, 1035, 0, 0), ([1100], 2048, 2050, 0, 0), ([8000], 129, 130, 0, 0)])
 def test_weight_gradient_of_mx8_rows(lib, counts, m, n, before, extra, dtype):
     rng = np.random.default_rng(m + n)
     G, live, dt = len(counts), sum(counts), DT[dtype]
