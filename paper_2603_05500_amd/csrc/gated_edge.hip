@@ -130,11 +130,11 @@ void go(const Call& c, hipStream_t st) {
 template <class T, Mode MODE>
 void pick(grouped::Kernel k, const Call& c, hipStream_t st) {
   constexpr int D = 128 / (int)sizeof(T);
-  if (k == grouped::EDGE_128) go<T, 128, 128, D, 2, 2, 4, MODE>(c, st);
-  else if constexpr (MODE == HOLD_MX8) go<T, 32, 64, 2 * D, 1, 1, 4, MODE>(c, st);
-  else if (k == grouped::EDGE_64) go<T, 64, 64, D, 2, 2, 4, MODE>(c, st);
+  // EDGE_128 is not among what plan() gives a forward product.  HOLD_MX8: a wave's columns are whole blocks
+  if constexpr (MODE == HOLD_MX8) k == grouped::EDGE_64 ? go<T, 64, 64, D, 2, 1, 4, MODE>(c, st) : go<T, 32, 64, 2 * D, 1, 1, 4, MODE>(c, st);
   else if (k == grouped::EDGE_32) go<T, 32, 32, 2 * D, 1, 1, 4, MODE>(c, st);
-  else go<T, 32, 32, 8 * D, 1, 1, 16, MODE>(c, st);
+  else if (k == grouped::EDGE_32_DEEP) go<T, 32, 32, 8 * D, 1, 1, 16, MODE>(c, st);
+  else go<T, 64, 64, D, 2, 2, 4, MODE>(c, st);
 }
 
 }  // namespace

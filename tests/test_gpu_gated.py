@@ -360,6 +360,22 @@ def test_gated_large(lib, counts, m, n, pads, dtype, act, weight):
     run_all(counts, m, n, dtype, act, weight, pads=pads, before=3, extra=5)
 
 
+# One for every kernel that these lists do not reach, 8 more rows than the groups have counting: tiles of 256 x 256 and 128 x 128 and contractions in ranges, of whole vectors and not; a 4-bit
+# weight decoded in ranges, on the largest tile, for a handful of rows, and written out first; fp32 tiles of 128 x 128.
+PATHS = [
+    ([2992], 136, 2056, "bf16", "dense"), ([2992], 520, 520, "bf16", "dense"), ([5992], 136, 1001, "bf16", "dense"), ([2000, 80, 2000], 136, 1032, "bf16", "dense"),
+    ([92], 4104, 1032, "bf16", "dense"), ([192], 2056, 2100, "bf16", "dense"), ([1000, 1040], 4104, 66, "bf16", "dense"), ([292], 65, 1001, "bf16", "dense"),
+    ([32], 4104, 2056, "bf16", "mx4"), ([1092, 1900], 6152, 130, "bf16", "mx4"), ([3000, 0, 2992], 264, 1001, "bf16", "mx4"), ([120], 65, 8192, "bf16", "mx4"),
+    ([8], 64, 6200, "bf16", "mx4"), ([5992], 136, 2056, "bf16", "mx4"), ([1500, 1492], 65, 130, "bf16", "mx4"),
+    ([1492], 2056, 2100, "f32", "dense"), ([700, 1348], 2056, 72, "f32", "dense"), ([292], 1032, 1032, "f32", "dense"), ([2992], 65, 130, "f32", "dense"),
+]
+
+
+@pytest.mark.parametrize("counts,m,n,dtype,weight", PATHS)
+def test_gated_on_every_kernel(lib, counts, m, n, dtype, weight):
+    run_all(counts, m, n, dtype, "silu" if n % 2 else "gelu", weight, before=3, extra=5)
+
+
 @pytest.mark.parametrize("held", ["same", "mx8"])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("act", ["silu", "gelu"])
@@ -456,7 +472,8 @@ def test_gated_offsets_out_of_range(lib):
 @pytest.mark.parametrize("counts,m,n,before,extra", [([1], 1, 1, 0, 0), ([0], 8, 8, 0, 0), ([3], 7, 5, 1, 2), ([5, 1, 0, 130, 64], 64, 96, 0, 3), ([300, 0, 1, 211], 256, 320, 0, 0),
                                                      ([31, 33, 32], 100, 60, 40, 0), ([1] * 70, 64, 64, 0, 0), ([513], 1408, 264, 0, 130), ([128, 129], 136, 200, 8, 8),
                                                      ([4598], 384, 480, 0, 1), ([3000, 0, 2001], 257, 263, 5, 0), ([2500], 1030, 1001, 0, 0), ([700, 650], 1026, 1032, 1, 1),
-                                                     ([900] * 3, 1032, 1035, 0, 0), ([1100], 2048, 2050, 0, 0), ([8000], 129, 130, 0, 0)])
+                                                     ([900] * 3, 1032, 1035, 0, 0), ([1100], 2048, 2050, 0, 0), ([8000], 129, 130, 0, 0),
+                                                     ([4000, 3999], 1032, 136, 1, 0), ([4001], 2056, 4104, 0, 0)])
 def test_weight_gradient_of_mx8_rows(lib, counts, m, n, before, extra, dtype):
     rng = np.random.default_rng(m + n)
     G, live, dt = len(counts), sum(counts), DT[dtype]
