@@ -3,8 +3,9 @@
     python examples/experts.py                      # experts in four bits, activations in bf16
     python examples/experts.py --activations mx4    # activations of the forward products in four bits as well
     python examples/experts.py --weights dense      # experts that are trained themselves: weight gradients too
+    python examples/experts.py --expert gated       # gated experts; --held mx8 keeps their activations in eight bits
 
-Each expert is y = W2 relu(W1 x)^2.  Its base weights carry orthogonal factors (blocks of a Cayley-Neumann series under a
+Each expert is y = W2 relu(W1 x)^2, or gated y = W2 (silu(Wg x) * Wu x).  Its base weights carry orthogonal factors (blocks of a Cayley-Neumann series under a
 permutation; random here), which are folded in once, as in the outer loop's merge step, and not trained any further; frozen
 experts are then kept in four bits, and gradients go to the inputs and the router's shares.  A router gives every token its experts; tokens are put in the experts' order on the device, and the products of all
 experts are one launch each, whatever the router says: no group size ever comes to the host.
@@ -92,10 +93,7 @@ class Experts:
         self.choice = at.clamp(min=0)
         self.token = self.choice // self.top_k
         self.gate = gates.reshape(-1)[self.choice].unsqueeze(1) * self.live
-        self.x = x[self.token]
-        self.h = self.up.forward(self.x, self.offsets)
-        self.a = self.h.clamp(min=0) ** 2
-        self.y = self.down.forward(self.a, self.offsets)
+        self.y = self.down.forward(self.hidden(x[self.token]), self.offsets)
         return torch.zeros_like(x, dtype=torch.float32).index_add_(0, self.token, self.y.float() * self.gate)
 
     def backward(self, dout, weights=False):
@@ -103,10 +101,72 @@ class Experts:
         d = dout[self.token]
         dgate = torch.zeros(len(self.choice), device="cuda").index_add_(0, self.choice, ((d * self.y.float()).sum(1, keepdim=True) * self.live).squeeze(1))
         dy = (d * self.gate).to(self.y.dtype)
-        dh = self.down.input_gradient(dy, self.offsets) * (2 * self.h.clamp(min=0))
+        dh = self.hidden_gradient(self.down.input_gradient(dy, self.offsets))
         dx = torch.zeros_like(dout).index_add_(0, self.token, self.up.input_gradient(dh, self.offsets).float() * self.live)
-        dW = (self.up.weight_gradient(self.x, dh, self.offsets), self.down.weight_gradient(self.a, dy, self.offsets)) if weights else None
+        dW = (self.first_weight_gradient(dh), self.down.weight_gradient(self.a, dy, self.offsets)) if weights else None
         return dx, dgate.view(-1, self.top_k), dW
+
+    def hidden(self, x):
+        """The rows that the second product takes."""
+        self.x, self.h = x, self.up.forward(x, self.offsets)
+        self.a = self.h.clamp(min=0) ** 2
+        return self.a
+
+    def hidden_gradient(self, da):
+        return da * (2 * self.h.clamp(min=0))
+
+    def first_weight_gradient(self, dh):
+        return self.up.weight_gradient(self.x, dh, self.offsets)
+
+
+class GatedExperts(Experts):
+    """W1 is Wg above Wu.  What the backward pass needs of the forward is kept in the type, in eight bits (held="mx8") or, but for x, not at all ("nothing")."""
+
+    def __init__(self, W1, W2, tokens, top_k, mx4=False, held="same"):
+        super().__init__(W1, W2, tokens, top_k, mx4)
+        groups, n2, m = W1.shape
+        self.n, self.m, self.rows, self.dtype, self.held = n2 // 2, m, tokens * top_k, W1.dtype, held
+        flags = (px.GATED_W_MX4 if mx4 else 0) | (px.GATED_HELD_MX8 if held == "mx8" else 0)
+        self.block = px.make_gated_desc(m, self.n, groups, self.rows, px.dtype_code(W1), px.GATED_SILU, flags)
+        self.block_ws = _scratch(px.poetx_gated_workspace_bytes(self.block))
+        self.x8 = px.make_grouped_desc(m, n2, groups, self.rows, px.dtype_code(W1), px.GROUPED_X_MX8)
+        if not mx4 and held == "mx8":
+            self.x8_ws = _scratch(px.poetx_grouped_workspace_bytes(self.x8))
+
+    def _matrix(self, d):
+        return torch.zeros((self.rows, d), dtype=self.dtype, device="cuda")      # rows of no expert stay zero
+
+    def _kept(self, d):
+        return _scratch(px.poetx_mx8_bytes(self.rows, d)) if self.held == "mx8" else torch.empty((self.rows, d), dtype=self.dtype, device="cuda")
+
+    def hidden(self, x):
+        self.a, self.x = self._matrix(self.n), x
+        self.G, self.U = (None, None) if self.held == "nothing" else (self._kept(self.n), self._kept(self.n))
+        px.poetx_gated_fwd(self.block, x, self.up.W, self.offsets, self.a, self.G, self.U, self.block_ws)
+        a = self.a
+        if self.held != "same":
+            self.a = None                              # made again in the backward pass
+        if self.held == "mx8":
+            self.x = self._kept(self.m)
+            px.poetx_mx8_quantize(x, self.x)
+        return a
+
+    def hidden_gradient(self, da):
+        dGU, a = self._matrix(2 * self.n), self._matrix(self.n)
+        dG, dU = dGU[:, : self.n], dGU[:, self.n:]
+        if self.held == "nothing":
+            px.poetx_gated_bwd_recompute(self.block, da, self.x, self.up.W, self.offsets, dG, dU, a, self.block_ws)
+        else:
+            px.poetx_gated_bwd(self.block, da, self.G, self.U, self.offsets, dG, dU, a)
+        self.a = a
+        return dGU
+
+    def first_weight_gradient(self, dh):
+        if self.held != "mx8":
+            return super().first_weight_gradient(dh)
+        dW = torch.empty(self.up.W.shape, device="cuda")
+        px.poetx_grouped_bwd_weight(self.x8, self.x, dh, self.offsets, dW, False, self.x8_ws)
+        return dW
 
 
 def main(argv=None):
@@ -119,14 +179,21 @@ def main(argv=None):
     ap.add_argument("--block", type=int, default=128)
     ap.add_argument("--weights", choices=("mx4", "dense"), default="mx4")
     ap.add_argument("--activations", choices=("same", "mx4"), default="same")
+    ap.add_argument("--expert", choices=("plain", "gated"), default="plain")
+    ap.add_argument("--held", choices=("same", "mx8", "nothing"), default="same")
     ap.add_argument("--steps", type=int, default=10)
     a = ap.parse_args(argv)
     if a.activations == "mx4" and a.weights != "mx4":
         ap.error("activations in four bits need weights in four bits")
+    if a.expert == "gated" and a.activations != "same":
+        ap.error("gated experts take activations in bf16")
+    if a.expert != "gated" and a.held != "same":
+        ap.error("--held is of gated experts")
     gen = torch.Generator(device="cuda").manual_seed(0)
     W1, W2 = (torch.stack([merged((torch.randn(s, device="cuda", generator=gen) * 0.02).bfloat16(), a.block, 4, 0.01, gen) for _ in range(a.experts)])
-              for s in ((a.hidden, a.d), (a.d, a.hidden)))
-    layer = Experts(W1, W2, a.tokens, a.top_k, a.weights == "mx4", a.activations == "mx4")
+              for s in ((a.hidden * (2 if a.expert == "gated" else 1), a.d), (a.d, a.hidden)))
+    mx4 = a.weights == "mx4"
+    layer = GatedExperts(W1, W2, a.tokens, a.top_k, mx4, a.held) if a.expert == "gated" else Experts(W1, W2, a.tokens, a.top_k, mx4, a.activations == "mx4")
     router = torch.randn((a.d, a.experts), device="cuda", generator=gen) / a.d ** 0.5
     x = torch.randn((a.tokens, a.d), device="cuda", generator=gen).bfloat16()
     target = torch.randn((a.tokens, a.d), device="cuda", generator=gen) * 0.05
@@ -145,7 +212,7 @@ def main(argv=None):
     torch.cuda.synchronize()
     ms = (time.perf_counter() - t) / a.steps * 1e3
     finite = all(bool(torch.isfinite(v).all()) for v in (out, grads[0], grads[1], *(grads[2] or ())))
-    print(f"{a.tokens} tokens, {a.top_k} of {a.experts} experts of {a.hidden} x {a.d}, weights {a.weights}, activations {a.activations}: "
+    print(f"{a.tokens} tokens, {a.top_k} of {a.experts} experts of {a.hidden} x {a.d}, weights {a.weights}, activations {a.activations}{', gated, held ' + a.held if a.expert == 'gated' else ''}: "
           f"loss {float(((out - target) ** 2).mean()):.5f}, {ms:.2f} ms per forward and backward, {'finite' if finite else 'NOT FINITE'}")
     return 0 if finite else 1
 

@@ -85,10 +85,10 @@ void products(const poetx_gated_desc* d, const void* X, i64 ldx, const void* W, 
   const bool handful = few(d, !four ? grouped::DENSE_WEIGHT : streamed ? grouped::VALUES_STREAMED_MX4 : grouped::VALUES_MX4);
   const Scratch s = scratch_of(d);
   void* sums = (char*)ws + s.weight;
-  {
+  if (streamed && gated::values_launch(q, handful, sums, s.sums, s.sums, st)) return;
+  if (handful) {
     StageTimer tm(POETX_STAGE_DENSE, st);
-    if (streamed && gated::values_launch(q, handful, sums, s.sums, s.sums, st)) return;
-    if (handful) return gated::few_launch(d->dtype, four, q, st);
+    return gated::few_launch(d->dtype, four, q, st);
   }
   if (four) {
     StageTimer tm(POETX_STAGE_DEQUANT, st);

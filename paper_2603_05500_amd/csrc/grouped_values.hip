@@ -340,6 +340,7 @@ bool values_launch(const Call& c, bool few, void* sums, size_t sums_bytes, size_
   const poetx_grouped_desc d = twice(c.m, c.n, c.groups, c.rows);
   const grouped::ValuesPlan p = grouped::values_plan(&d, product_of(c.X, c.ldx, c.W, c.offsets, c.rows, c.m, c.n, c.groups), few, true, c.n % 2 == 0 ? sums_bytes : 0, scratch);
   if (!p.better) return false;
+  StageTimer tm(POETX_STAGE_DENSE, st);
   const mx4::View w = mx4::view(c.W, 2 * (i64)c.groups * c.n, c.m);
   grouped::ValuesArgs a{(const uint16_t*)c.X, c.ldx, w.codes, w.scales, nullptr, 0, c.offsets, c.rows, c.m, c.n, c.groups, mx4::units(c.m), 0, p.ranges, (float*)sums, c.out};
   if (p.ranges > 1) {

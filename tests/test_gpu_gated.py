@@ -501,6 +501,30 @@ def test_weight_gradient_of_mx8_rows(lib, counts, m, n, before, extra, dtype):
             assert (err <= k * ((q - p + 4) * U24 * mag + 2 * U24 * np.abs(ref)) + 1e-37).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,pad,shift,out_shift", [(136, 3, 0, 0), (136, 8, 1, 0), (136, 8, 0, 1), (131, 5, 3, 0), (131, 5, 0, 2)])
+def test_weight_gradient_of_mx8_rows_elsewhere(lib, n, pad, shift, out_shift, dtype):
+    """dZ and dW on any alignment, dZ of any leading dimension."""
+    rng = np.random.default_rng(n + pad)
+    counts, m, dt = [700, 0, 611], 260, DT[dtype]
+    rows, ends = sum(counts), np.r_[0, np.cumsum(counts)]
+    off = torch.tensor(ends, dtype=torch.int32, device="cuda")
+    dZ, _ = strided(rows, n, pad, dt, shift)
+    dZ.copy_(torch.from_numpy(rng.standard_normal((rows, n)) * 0.1).to(dt))
+    Q = mx8_of(torch.from_numpy(rng.standard_normal((rows, m))).to(dt).cuda())
+    xh, zh = mx8_values(*split_mx8(Q, rows, m), m), host(dZ).numpy()
+    desc = px.make_grouped_desc(m, n, 3, rows, CODE[dtype], px.GROUPED_X_MX8)
+    flat = torch.full((3 * n * m + 8,), 3.0, device="cuda")
+    dW = flat[out_shift: out_shift + 3 * n * m].view(3, n, m)
+    px.poetx_grouped_bwd_weight(desc, Q, dZ, off, dW, False, scratch(px.poetx_grouped_workspace_bytes(desc)))
+    for g in range(3):
+        p, q = ends[g], ends[g + 1]
+        ref, mag = zh[p:q].T @ xh[p:q], np.abs(zh[p:q]).T @ np.abs(xh[p:q])
+        assert (np.abs(host(dW[g]).numpy() - ref) <= (q - p + 4) * U24 * mag + 2 * U24 * np.abs(ref) + 1e-37).all()
+    dW.fill_(3.0)
+    assert bool((flat == 3.0).all())
+
+
 # ------------------------------------------------------------------------------------ together
 @pytest.mark.parametrize("dtype,act", [("bf16", "silu"), ("f32", "gelu")])
 def test_training_step(lib, dtype, act):
@@ -683,3 +707,69 @@ def test_rows_past_32_bits(lib):
     px.poetx_gated_bwd(desc, dHn, Gn, Un, b.off, dG, dU)
     px.poetx_gated_bwd(desc, dH, G, U, b.off, dGn, dUn)
     assert torch.equal(dGn, dG) and torch.equal(dUn, dU)
+
+
+def test_mx8_past_32_bits(lib):
+    """More than 2^31 elements: the last rows come back as the first."""
+    rows, cols = 33000, 65600
+    x = torch.randn((4, cols), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).bfloat16()
+    X = x.repeat(rows // 4, 1)
+    Q = torch.empty(px.poetx_mx8_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+    px.poetx_mx8_quantize(X, Q)
+    X.zero_()
+    px.poetx_mx8_dequantize(Q, X)
+    want = torch.from_numpy(mx8_values(*oracle_mx8(host(x).numpy()), cols)).to(torch.bfloat16).cuda()
+    assert torch.equal(X.view(rows // 4, 4, cols), want.expand(rows // 4, 4, cols))
+
+
+@pytest.mark.parametrize("activation", ["silu", "gelu"])
+def test_profiled_and_refused(lib, activation):
+    """Stage timing counts the block's launches; a tensor of another shape or type is refused by the binding."""
+    b = Block([20, 300], 128, 96, "bf16", activation)
+    desc = b.desc()
+    H, ws = torch.empty((b.rows, b.n), dtype=b.dt, device="cuda"), b.ws(desc)
+    px.poetx_profile_begin(16)
+    px.poetx_gated_fwd(desc, b.X, b.W, b.off, H, ws=ws)
+    stages = px.poetx_profile_end()
+    assert stages["dense"][1] == 1 and stages["dequant"][1] == 0
+    with pytest.raises(AssertionError):
+        px.poetx_gated_fwd(desc, b.X, b.W, b.off, H.float(), ws=ws)
+    with pytest.raises(AssertionError):
+        px.poetx_gated_fwd(desc, b.X[:, :64], b.W, b.off, H, ws=ws)
+    with pytest.raises(AssertionError):
+        px.poetx_gated_fwd(desc, b.X, b.W[:1], b.off, H, ws=ws)
+    with pytest.raises(px.PoetxError):
+        px.poetx_gated_fwd(desc, b.X, b.W, b.off, b.dH.new_empty(0).set_(b.X.untyped_storage(), 0, (b.rows, b.n), (b.m, 1)), ws=ws)
+
+
+@pytest.mark.parametrize("held", ["same", "nothing", "mx8"])
+def test_gated_experts_example(lib, held):
+    """The example layer of gated experts in fp32 against torch autograd in float64.  What is kept in eight bits moves gradients by up to 2^-6 of the largest of 32 elements, and act, act' and
+    their products by a few times that: a tenth of the largest gradient bounds it there."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "experts.py")
+    spec = importlib.util.spec_from_file_location("experts_example", path)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    tokens, d, f, E, k = 50, 64, 96, 5, 2
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    W1, W2 = (torch.stack([ex.merged(torch.randn(s, device="cuda", generator=gen) * 0.1, 16, 3, 0.02, gen) for _ in range(E)]) for s in ((2 * f, d), (d, f)))
+    x, dout = (torch.randn((tokens, d), device="cuda", generator=gen) for _ in range(2))
+    ids = torch.randint(-1, E, (tokens, k), device="cuda", generator=gen)
+    gates = torch.rand((tokens, k), device="cuda", generator=gen)
+    layer = ex.GatedExperts(W1, W2, tokens, k, held=held)
+    out = layer.forward(x, ids, gates)
+    dx, dgate, (dW1, dW2) = layer.backward(dout, weights=True)
+    leaves = [t.double().cpu().requires_grad_() for t in (x, gates, W1, W2)]
+    xr, gr, W1r, W2r = leaves
+    e = ids.cpu().clamp(min=0)
+    gu = (W1r[e] * xr[:, None, None, :]).sum(3)
+    h = torch.nn.functional.silu(gu[..., :f]) * gu[..., f:]
+    ref = ((W2r[e] * h[:, :, None, :]).sum(3) * (gr * (ids.cpu() >= 0)).unsqueeze(2)).sum(1)
+    ref.backward(dout.double().cpu())
+    for got, want, exact in ((out, ref, True), (dx, xr.grad, held != "mx8"), (dgate, gr.grad, True), (dW1, W1r.grad, held != "mx8"), (dW2, W2r.grad, held != "mx8")):
+        assert float((host(got) - want.detach()).abs().max()) <= (1e-5 if exact else 0.1) * float(want.detach().abs().max())
+    small = ["--tokens", "70", "--experts", "4", "--d", "256", "--hidden", "192", "--block", "64", "--steps", "1", "--expert", "gated", "--held", held]
+    for more in ([], ["--weights", "dense"]):
+        assert ex.main(small + more) == 0
