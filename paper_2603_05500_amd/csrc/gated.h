@@ -11,29 +11,24 @@
 namespace poetx {
 namespace gated {
 
-// -z log2(e) = g (c1 + c3 g^2): both activations by the same instructions
+// -z log2(e) = g (c1 + c3 g^2): both activations by the same instructions.  silu: c3 = -1e-38, nothing beside c1 wherever s is not 0 or 1, but no zero for an infinity to meet.
 struct Act {
   float c1, c3;
 };
-inline Act act_of(int activation) { return activation == POETX_GATED_GELU ? Act{-2.3022081963f, -0.10294323954f} : Act{-1.4426950409f, 0.f}; }
+inline Act act_of(int activation) { return activation == POETX_GATED_GELU ? Act{-2.3022081963f, -0.10294323954f} : Act{-1.4426950409f, -1e-38f}; }
 
-// The larger (smaller) of two, NaN if either is.
+// The larger of two, NaN if either is.
 __device__ __forceinline__ float maximum(float a, float b) {
   float r;
   asm("v_maximum3_f32 %0, %1, %2, %2" : "=v"(r) : "v"(a), "v"(b));
   return r;
 }
-__device__ __forceinline__ float minimum(float a, float b) {
-  float r;
-  asm("v_minimum3_f32 %0, %1, %2, %2" : "=v"(r) : "v"(a), "v"(b));
-  return r;
-}
 
-// Its value and derivative.  Beyond 1e18 z keeps its sign (and no zero meets an infinity); beyond 1000 the derivative is 0 or 1 whatever g is, and 1 - s or s is zero.  NaN stays
+// Its value and derivative.  Below -1e18 the value is that of -1e18, which is 0; beyond 1000 the derivative is 0 or 1 whatever g is, and 1 - s or s is zero.  NaN stays
 // NaN.  exp and the reciprocal are the hardware's, a unit in the last place each; its rounded argument costs e^-z |z| 2^-24 of itself, times 4 for its roundings and constants.
 __device__ __forceinline__ void act_both(Act k, float g, float& a, float& da) {
-  const float lo = maximum(g, -1e18f), c = minimum(lo, 1e18f);
-  const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(c * fmaf(k.c3, c * c, k.c1)));
+  const float lo = maximum(g, -1e18f);
+  const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(lo * fmaf(k.c3, lo * lo, k.c1)));
   const float t = __builtin_amdgcn_fmed3f(g, -1000.f, 1000.f);
   a = lo * s;
   da = s * fmaf(t * fmaf(-3.f * 0.6931471806f * k.c3, t * t, -0.6931471806f * k.c1), 1.f - s, 1.f);

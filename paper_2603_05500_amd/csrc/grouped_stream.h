@@ -254,16 +254,18 @@ __device__ __forceinline__ void gated_tile(const StreamArgs& g, floatx4 (&acc)[C
   // codes and the scale of a block of 32 columns (two pieces) of each row; columns past the last are no part of it and have codes of zero
   auto quantise = [&](const float (&z)[AT_ONCE][4], int p, uint32_t& d0, uint32_t& d1, uint32_t& sb) __attribute__((always_inline)) {
     const bool in0 = 16 * p + 4 * q4 < cols, in1 = 16 * p + 16 + 4 * q4 < cols;
-    const uint32_t m0 = in0 ? mx8::largest4(z[0][0], z[0][1], z[0][2], z[0][3]) : 0;
-    const uint32_t m1 = in1 ? mx8::largest4(z[AT_ONCE - 1][0], z[AT_ONCE - 1][1], z[AT_ONCE - 1][2], z[AT_ONCE - 1][3]) : 0;
+    // worked out for every lane and then chosen: as arms of a conditional these were branches, 128 of them in a tile
+    uint32_t m0 = mx8::largest4(z[0][0], z[0][1], z[0][2], z[0][3]), m1 = mx8::largest4(z[AT_ONCE - 1][0], z[AT_ONCE - 1][1], z[AT_ONCE - 1][2], z[AT_ONCE - 1][3]);
+    m0 = in0 ? m0 : 0, m1 = in1 ? m1 : 0;
     uint32_t m = m0 > m1 ? m0 : m1;
     const auto t = __builtin_amdgcn_permlane16_swap(m, m, false, false);      // over the four groups of 16 lanes
     m = t[0] > t[1] ? t[0] : t[1];
     const auto f = __builtin_amdgcn_permlane32_swap(m, m, false, false);
     m = f[0] > f[1] ? f[0] : f[1];
     sb = mx8::scale_byte(m);
-    d0 = in0 ? mx8::to_codes4(z[0][0], z[0][1], z[0][2], z[0][3], sb) : 0;
-    d1 = in1 ? mx8::to_codes4(z[AT_ONCE - 1][0], z[AT_ONCE - 1][1], z[AT_ONCE - 1][2], z[AT_ONCE - 1][3], sb) : 0;
+    d0 = mx8::to_codes4(z[0][0], z[0][1], z[0][2], z[0][3], sb);
+    d1 = mx8::to_codes4(z[AT_ONCE - 1][0], z[AT_ONCE - 1][1], z[AT_ONCE - 1][2], z[AT_ONCE - 1][3], sb);
+    d0 = in0 ? d0 : 0, d1 = in1 ? d1 : 0;
   };
   // A group of 16 lanes gives its four columns of every piece for all columns of one (P = 4; P = 2: half of one).
   auto store_codes = [&](const uint32_t (&d)[P], const uint32_t (&sb)[(P + 1) / 2], Matrix& mc, Matrix& ms) __attribute__((always_inline)) {
