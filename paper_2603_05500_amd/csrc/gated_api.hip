@@ -79,6 +79,18 @@ size_t workspace_bytes(const poetx_gated_desc* d) {
   return s.weight + s.sums;
 }
 
+// The tile of the streams for bf16 groups whose rows are fewer than the largest one's: what the choice for plain products goes by leaves out that such groups read the weights at the rate of the
+// memory, for which smaller tiles divide the work more evenly, and that a tile ends with the activation.  Forward that keeps G and U, groups of uneven sizes, us on tiles of
+// 256 x 256 / 256 x 128 / 128 x 128, by rows per group: 64 of 2 x 1376 x 2048 (7 without any), 89 rows 218 / 198 / 178, 127 221 / 220 / 200, 160 220 / 227 / 226, 191 269 / 256 / 254,
+// 228 273 / 287 / 285; 8 of 2 x 8192 x 4096, 100 rows 290 / 266 / 247, 143 297 / 279 / 286, 180 385 / 334 / 338, 215 366 / 351 / 420, 256 368 / 395 / 490; 3 of 2 x 11008 x 4096, 143 rows
+// 241 / 195 / 174; 24 of 2 x 704 x 1024, 143 rows 43 / 47 / 33, 200 44 / 48 / 44.
+grouped::Kernel tile_for_groups(const poetx_gated_desc* d, grouped::Kernel k) {
+  const i64 live = d->rows < d->groups ? d->rows : d->groups, mean = d->rows / live;
+  const bool large = k == grouped::STREAM_256, wide = k == grouped::STREAM_256x128;
+  if (d->groups == 1 || mean > 220 || !(large || wide)) return k;
+  return mean <= 150 ? grouped::STREAM_128 : grouped::STREAM_256x128;
+}
+
 void products(const poetx_gated_desc* d, const void* X, i64 ldx, const void* W, const int32_t* offsets, gated::Mode mode, const gated::Out& out, void* ws, hipStream_t st) {
   gated::Call q{X, W, ldx, offsets, d->rows, d->d_in, d->d_hidden, d->groups, mode, out};
   const bool four = d->flags & POETX_GATED_W_MX4, streamed = four && gated::values_supported(q);
@@ -99,7 +111,7 @@ void products(const poetx_gated_desc* d, const void* X, i64 ldx, const void* W, 
   const grouped::Call c = product_of(d, X, ldx, W, offsets);
   const grouped::Plan p = grouped::plan(d->dtype, grouped::FWD, c, gated::stream_supported(d->dtype, q), d->d_hidden % 2 == 0 ? s.sums : 0);      // sums are stored in whole vectors
   if (p.kernel < grouped::STREAM_256) return gated::edge_launch(d->dtype, p.kernel, q, st);
-  if (p.splits == 1) return gated::stream_launch(d->dtype, p.kernel, q, st);
+  if (p.splits == 1) return gated::stream_launch(d->dtype, tile_for_groups(d, p.kernel), q, st);
   grouped::stream_sums(d->dtype, p, c, sums, st);
   gated::rows_launch(d->dtype, gated::SUMS, gated::In{sums, nullptr, 0, p.splits}, offsets, d->groups, d->rows, d->d_hidden, mode, out, st);
 }
