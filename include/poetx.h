@@ -429,7 +429,9 @@ typedef struct {
  *                      gradient, which needs them, and for the forwards that are faster so.  us in all of it / none: 1 row by 14336 x 4096 10 / 10, 4096 rows 411 / 399,
  *                      16384 rows by 4096 x 4096 411 / 446, few tiles (219 rows, 12032 -> 1152) 20 / 41, no whole 16-byte vectors (4096 rows, 4001 -> 4001) 396 / 670.
  *   W_MX4 and X_MX4    nothing: codes of X, re-laid scales, or the values of both are made there.
- *   X_MX8              nothing: X's values are made there. */
+ *   X_MX8              nothing: X's values are made there; dZ in rows of whole 16-byte vectors where its own have another length; and fp32 sums of a gradient whose contraction is split among
+ *                      workgroups, or whose rows are no whole vectors.  Its order of the sums is then another than that of the dense call.  us, 2752 x 512 from 16384 rows 79 (dense X, not split: 148),
+ *                      2048 x 11264 from 4095 211 (213). */
 size_t poetx_grouped_workspace_bytes(const poetx_grouped_desc* desc);
 
 int poetx_grouped_fwd(const poetx_grouped_desc* desc, const void* X, int64_t ldx, const void* W, const int32_t* offsets,
@@ -501,8 +503,14 @@ typedef struct {
 #define POETX_GATED_W_MX4 1      /* W in four bits */
 #define POETX_GATED_HELD_MX8 2   /* G and U are kept in eight bits */
 
-/* Scratch of the larger of poetx_gated_fwd and poetx_gated_bwd_recompute, 16-byte aligned, apart from the tensors; 0 for an
- * invalid descriptor. */
+/* Scratch of the larger of poetx_gated_fwd and poetx_gated_bwd_recompute, all of which they need where it is not 0; 16-byte
+ * aligned, apart from the tensors; 0 for an invalid descriptor.  It holds fp32 sums of parts of the contraction where a product has
+ * few tiles, and a 4-bit weight's values where they are written out first (a few large products, and whatever X's alignment
+ * keeps from being decoded on the way); G and U themselves are never there.  MB: 16384 x 14336 x 4096 0, with a weight in four
+ * bits 235; 64 groups of 1376 x 2048 with 8190 rows 0, four bits 721.
+ * Which kernels run follows, as in the grouped products, from the descriptor, the strides and the alignment: rows of X (and a
+ * dense W) of whole 16-byte vectors with up to 256 groups on the streaming kernels, whatever the other tensors' strides and
+ * alignments and d_hidden; a handful of rows per group on short ones; the rest on edge-handling ones. */
 size_t poetx_gated_workspace_bytes(const poetx_gated_desc* desc);
 
 /* H (out).  G, U (out): kept for the backward pass, or both NULL. */

@@ -1,7 +1,7 @@
 // The gated block's elementwise half: from G and U (as they were kept, or as sums of parts of the contraction) to H, what is kept, or the gradients dG, dU and H again.
 //
 // One pass: sixteen lanes take 128 columns of a row, eight each, of G, U and dH, so that 8-bit buffers come by whole units and every access of a wave is contiguous.
-// Bound by bytes.
+// Bound by bytes: 16384 x 14336 from eight bits, dG, dU and H in bf16, 403 to 420 us for 2.36 GB (5.7 TB/s; a large copy makes 5.1); 1001 x 1376 in fp32 9.2 us, of which 6.4 for the bytes.
 #include "gated.h"
 
 namespace poetx {

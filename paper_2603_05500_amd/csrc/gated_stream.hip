@@ -1,4 +1,13 @@
 // The gated block on the streaming kernel: both projections, the activation and the product in one launch, and the backward pass that makes G and U again.
+//
+// A tile of the weight has 16 rows of gate and 16 of up in turn, so that each lane ends with G and U of the same four elements: nothing is exchanged for the product, and a block of 32 columns
+// of eight bits lies in one wave's registers.  G and U reach memory only where they are kept.
+// What bounds it: the product, and what a tile writes while its CU multiplies nothing.  16384 x 4096 by 2 x 14336 x 4096, us and PFLOP/s: H alone 2855 (1.35; the grouped product of
+// the same columns, which writes G and U, 2960), G and U kept 3170 (1.21), in eight bits 3140 (1.23), gradients from G and U made again 3280 (1.17).  The multiplications take 61 % of the
+// cycles at 1.9 GHz, tiles' ends 9 to 20 us of each 110 (by what they write, at 5 TB/s, and 2300 to 4400 vector instructions of a wave), the rest waits for a stage's loads.  With operands in
+// 64-byte pieces three stages ahead, instead of whole lines one unit ahead, 2 to 5 % more (8 groups of 2 x 8192 x 4096 1830 against 1724); loads of a unit in the first half of the
+// stage 3 % more; two workgroups of 128 x 128 a CU, so that one ends tiles while the other multiplies, 5 to 15 % more but for contractions of 512 and less.
+// Few rows per group: the bytes of the weights (57 groups, 8190 rows of 2 x 1376 x 2048 200 us for 743 MB, of which a copy would take 145).
 #include "grouped_stream.h"
 
 namespace poetx {

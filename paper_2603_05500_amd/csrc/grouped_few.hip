@@ -9,7 +9,8 @@
 //   VALUES  32 codes with their scale, decoded in registers: four MFMAs of depth 32, in which the four groups of 16 lanes hold four different blocks of 32
 //           (the order of a contraction is free as long as both operands keep it)
 //   CODES   32 codes, and 32 of X: one scaled MFMA of depth 128
-// A gated block's weight rows come in turn from gate and up, so that a tile has G and U of half as many columns of H.
+// A gated block's weight rows come in turn from gate and up, so that a tile has G and U of half as many columns of H.  One row by 2 x 14336 x 4096 in bf16 37 to 47 us (235 MB: 5.0 TB/s with
+// weights from memory), eight rows, one each for eight of 64 groups of 2 x 1376 x 2048 in four bits 8.3.
 #include "gated.h"
 
 namespace poetx {

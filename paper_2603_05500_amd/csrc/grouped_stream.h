@@ -15,6 +15,7 @@
 //  - A stage is 64 bytes of a row whatever they hold: 32 bf16, 16 fp32, or 128 codes with a word of four scales.  An MFMA of 16 x 16 x 128 codes takes as long
 //    as one of 16 x 16 x 32 bf16: the same stream carries four times the products.  The fp32 ones take eight times as long for the bytes: smaller tiles and several
 //    workgroups per CU.
+//  - A gated block's tile has rows of gate and of up in turn and makes of them H, what is kept for the backward pass, or the gradients (gated_tile).
 // What bounds it: large bf16 products by power, as the dense one (16384 rows, 8 groups of 8192 x 4096: 960 to 1015 us, 1.08 to 1.15 PFLOP/s with the ragged tiles); products of codes by the
 // loads of a stage, which take as long as its multiplications (16384 x 4096 by 14336 x 4096 465 us, 4.1 PFLOP/s; without loads 384); many small groups by the weights' bytes (8190 rows,
 // 57 groups of 1376 x 2048, input gradient 92 to 103 us); weight gradients by their stores (8192 rows, 16 groups of 1376 x 2048 93 us for 180 MB).

@@ -29,7 +29,7 @@ struct ValuesArgs {
   gated::Out block;      // MODE: of a gated block (n: d_hidden)
 };
 
-// MODE: a gated block, a tile's first half of columns being gate's and its second half up's of as many columns of H.
+// MODE: a gated block (14187 rows over 3 groups of 2 x 544 x 2336 107 us, 134 with the weight written out first), a tile's first half of columns being gate's and its second half up's of as many columns of H.
 template <int BM, int BN, int NS, bool PARTS, int MODE>
 __global__ __launch_bounds__(256) void grouped_values_kernel(ValuesArgs g, int first) {
   constexpr int A_BYTES = BM * 256, B_BYTES = BN * 64, STAGE_BYTES = A_BYTES + B_BYTES + BN * 4;

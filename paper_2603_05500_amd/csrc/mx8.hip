@@ -2,6 +2,7 @@
 //
 // Plain streams, as of the 4-bit buffers: sixteen lanes take a unit of 128 columns, eight elements each, four lanes share a block of 32 and its largest magnitude.  The
 // scale is that magnitude's exponent, so that a code is the element with another exponent, rounded to a whole number: no division, and reading it back is exact.
+// Bound by bytes: 16384 x 4096 bf16 to codes 40 to 46 us (4.5 to 5 TB/s), back 30 (its codes in the Infinity Cache); 16384 x 14336 back 108 to 125 (5.7 to 6.6 TB/s).
 #include "edge_gemm.h"
 #include "grouped.h"
 #include "mx8.h"
