@@ -505,12 +505,13 @@ typedef struct {
 
 /* Scratch of the larger of poetx_gated_fwd and poetx_gated_bwd_recompute, all of which they need where it is not 0; 16-byte
  * aligned, apart from the tensors; 0 for an invalid descriptor.  It holds fp32 sums of parts of the contraction where a product has
- * few tiles, and a 4-bit weight's values where they are written out first (a few large products, and whatever X's alignment
- * keeps from being decoded on the way); G and U themselves are never there.  MB: 16384 x 14336 x 4096 0, with a weight in four
+ * few tiles, a 4-bit weight's values where they are written out first (a few large products, and whatever X's alignment
+ * keeps from being decoded on the way), and, where d_in is no multiple of 16 bytes, X in rows that are and, where that pays, a
+ * dense W too; G and U themselves are never there.  MB: 16384 x 14336 x 4096 0, with a weight in four
  * bits 235; 64 groups of 1376 x 2048 with 8190 rows 0, four bits 721.
  * Which kernels run follows, as in the grouped products, from the descriptor, the strides and the alignment: rows of X (and a
- * dense W) of whole 16-byte vectors with up to 256 groups on the streaming kernels, whatever the other tensors' strides and
- * alignments and d_hidden; a handful of rows per group on short ones; the rest on edge-handling ones. */
+ * dense W) of whole 16-byte vectors, as they are or as they are laid anew, with up to 256 groups on the streaming kernels,
+ * whatever the other tensors' strides and alignments and d_hidden; a handful of rows per group on short ones; the rest on edge-handling ones. */
 size_t poetx_gated_workspace_bytes(const poetx_gated_desc* desc);
 
 /* H (out).  G, U (out): kept for the backward pass, or both NULL. */

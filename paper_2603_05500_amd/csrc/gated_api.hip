@@ -54,13 +54,38 @@ size_t stream_sums_bytes(const poetx_gated_desc* d) {
   const gated::Call q{nullptr, nullptr, d->d_in, nullptr, d->rows, d->d_in, d->d_hidden, d->groups, gated::FWD, {}};
   return d->d_hidden % 2 == 0 && gated::stream_supported(d->dtype, q) ? align256(grouped::plan(d->dtype, grouped::FWD, c, true, ~(size_t)0).parts) : 0;
 }
-// The workspace: a 4-bit weight's values, where a call may need them (which of two kernels for a handful of rows takes one depends on its tensors), then sums.
+// Where a row of X is no whole 16-byte vectors, by its length alone: are X and a dense W laid anew in rows that are, zeros behind their columns, for the streams?  A model of the times with and without
+// says so; a 4-bit weight, whose rows are whole anyway, leaves only X.  us, without / with: 11484 rows, 916 -> 2 x 6560 in four bits 897 / 366; 309 rows, 3366 -> 2 x 416 in four bits 37.5 / 19.5; 2048
+// rows, 4001 -> 2 x 4000 398 / 154; 4000 rows over 8 groups, 1001 -> 2 x 2000 116 / 100; fp32 1405 rows, 1014 -> 2 x 544 59.9 / 54.5.
+bool relaid(const poetx_gated_desc* d, poetx_gated_desc* as) {
+  const i64 es = (i64)esize(d->dtype), v = 16 / es;
+  const bool four = d->flags & POETX_GATED_W_MX4;
+  if (d->d_in % v == 0 || few(d, four ? grouped::VALUES_MX4 : grouped::DENSE_WEIGHT)) return false;
+  *as = *d;
+  as->d_in = (int)((d->d_in + v - 1) / v * v);
+  if (four) return true;
+  const gated::Call q{nullptr, nullptr, as->d_in, nullptr, d->rows, as->d_in, d->d_hidden, d->groups, gated::FWD, {}};
+  if (!gated::stream_supported(d->dtype, q)) return false;
+  const double copies = 6 + ((double)d->rows + 2. * d->groups * d->d_hidden) * (d->d_in + as->d_in) * es / 4.5e6;
+  const grouped::Call c = product_of(d, nullptr, d->d_in, nullptr, nullptr), w = product_of(as, nullptr, as->d_in, nullptr, nullptr);
+  return copies + grouped::plan(d->dtype, grouped::FWD, w, true, 0).us < grouped::plan(d->dtype, grouped::FWD, c, false, 0).us;
+}
+
+// The workspace: X again, where it is laid anew; a 4-bit weight's values, where a call may need them (which of two kernels for a handful of rows takes one depends on its tensors), or a dense one laid
+// anew; then sums.
 struct Scratch {
-  size_t weight, sums;
+  size_t x, weight, sums;
 };
 Scratch scratch_of(const poetx_gated_desc* d) {
-  Scratch s{0, 0};
+  Scratch s{0, 0, 0};
   if (d->rows == 0) return s;
+  poetx_gated_desc as;
+  if (relaid(d, &as)) {
+    s = scratch_of(&as);
+    s.x = align256((size_t)d->rows * as.d_in * esize(d->dtype));
+    if (!(d->flags & POETX_GATED_W_MX4)) s.weight = align256((size_t)d->groups * 2 * d->d_hidden * as.d_in * esize(d->dtype));
+    return s;
+  }
   if (!(d->flags & POETX_GATED_W_MX4)) {
     s.sums = few(d, grouped::DENSE_WEIGHT) ? 0 : stream_sums_bytes(d);
     return s;
@@ -76,7 +101,7 @@ Scratch scratch_of(const poetx_gated_desc* d) {
 }
 size_t workspace_bytes(const poetx_gated_desc* d) {
   const Scratch s = scratch_of(d);
-  return s.weight + s.sums;
+  return s.x + s.weight + s.sums;
 }
 
 // The tile of the streams for bf16 groups whose rows are fewer than the largest one's: what the choice for plain products goes by leaves out that such groups read the weights at the rate of the
@@ -91,29 +116,45 @@ grouped::Kernel tile_for_groups(const poetx_gated_desc* d, grouped::Kernel k) {
   return mean <= 150 ? grouped::STREAM_128 : grouped::STREAM_256x128;
 }
 
-void products(const poetx_gated_desc* d, const void* X, i64 ldx, const void* W, const int32_t* offsets, gated::Mode mode, const gated::Out& out, void* ws, hipStream_t st) {
+// weight, sums: the workspace's parts
+void products_of(const poetx_gated_desc* d, const void* X, i64 ldx, const void* W, const int32_t* offsets, gated::Mode mode, const gated::Out& out, char* weight, char* sums, size_t sums_bytes,
+                 hipStream_t st) {
   gated::Call q{X, W, ldx, offsets, d->rows, d->d_in, d->d_hidden, d->groups, mode, out};
   const bool four = d->flags & POETX_GATED_W_MX4, streamed = four && gated::values_supported(q);
   const bool handful = few(d, !four ? grouped::DENSE_WEIGHT : streamed ? grouped::VALUES_STREAMED_MX4 : grouped::VALUES_MX4);
-  const Scratch s = scratch_of(d);
-  void* sums = (char*)ws + s.weight;
-  if (streamed && gated::values_launch(q, handful, sums, s.sums, s.sums, st)) return;
+  if (streamed && gated::values_launch(q, handful, sums, sums_bytes, sums_bytes, st)) return;
   if (handful) {
     StageTimer tm(POETX_STAGE_DENSE, st);
     return gated::few_launch(d->dtype, four, q, st);
   }
   if (four) {
     StageTimer tm(POETX_STAGE_DEQUANT, st);
-    mx4_dequantize_groups_launch(W, d->groups, 2 * d->d_hidden, d->d_in, offsets, d->rows, ws, st);
-    q.W = W = ws;
+    mx4_dequantize_groups_launch(W, d->groups, 2 * d->d_hidden, d->d_in, offsets, d->rows, weight, st);
+    q.W = weight;
   }
   StageTimer tm(POETX_STAGE_DENSE, st);
-  const grouped::Call c = product_of(d, X, ldx, W, offsets);
-  const grouped::Plan p = grouped::plan(d->dtype, grouped::FWD, c, gated::stream_supported(d->dtype, q), d->d_hidden % 2 == 0 ? s.sums : 0);      // sums are stored in whole vectors
+  const grouped::Call c = product_of(d, X, ldx, q.W, offsets);
+  const grouped::Plan p = grouped::plan(d->dtype, grouped::FWD, c, gated::stream_supported(d->dtype, q), d->d_hidden % 2 == 0 ? sums_bytes : 0);      // sums are stored in whole vectors
   if (p.kernel < grouped::STREAM_256) return gated::edge_launch(d->dtype, p.kernel, q, st);
   if (p.splits == 1) return gated::stream_launch(d->dtype, tile_for_groups(d, p.kernel), q, st);
   grouped::stream_sums(d->dtype, p, c, sums, st);
   gated::rows_launch(d->dtype, gated::SUMS, gated::In{sums, nullptr, 0, p.splits}, offsets, d->groups, d->rows, d->d_hidden, mode, out, st);
+}
+
+void products(const poetx_gated_desc* d, const void* X, i64 ldx, const void* W, const int32_t* offsets, gated::Mode mode, const gated::Out& out, void* ws, hipStream_t st) {
+  const Scratch s = scratch_of(d);
+  char *x = (char*)ws, *weight = x + s.x, *sums = weight + s.weight;
+  poetx_gated_desc as;
+  if (!relaid(d, &as)) return products_of(d, X, ldx, W, offsets, mode, out, weight, sums, s.sums, st);
+  {
+    StageTimer tm(POETX_STAGE_LAYOUT, st);
+    relay_rows_launch(d->dtype, X, d->rows, d->d_in, ldx, x, as.d_in, st, offsets, d->groups);
+    if (!(d->flags & POETX_GATED_W_MX4)) {
+      relay_rows_launch(d->dtype, W, 2 * (i64)d->groups * d->d_hidden, d->d_in, d->d_in, weight, as.d_in, st);
+      W = weight;
+    }
+  }
+  products_of(&as, x, as.d_in, W, offsets, mode, out, weight, sums, s.sums, st);
 }
 
 }  // namespace

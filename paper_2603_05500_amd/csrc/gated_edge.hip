@@ -1,6 +1,6 @@
 // The gated block for any sizes, strides and alignments, bf16 and fp32: the edge-handling product over rows of gate and up in turn, one tile of H of one group per
 // workgroup, as the grouped edge products.  A lane gets eight neighbouring columns of a row, which are G and U of four elements.  Bound, as they are, by the latency of
-// the stages of short or narrow products and by the loads' bounds checks of large ones (1967 rows over 11 groups of 2 x 1280 x 4142, whose rows no stream can read, 195 us, 0.21 PFLOP/s).
+// the stages of short or narrow products and by the loads' bounds checks of large ones (1967 rows over 11 groups of 2 x 1280 x 4142, whose weights would take as long to lay anew for a stream, 198 us, 0.21 PFLOP/s).
 #include "gated.h"
 
 namespace poetx {
@@ -130,11 +130,15 @@ void go(const Call& c, hipStream_t st) {
 template <class T, Mode MODE>
 void pick(grouped::Kernel k, const Call& c, hipStream_t st) {
   constexpr int D = 128 / (int)sizeof(T);
-  // EDGE_128 is not among what plan() gives a forward product.  HOLD_MX8: a wave's columns are whole blocks
-  if constexpr (MODE == HOLD_MX8) k == grouped::EDGE_64 ? go<T, 64, 64, D, 2, 1, 4, MODE>(c, st) : go<T, 32, 64, 2 * D, 1, 1, 4, MODE>(c, st);
-  else if (k == grouped::EDGE_32) go<T, 32, 32, 2 * D, 1, 1, 4, MODE>(c, st);
-  else if (k == grouped::EDGE_32_DEEP) go<T, 32, 32, 8 * D, 1, 1, 16, MODE>(c, st);
-  else go<T, 64, 64, D, 2, 2, 4, MODE>(c, st);
+  // What plan() gives forward products: 64 x 64, 32 x 32, and in bf16 32 x 32 with deep stages.  HOLD_MX8: a wave's columns are whole blocks.
+  if constexpr (MODE == HOLD_MX8) {
+    k == grouped::EDGE_64 ? go<T, 64, 64, D, 2, 1, 4, MODE>(c, st) : go<T, 32, 64, 2 * D, 1, 1, 4, MODE>(c, st);
+  } else {
+    if constexpr (sizeof(T) == 2) {
+      if (k == grouped::EDGE_32_DEEP) return go<T, 32, 32, 8 * D, 1, 1, 16, MODE>(c, st);
+    }
+    k == grouped::EDGE_32 ? go<T, 32, 32, 2 * D, 1, 1, 4, MODE>(c, st) : go<T, 64, 64, D, 2, 2, 4, MODE>(c, st);
+  }
 }
 
 }  // namespace

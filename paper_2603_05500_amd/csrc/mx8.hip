@@ -75,7 +75,7 @@ __global__ __launch_bounds__(256) void relay_rows_kernel(const T* __restrict__ X
   constexpr int V = 16 / sizeof(T);
   const i64 across = ldo / V, i = (block0 + (i64)blockIdx.x) * 256 + threadIdx.x, row = i / across;
   const int col = (int)(i - row * across) * V;
-  const i64 r0 = grouped::offset_at(offsets, 0, rows), r1 = grouped::furthest_end(offsets, groups, rows);
+  const i64 r0 = offsets ? grouped::offset_at(offsets, 0, rows) : 0, r1 = offsets ? grouped::furthest_end(offsets, groups, rows) : rows;
   if (row < r0 || row >= r1) return;
   *reinterpret_cast<edge::u32x4*>(out + row * ldo + col) = edge::load_branched(X + row * ld, col, cols, true);
 }

@@ -187,8 +187,8 @@ void mx8_quantize_launch(int dtype, const void* X, i64 rows, int cols, i64 ld, v
 // offsets: only the rows that one of `groups` groups has
 void mx8_dequantize_launch(const void* Q, i64 rows, int cols, int dtype, void* out, i64 ld, hipStream_t st, const int32_t* offsets = nullptr, int groups = 0);
 
-// out (row stride ldo, whole 16-byte vectors) = the rows of X that one of `groups` groups has
-void relay_rows_launch(int dtype, const void* X, i64 rows, int cols, i64 ld, void* out, i64 ldo, hipStream_t st, const int32_t* offsets, int groups);
+// out (row stride ldo, whole 16-byte vectors, zeros past the columns) = X, or (offsets) the rows that one of `groups` groups has
+void relay_rows_launch(int dtype, const void* X, i64 rows, int cols, i64 ld, void* out, i64 ldo, hipStream_t st, const int32_t* offsets = nullptr, int groups = 0);
 
 // ---- rows in the order of their groups (group_order.hip) ---------------------------------------
 size_t group_order_workspace_bytes(i64 n, int groups);

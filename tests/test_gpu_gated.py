@@ -367,6 +367,8 @@ PATHS = [
     ([92], 4104, 1032, "bf16", "dense"), ([192], 2056, 2100, "bf16", "dense"), ([1000, 1040], 4104, 66, "bf16", "dense"), ([292], 65, 1001, "bf16", "dense"),
     ([32], 4104, 2056, "bf16", "mx4"), ([1092, 1900], 6152, 130, "bf16", "mx4"), ([3000, 0, 2992], 264, 1001, "bf16", "mx4"), ([120], 65, 8192, "bf16", "mx4"),
     ([8], 64, 6200, "bf16", "mx4"), ([5992], 136, 2056, "bf16", "mx4"), ([1500, 1492], 65, 130, "bf16", "mx4"),
+    ([2040], 1001, 1000, "bf16", "dense"), ([700, 0, 800], 1001, 515, "bf16", "dense"), ([1492], 916, 1032, "bf16", "mx4"), ([290], 3366, 416, "bf16", "mx4"), ([1397], 1014, 544, "f32", "dense"),
+    ([20] * 300, 72, 40, "bf16", "dense"), ([20] * 300, 72, 40, "bf16", "mx4"), ([5] * 300, 72, 264, "f32", "dense"),
     ([1492], 2056, 2100, "f32", "dense"), ([700, 1348], 2056, 72, "f32", "dense"), ([292], 1032, 1032, "f32", "dense"), ([2992], 65, 130, "f32", "dense"),
 ]
 
