@@ -1,8 +1,8 @@
 """8-bit buffers, the gated feed-forward block, its backward pass and the weight gradient that reads 8-bit rows, against plain float64 forms written here.
 
 Bounds, per element, with u = 2^-24 (half a step of fp32) and r the half step of the result's type (2^-8 bf16, u fp32):
-  G, U     products of two bf16 (or of a bf16 and a 4-bit value) are exact in fp32, so a sum of K of them is off by at most eG = (K + 1) u sum |x w| (fp32: a rounding
-           more per product, within the same + u), kept ones by r |G| more.
+  G, U     products of two bf16 (or of a bf16 and a 4-bit value) are exact in fp32, so a sum of K of them is off by at most eG = (K + 2) u sum |x w| (fp32: a rounding
+           more per product, within the same), kept ones by r |G| more.
   s        z is rounded up to 5 times and multiplied by a rounded log2(e): the exponent is off by 7 u |z|; exp, the sum and the reciprocal by 2u, u, 2u of themselves.  What
            reaches s = 1 / (1 + e^-z) of an error of e^-z is its share 1 - s:      es = (1 - s) (7 |z| + 2) u + 3 u, relative.
   act      g s: relative es + u, and act' is at most 1.13 in size for either activation:      ea = |act| (es + u) + 1.13 eG.
