@@ -8,6 +8,11 @@ import sys
 import tempfile
 from concurrent.futures import ThreadPoolExecutor
 
+try:
+    from .load_waits import too_close
+except ImportError:      # run as a file
+    from load_waits import too_close
+
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
@@ -41,8 +46,20 @@ def build(verbose: bool = False) -> str:
     with tempfile.TemporaryDirectory() as tmp:
         objects = [os.path.join(tmp, os.path.basename(s)[:-4] + ".o") for s in sources()]
         compile_flags = [f for f in FLAGS if f != "-shared"]
+
+        def compile_one(source, obj):
+            for waits in ([], ["-DPOETX_LOAD_WAITS"]):
+                run([hipcc, *compile_flags, *waits, "--save-temps=obj", "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c", source, "-o", obj])
+                with open(obj[:-2] + "-hip-amdgcn-amd-amdhsa-gfx950.s") as f:
+                    found = too_close(f.read())
+                if not found:
+                    return
+                if verbose:
+                    print(source + ": loads that need waits:", *found, sep="\n  ", flush=True)
+            raise RuntimeError(f"{source}: scalar operands read too soon: {found}")
+
         with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
-            list(pool.map(lambda so: run([hipcc, *compile_flags, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c", so[0], "-o", so[1]]), zip(sources(), objects)))
+            list(pool.map(compile_one, sources(), objects))
         run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-fno-gpu-rdc", *objects, "-o", LIB])
     # the measurement tool: machine ceilings next to the dense kernel and its feed-less variants
     tool = [hipcc, "--offload-arch=gfx950", "-O3", "-std=c++17", "-Xclang", "-target-feature", "-Xclang",

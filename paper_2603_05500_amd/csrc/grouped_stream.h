@@ -80,17 +80,17 @@ struct StreamArgs {
 };
 
 // 16 (4) bytes per lane from base + voff straight into LDS at lds + 16 (4) * lane; zeros from the descriptor's end on.  Between M0's write and its use there has to be
-// an instruction.
+// an instruction, and more where a word of the descriptor has just come back from a vector register's lane, which the build looks for (load_waits.py).
 __device__ __forceinline__ void dma16b(const u32x4& rsrc, uint32_t voff, uint32_t lds) {
-  asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "{m0}"(lds) : "memory");
+  asm volatile(POETX_BEFORE_LOAD "buffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "{m0}"(lds) : "memory");
 }
 __device__ __forceinline__ void dma4b(const u32x4& rsrc, uint32_t voff, uint32_t lds) {
-  asm volatile("s_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "{m0}"(lds) : "memory");
+  asm volatile(POETX_BEFORE_LOAD "buffer_load_dword %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "{m0}"(lds) : "memory");
 }
 // The same, the lanes in `off` behind the descriptor's end.
 __device__ __forceinline__ void dma16b_but(uint64_t off, const u32x4& rsrc, uint32_t voff, uint32_t lds) {
   uint32_t v;
-  asm volatile("v_cndmask_b32 %0, %1, %2, %3\n\tbuffer_load_dwordx4 %0, %4, 0 offen lds" : "=&v"(v) : "v"(voff), "v"(0xfffffff0u), "s"(off), "s"(rsrc), "{m0}"(lds) : "memory");
+  asm volatile(POETX_BEFORE_MASKED_LOAD "v_cndmask_b32 %0, %1, %2, %3\n\tbuffer_load_dwordx4 %0, %4, 0 offen lds" : "=&v"(v) : "v"(voff), "v"(0xfffffff0u), "s"(off), "s"(rsrc), "{m0}"(lds) : "memory");
 }
 
 // The same value in every lane, in scalar registers.

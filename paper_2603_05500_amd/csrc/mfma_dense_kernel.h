@@ -133,7 +133,7 @@ __device__ __forceinline__ void pack_pair(const floatx4& x, const floatx4& y, ui
 // there has to be an instruction, which the compiler does not see to here.  Completion is tracked by hand through vmcnt.
 template <int OFF>
 __device__ inline void dma16g(const void* sbase, uint32_t voff, uint32_t lds_group) {
-  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 offset:%2" ::"v"(voff), "s"(sbase), "n"(OFF), "{m0}"(lds_group) : "memory");
+  asm volatile(POETX_BEFORE_LOAD "global_load_lds_dwordx4 %0, %1 offset:%2" ::"v"(voff), "s"(sbase), "n"(OFF), "{m0}"(lds_group) : "memory");
 }
 // load s of a wave's group of up to four (s is a constant wherever this is called)
 __device__ inline void dma16g_s(int s, const void* sbase, uint32_t voff, uint32_t lds_group) {

@@ -6,6 +6,16 @@
 
 #include "poetx.h"
 
+// In front of a load into LDS written in assembly: an instruction between M0's write and its use.  POETX_LOAD_WAITS, which the build sets for a source that needs it (load_waits.py): five, for a
+// scalar operand that a vector instruction has just written.
+#ifdef POETX_LOAD_WAITS
+#define POETX_BEFORE_LOAD "s_nop 4\n\t"
+#define POETX_BEFORE_MASKED_LOAD POETX_BEFORE_LOAD
+#else
+#define POETX_BEFORE_LOAD "s_nop 0\n\t"
+#define POETX_BEFORE_MASKED_LOAD      // opens with another instruction
+#endif
+
 namespace poetx {
 
 typedef long long i64;
