@@ -9,6 +9,7 @@
 // a part per multiplication and the scales are converted when they are used (14336 x 4096, 128 rows, 128 x 128: 34 us with both in one place, 29 so; 40 with the accumulators left to the
 // compiler).  4096 rows over 8 groups of 8192 x 4096 266 us (1.03 PFLOP/s; 426 by writing the weight out first).  The smallest tile leaves room for a second workgroup on a CU.
 #include "grouped_stream.h"
+#include "values_tile.h"
 
 namespace poetx {
 namespace grouped {
@@ -50,8 +51,8 @@ __global__ __launch_bounds__(256) void grouped_values_kernel(ValuesArgs g, int f
   const int n0 = id % g.tiles_n * BW;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1, q4 = lane >> 4, li = lane & 15;
   const int rows = t.r1 - t.r0 < BM ? t.r1 - t.r0 : BM, cols = g.n - n0 < BW ? g.n - n0 : BW;
-  auto weight_row = [&](int r) __attribute__((always_inline)) { return GATED && r >= BW ? g.n - BW + r : r; };      // from the tile's first one
-  const int wrows = GATED ? g.n + cols : cols;      // that the descriptors reach over
+  auto weight_row = [&](int r) __attribute__((always_inline)) { return GATED ? values::gated_row(r, g.n, BW) : r; };      // from the tile's first one
+  const int wrows = GATED ? values::gated_reach(g.n, n0, BW) : cols;      // that the descriptors reach over
 
   // ---- loads: X a row's 16 chunks in the order chunk ^ row % 8, so that 8 rows' same chunk lies in different banks
   const int lda = 2 * (int)g.ldx, ldb = g.units * 64;
