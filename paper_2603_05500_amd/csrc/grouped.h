@@ -75,6 +75,25 @@ __device__ inline int furthest_end(const int32_t* offsets, int groups, i64 rows)
   }
   return __builtin_amdgcn_readfirstlane(most);
 }
+// Rows that weight gradients may sum over, from the first to the last, the same in every lane: those that some group's own two offsets name, which may lie below the first offset.
+__device__ inline Range own_rows(const int32_t* offsets, int groups, i64 rows) {
+  Range all{offset_at(offsets, 0, rows), offset_at(offsets, groups, rows)};
+  int r0 = all.r0, r1 = all.r1;
+  for (int g = (int)(threadIdx.x & 63); g < groups; g += 64) {
+    const Range own = own_range(offsets, g, rows);
+    if (own.r0 == own.r1) continue;
+    r0 = own.r0 < r0 ? own.r0 : r0;
+    r1 = own.r1 > r1 ? own.r1 : r1;
+  }
+  if (__builtin_expect(__ballot(r0 < all.r0 || r1 > all.r1) == 0, 1)) return all;
+#pragma unroll 1
+  for (int s = 1; s < 64; s *= 2) {
+    const int a = __shfl_xor(r0, s), b = __shfl_xor(r1, s);
+    r0 = a < r0 ? a : r0;
+    r1 = b > r1 ? b : r1;
+  }
+  return Range{__builtin_amdgcn_readfirstlane(r0), __builtin_amdgcn_readfirstlane(r1)};
+}
 
 // Sum over a wave of the values of lower lanes and this one.
 __device__ __forceinline__ int wave_scan(int v) {

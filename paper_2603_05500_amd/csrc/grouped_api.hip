@@ -247,7 +247,7 @@ int poetx_grouped_bwd_weight(const poetx_grouped_desc* d, const void* X, int64_t
       mx8_dequantize_launch(X, d->rows, d->d_in, d->dtype, ws, h.ldx, st, offsets, d->groups);
       if (h.lddz) {
         c.in2 = (char*)ws + h.x;
-        relay_rows_launch(d->dtype, dZ, d->rows, d->d_out, lddz, (char*)ws + h.x, h.lddz, st, offsets, d->groups);
+        relay_rows_launch(d->dtype, dZ, d->rows, d->d_out, lddz, (char*)ws + h.x, h.lddz, st, offsets, d->groups, true);
       } else {
         c.ld_in2 = lddz;
       }

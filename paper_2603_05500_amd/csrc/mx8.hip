@@ -38,15 +38,16 @@ __global__ __launch_bounds__(256) void mx8_quantize_kernel(const T* __restrict__
   }
 }
 
-// Every row, or (offsets) those that some group has.
+// Every row, or (offsets) those that weight gradients sum over.
 template <class T>
 __global__ __launch_bounds__(256) void mx8_dequantize_kernel(mx8::View q, int cols, int upr, i64 rows, T* __restrict__ out, i64 ld, int block0, const int32_t* offsets, int groups) {
   const int lane = threadIdx.x & 15;
   const i64 first = (i64)(block0 + blockIdx.x) * (16 * UPL) + (threadIdx.x >> 4);
   i64 u0 = 0, u1 = rows * upr;
   if (offsets) {
-    u0 = (i64)grouped::offset_at(offsets, 0, rows) * upr;
-    u1 = (i64)grouped::furthest_end(offsets, groups, rows) * upr;
+    const grouped::Range own = grouped::own_rows(offsets, groups, rows);
+    u0 = (i64)own.r0 * upr;
+    u1 = (i64)own.r1 * upr;
   }
   u32x2 c[UPL];
   uint32_t sb[UPL];
@@ -69,23 +70,26 @@ __global__ __launch_bounds__(256) void mx8_dequantize_kernel(mx8::View q, int co
   }
 }
 
-// Rows of whole vectors from rows of any length and alignment: a vector a lane, zeros past the columns.
-template <class T>
+// Rows of whole vectors from rows of any length and alignment: a vector a lane, zeros past the columns.  Every row, or (offsets) those that some group has, or (OWN) that weight gradients sum over.
+template <class T, bool OWN>
 __global__ __launch_bounds__(256) void relay_rows_kernel(const T* __restrict__ X, i64 ld, int cols, i64 rows, T* __restrict__ out, i64 ldo, int block0, const int32_t* offsets, int groups) {
   constexpr int V = 16 / sizeof(T);
   const i64 across = ldo / V, i = (block0 + (i64)blockIdx.x) * 256 + threadIdx.x, row = i / across;
   const int col = (int)(i - row * across) * V;
-  const i64 r0 = offsets ? grouped::offset_at(offsets, 0, rows) : 0, r1 = offsets ? grouped::furthest_end(offsets, groups, rows) : rows;
-  if (row < r0 || row >= r1) return;
+  grouped::Range all{0, (int)rows};
+  if (offsets) all = OWN ? grouped::own_rows(offsets, groups, rows) : grouped::Range{grouped::offset_at(offsets, 0, rows), grouped::furthest_end(offsets, groups, rows)};
+  if (row < all.r0 || row >= all.r1) return;
   *reinterpret_cast<edge::u32x4*>(out + row * ldo + col) = edge::load_branched(X + row * ld, col, cols, true);
 }
 
 }  // namespace
 
-void relay_rows_launch(int dtype, const void* X, i64 rows, int cols, i64 ld, void* out, i64 ldo, hipStream_t st, const int32_t* offsets, int groups) {
+void relay_rows_launch(int dtype, const void* X, i64 rows, int cols, i64 ld, void* out, i64 ldo, hipStream_t st, const int32_t* offsets, int groups, bool own) {
   auto go = [&](auto* x, auto* o) {
+    typedef std::remove_pointer_t<decltype(o)> T;
+    auto kern = own ? relay_rows_kernel<T, true> : relay_rows_kernel<T, false>;
     launch_in_rows((rows * (ldo * (i64)sizeof(*o) / 16) + 255) / 256, [&](int block0, unsigned count) {
-      hipLaunchKernelGGL(relay_rows_kernel, dim3(count), dim3(256), 0, st, x, ld, cols, rows, o, ldo, block0, offsets, groups);
+      hipLaunchKernelGGL(kern, dim3(count), dim3(256), 0, st, x, ld, cols, rows, o, ldo, block0, offsets, groups);
     });
   };
   dtype == POETX_F32 ? go((const float*)X, (float*)out) : go((const uint16_t*)X, (uint16_t*)out);

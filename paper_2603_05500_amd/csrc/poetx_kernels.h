@@ -184,11 +184,12 @@ void mx4_dequantize_groups_launch(const void* Q, int groups, int n, int cols, co
 
 // ---- 8-bit buffers (mx8.hip; layout: mx8.h) -----------------------------------------------------
 void mx8_quantize_launch(int dtype, const void* X, i64 rows, int cols, i64 ld, void* Q, hipStream_t st);
-// offsets: only the rows that one of `groups` groups has
+// offsets: only the rows that the weight gradients of `groups` groups sum over
 void mx8_dequantize_launch(const void* Q, i64 rows, int cols, int dtype, void* out, i64 ld, hipStream_t st, const int32_t* offsets = nullptr, int groups = 0);
 
-// out (row stride ldo, whole 16-byte vectors, zeros past the columns) = X, or (offsets) the rows that one of `groups` groups has
-void relay_rows_launch(int dtype, const void* X, i64 rows, int cols, i64 ld, void* out, i64 ldo, hipStream_t st, const int32_t* offsets = nullptr, int groups = 0);
+// out (row stride ldo, whole 16-byte vectors, zeros past the columns) = X, or (offsets) the rows that one of `groups` groups has, or (own) that their weight gradients sum over
+void relay_rows_launch(int dtype, const void* X, i64 rows, int cols, i64 ld, void* out, i64 ldo, hipStream_t st, const int32_t* offsets = nullptr, int groups = 0,
+                       bool own = false);
 
 // ---- rows in the order of their groups (group_order.hip) ---------------------------------------
 size_t group_order_workspace_bytes(i64 n, int groups);
