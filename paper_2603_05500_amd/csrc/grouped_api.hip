@@ -233,7 +233,7 @@ int poetx_grouped_bwd_weight(const poetx_grouped_desc* d, const void* X, int64_t
   if (mx8 && d->rows > 0) {
     if (!enough(d, ws, ws_bytes)) return POETX_ERR_WORKSPACE;
     const size_t wb = workspace_bytes(d);
-    if (overlap(ws, wb, X, xb) || overlap(ws, wb, dZ, zb) || overlap(ws, wb, dW, ob)) return POETX_ERR_INVALID_ARG;
+    if (overlap(ws, wb, X, xb) || overlap(ws, wb, dZ, zb) || overlap(ws, wb, dW, ob) || overlap(ws, wb, offsets, 4 * ((size_t)d->groups + 1))) return POETX_ERR_INVALID_ARG;
     const Held h = held_of(d);
     grouped::Call c = held_call(d, h);
     c.in = ws;
