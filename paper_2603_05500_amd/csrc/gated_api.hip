@@ -185,7 +185,7 @@ int poetx_gated_fwd(const poetx_gated_desc* d, const void* X, int64_t ldx, const
     const Area scratch[] = {{ws, need}};
     if (!apart(scratch, 1, ins, 3) || !apart(scratch, 1, outs, 3)) return POETX_ERR_INVALID_ARG;
   }
-  const gated::Out out{H, G, U, nullptr, ldh, ldgu, 0, gated::act_of(d->activation)};
+  const gated::Out out{H, G, U, nullptr, ldh, G && !mx8 ? ldgu : 0, 0, gated::act_of(d->activation)};      // a stride of nothing chooses no kernel
   products(d, X, ldx, W, offsets, !G ? gated::FWD : mx8 ? gated::HOLD_MX8 : gated::HOLD, out, ws, (hipStream_t)stream);
   return launch_status();
 }
@@ -206,7 +206,7 @@ int poetx_gated_bwd(const poetx_gated_desc* d, const void* dH, int64_t lddh, con
   if (!apart(outs, 3, ins, 4) || !apart(outs, 1, outs + 1, 2) || (rows > 0 && !pair_apart(dG, dU, rows, n, lddgu, es))) return POETX_ERR_INVALID_ARG;
   if (rows == 0) return POETX_OK;
   StageTimer tm(POETX_STAGE_LAYOUT, (hipStream_t)stream);
-  const gated::Out out{H, dG, dU, dH, ldh, lddgu, lddh, gated::act_of(d->activation)};
+  const gated::Out out{H, dG, dU, dH, H ? ldh : 0, lddgu, lddh, gated::act_of(d->activation)};
   gated::rows_launch(d->dtype, mx8 ? gated::MX8 : gated::SAME, gated::In{G, U, ldgu, 1}, offsets, d->groups, rows, d->d_hidden, gated::BWD, out, (hipStream_t)stream);
   return launch_status();
 }
@@ -231,7 +231,7 @@ int poetx_gated_bwd_recompute(const poetx_gated_desc* d, const void* dH, int64_t
     const Area scratch[] = {{ws, need}};
     if (!apart(scratch, 1, ins, 4) || !apart(scratch, 1, outs, 3)) return POETX_ERR_INVALID_ARG;
   }
-  const gated::Out out{H, dG, dU, dH, ldh, lddgu, lddh, gated::act_of(d->activation)};
+  const gated::Out out{H, dG, dU, dH, H ? ldh : 0, lddgu, lddh, gated::act_of(d->activation)};
   products(d, X, ldx, W, offsets, gated::BWD, out, ws, (hipStream_t)stream);
   return launch_status();
 }
