@@ -39,8 +39,14 @@ def parse(line):
     return 1, set(), set(), 0, operands[0] if op.startswith(("s_branch", "s_cbranch")) else None
 
 
+def into_lds(read):
+    """Is a memory instruction that reads these registers a load into LDS?  Only those take M0."""
+    return "m0" in read
+
+
 def too_close(assembly):
-    """Instructions of hand-written assembly that read a scalar register too soon, as (line number, instruction, the one that writes it)."""
+    """Instructions of hand-written assembly that read a scalar register too soon, as (line number, instruction, the one that writes it).  Every load into LDS is written by hand here: one that is
+    not marked as such says that the compiler marks hand-written assembly in another way than this looks for, which is a ValueError."""
     code, labels, by_hand = [], {}, False
     for number, line in enumerate(assembly.splitlines(), 1):
         text = line.strip()
@@ -53,6 +59,8 @@ def too_close(assembly):
         else:
             at = parse(text)
             if at:
+                if at[3] == MEMORY and into_lds(at[2]) and not by_hand:
+                    raise ValueError(f"line {number}, {text}: a load into LDS that is not marked as hand-written")
                 code.append((number, text, by_hand, at))
     found = set()
 
