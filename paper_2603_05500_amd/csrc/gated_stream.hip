@@ -16,24 +16,24 @@ namespace {
 
 using grouped::BF16;
 using grouped::F32;
-using grouped::StreamArgs;
+using grouped::GatedStreamArgs;
 using grouped::StreamTile;
 
 constexpr int kCUs = 256;
 
 template <class C>
-void go(const StreamArgs& a0, hipStream_t st) {
+void go(const GatedStreamArgs& a0, hipStream_t st) {
   auto kern = grouped::grouped_stream_kernel<grouped::FWD, C>;
   static const bool configured = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS_BYTES) == hipSuccess;
   (void)configured;
-  StreamArgs a = a0;
+  GatedStreamArgs a = a0;
   const int cols = C::GATED == HOLD_MX8 ? mx8::units(a.N) * mx8::UNIT : a.N;      // codes past the last column are zeros
   a.tiles_n = ceil_div(cols, C::BN / 2);
   hipLaunchKernelGGL(kern, dim3(kCUs * C::PER_CU), dim3(256), C::LDS_BYTES, st, a);
 }
 
 template <Mode MODE>
-void pick(grouped::Kernel k, const StreamArgs& a, hipStream_t st) {
+void pick(grouped::Kernel k, const GatedStreamArgs& a, hipStream_t st) {
   if (k == grouped::SINGLE_128) go<StreamTile<128, 128, 4, F32, 2, false, MODE>>(a, st);
   else if (k == grouped::SINGLE_64) {
     if constexpr (MODE == HOLD_MX8) go<StreamTile<128, 128, 4, F32, 2, false, MODE>>(a, st);      // a wave's columns have to be whole blocks
@@ -43,7 +43,7 @@ void pick(grouped::Kernel k, const StreamArgs& a, hipStream_t st) {
   else go<StreamTile<128, 128, 8, BF16, 1, false, MODE>>(a, st);
 }
 template <Mode MODE>
-void pick_narrow(grouped::Kernel k, const StreamArgs& a, hipStream_t st) {
+void pick_narrow(grouped::Kernel k, const GatedStreamArgs& a, hipStream_t st) {
   if (k == grouped::SINGLE_128 || k == grouped::SINGLE_64) go<StreamTile<128, 128, 4, F32, 2, false, MODE, true>>(a, st);
   else if (k == grouped::STREAM_256 || k == grouped::STREAM_256x128) go<StreamTile<256, 128, 6, BF16, 1, false, MODE, true>>(a, st);
   else go<StreamTile<128, 128, 8, BF16, 1, false, MODE, true>>(a, st);
@@ -60,7 +60,7 @@ bool stream_supported(int dtype, const Call& c) {
 
 void stream_launch(int dtype, grouped::Kernel k, const Call& c, hipStream_t st) {
   const int es = dtype == POETX_F32 ? 4 : 2;
-  StreamArgs a = {};
+  GatedStreamArgs a = {};
   a.A = (const char*)c.X;
   a.lda = (int)(es * c.ldx);
   a.B = (const char*)c.W;

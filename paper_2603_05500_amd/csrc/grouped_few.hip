@@ -35,14 +35,19 @@ struct FewArgs {
   const int32_t* offsets;
   i64 rows;
   int m, n, groups, units, tiles_n;
-  gated::Out block;         // GATED (n: d_hidden)
+};
+// of a gated block (n: d_hidden)
+struct GatedFewArgs : FewArgs {
+  gated::Out block;
 };
 
 constexpr int NOT_GATED = gated::NONE;
+template <int MODE>
+using FewArgsOf = std::conditional_t<MODE == NOT_GATED, FewArgs, GatedFewArgs>;      // in one struct they cost every launch of a plain product 0.3 us of 7.1
 
 // What a gated block makes of G and U of a tile, `part` being sums of NW waves [16 NT rows][8 RT pairs].  HOLD_MX8: RT = 4, the 32 columns of a block.
 template <int RT, int NT, int NW, int MODE, class T>
-__device__ __forceinline__ void gated_out(const FewArgs& a, const RowTile& t, int rows, int h0, const float (&part)[NW][RT * NT * 256]) {
+__device__ __forceinline__ void gated_out(const GatedFewArgs& a, const RowTile& t, int rows, int h0, const float (&part)[NW][RT * NT * 256]) {
   const gated::Out& o = a.block;
   for (int i = threadIdx.x; i < RT * NT * 128; i += 64 * NW) {
     const int row = i / (8 * RT), col = h0 + i % (8 * RT);
@@ -94,7 +99,7 @@ __device__ __forceinline__ void gated_out(const FewArgs& a, const RowTile& t, in
 }
 
 template <int RT, int NT, int NW, Kind KIND, int U, int MODE>
-__global__ __launch_bounds__(64 * NW) void grouped_few_kernel(FewArgs a, int first) {
+__global__ __launch_bounds__(64 * NW) void grouped_few_kernel(FewArgsOf<MODE> a, int first) {
   __shared__ float part[NW][RT * NT * 256];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -279,7 +284,7 @@ __global__ __launch_bounds__(64 * NW) void grouped_few_kernel(FewArgs a, int fir
 }
 
 template <int RT, int NT, int NW, Kind KIND, int U, int MODE = NOT_GATED>
-void go(FewArgs a, hipStream_t st) {
+void go(FewArgsOf<MODE> a, hipStream_t st) {
   a.tiles_n = MODE == NOT_GATED ? ceil_div(a.n, 16 * RT) : MODE == gated::HOLD_MX8 ? mx8::units(a.n) * 4 : ceil_div(a.n, 8 * RT);      // HOLD_MX8: codes past the last column are zeros
   const i64 total = (a.groups == 1 ? (a.rows + 16 * NT - 1) / (16 * NT) : most_row_tiles(a.rows, a.groups, 16 * NT)) * a.tiles_n;
   launch_in_rows(total, [&](int first, unsigned count) {
@@ -313,7 +318,7 @@ void pick(const FewArgs& a, hipStream_t st) {
 
 // a gated block: of twice as many weight rows
 template <Kind KIND, int MODE>
-void pick_gated(const FewArgs& a, hipStream_t st) {
+void pick_gated(const GatedFewArgs& a, hipStream_t st) {
   const i64 live = a.rows < a.groups ? a.rows : a.groups, mean = (a.rows + live - 1) / live, tiles = small_tiles(a.rows, a.groups, 2 * a.n);
   if constexpr (MODE != gated::HOLD_MX8) {
     if (tiles <= (KIND == SINGLE ? 1024 : 768)) return go<1, 1, 4, KIND, KIND == SINGLE ? 1 : 4, MODE>(a, st);
@@ -378,7 +383,7 @@ namespace gated {
 // `four`: W is a 4-bit buffer
 void few_launch(int dtype, bool four, const Call& c, hipStream_t st) {
   using namespace grouped;
-  FewArgs a{c.X, nullptr, c.W, nullptr, nullptr, c.ldx, 0, c.offsets, c.rows, c.m, c.n, c.groups, (c.m + 127) / 128, 0, c.out};
+  GatedFewArgs a{{c.X, nullptr, c.W, nullptr, nullptr, c.ldx, 0, c.offsets, c.rows, c.m, c.n, c.groups, (c.m + 127) / 128, 0}, c.out};
   auto typed = [&](auto MODE_) {
     constexpr int MODE = decltype(MODE_)::value;
     if (four) {

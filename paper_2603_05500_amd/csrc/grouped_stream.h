@@ -76,8 +76,13 @@ struct StreamArgs {
   int tiles_n;            // column tiles
   int accumulate;
   int splits;             // ranges of the contraction, whose sums go to [split][rows][N] (WEIGHT: [split][group][M][N]) at C; 1: the result does
-  gated::Out block;       // GATED: what is made of a tile; N: d_hidden, tiles_n: of so many columns (HOLD_MX8: rounded up to whole units)
 };
+// GATED: what is made of a tile; N: d_hidden, tiles_n: of so many columns (HOLD_MX8: rounded up to whole units)
+struct GatedStreamArgs : StreamArgs {
+  gated::Out block;
+};
+template <class C>
+using StreamArgsOf = std::conditional_t<C::GATED == NOT_GATED, StreamArgs, GatedStreamArgs>;
 
 // 16 (4) bytes per lane from base + voff straight into LDS at lds + 16 (4) * lane; zeros from the descriptor's end on.  Between M0's write and its use there has to be
 // an instruction, and more where a word of the descriptor has just come back from a vector register's lane, which the build looks for (load_waits.py).
@@ -135,7 +140,7 @@ __device__ __forceinline__ void mfma_fp32(floatx4& c, uint32_t a, uint32_t b) { 
 // ---- what a gated block makes of a wave's piece of a tile, rows r0 on of a group that ends with r1, columns j0 on --------------
 // Register a, c of a lane: row 16 a + (lane & 15), columns 4 (lane >> 4) .. + 3 of piece c / 2, of G where c is even and of U where it is odd.
 template <class C>
-__device__ __forceinline__ void gated_tile(const StreamArgs& g, floatx4 (&acc)[C::TM][C::TN], int r0, int r1, int j0, int wave, int lane, char* stg) {
+__device__ __forceinline__ void gated_tile(const GatedStreamArgs& g, floatx4 (&acc)[C::TM][C::TN], int r0, int r1, int j0, int wave, int lane, char* stg) {
   constexpr gated::Mode MODE = (gated::Mode)C::GATED;
   constexpr bool FP32 = C::ELEM == F32, PAIR = MODE == gated::HOLD || MODE == gated::BWD;      // PAIR: G and U, or dG and dU, as matrices
   constexpr int P = C::TN / 2, ES = FP32 ? 4 : 2, AT_ONCE = P < 2 ? P : 2;      // pieces of 16 columns
@@ -373,7 +378,7 @@ __device__ __forceinline__ void in_turn(std::integer_sequence<int, I...>, const 
 
 // GATED: columns of B come in pieces of 16, gate and up in turn, the tile's columns of H being half as many: a lane then holds G and U of the same four elements of a row.
 template <Dir DIR, class C>
-__global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgs g) {
+__global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgsOf<C> g) {
   constexpr bool GATED = C::GATED != NOT_GATED;
   static_assert(!GATED || (DIR == FWD && C::ELEM != CODES), "a gated block's products");
   constexpr bool FP4 = C::FP4, FP32 = C::ELEM == F32, A_K = DIR != WEIGHT, B_K = DIR == FWD;

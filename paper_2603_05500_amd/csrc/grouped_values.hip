@@ -27,12 +27,17 @@ struct ValuesArgs {
   int m, n, groups, units, tiles_n;
   int splits;      // PARTS: ranges of the contraction, whose fp32 sums go to parts, [split][rows][n]
   float* parts;
-  gated::Out block;      // MODE: of a gated block (n: d_hidden)
 };
+// MODE: of a gated block (n: d_hidden)
+struct GatedValuesArgs : ValuesArgs {
+  gated::Out block;
+};
+template <int MODE>
+using ValuesArgsOf = std::conditional_t<MODE == NOT_GATED, ValuesArgs, GatedValuesArgs>;
 
 // MODE: a gated block (14187 rows over 3 groups of 2 x 544 x 2336 107 us, 134 with the weight written out first), a tile's first half of columns being gate's and its second half up's of as many columns of H.
 template <int BM, int BN, int NS, bool PARTS, int MODE>
-__global__ __launch_bounds__(256) void grouped_values_kernel(ValuesArgs g, int first) {
+__global__ __launch_bounds__(256) void grouped_values_kernel(ValuesArgsOf<MODE> g, int first) {
   constexpr int A_BYTES = BM * 256, B_BYTES = BN * 64, STAGE_BYTES = A_BYTES + B_BYTES + BN * 4;
   constexpr int IPWA = BM / 16, IPWB = BN / 64, LPU = IPWA + IPWB + 1, TM = BM / 32, TN = BN / 32, MF = TM * TN;
   constexpr bool GATED = MODE != NOT_GATED;
@@ -232,7 +237,7 @@ __global__ __launch_bounds__(256) void grouped_values_kernel(ValuesArgs g, int f
 }
 
 template <int BM, int BN, int NS, bool PARTS = false, int MODE = NOT_GATED>
-void go(ValuesArgs a, hipStream_t st) {
+void go(ValuesArgsOf<MODE> a, hipStream_t st) {
   constexpr int BYTES = NS * (BM * 256 + BN * 68);
   auto kern = grouped_values_kernel<BM, BN, NS, PARTS, MODE>;
   static const bool configured = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, BYTES) == hipSuccess;
@@ -300,7 +305,7 @@ bool values_launch(const poetx_grouped_desc* d, const void* X, i64 ldx, const vo
   if (!p.better) return false;
   StageTimer tm(POETX_STAGE_DENSE, st);
   const mx4::View w = mx4::view(Wq, (i64)d->groups * d->d_out, d->d_in);
-  const ValuesArgs a{(const uint16_t*)X, ldx, w.codes, w.scales, (uint16_t*)Z, ldz, offsets, d->rows, d->d_in, d->d_out, d->groups, mx4::units(d->d_in), 0, p.ranges, (float*)ws, {}};
+  const ValuesArgs a{(const uint16_t*)X, ldx, w.codes, w.scales, (uint16_t*)Z, ldz, offsets, d->rows, d->d_in, d->d_out, d->groups, mx4::units(d->d_in), 0, p.ranges, (float*)ws};
   if (p.ranges > 1) {
     parts_launch(p.tile, a, st);
     add_parts(POETX_BF16, ws, p.ranges, d->d_out, c, st);
@@ -343,7 +348,7 @@ bool values_launch(const Call& c, bool few, void* sums, size_t sums_bytes, size_
   if (!p.better) return false;
   StageTimer tm(POETX_STAGE_DENSE, st);
   const mx4::View w = mx4::view(c.W, 2 * (i64)c.groups * c.n, c.m);
-  grouped::ValuesArgs a{(const uint16_t*)c.X, c.ldx, w.codes, w.scales, nullptr, 0, c.offsets, c.rows, c.m, c.n, c.groups, mx4::units(c.m), 0, p.ranges, (float*)sums, c.out};
+  grouped::GatedValuesArgs a{{(const uint16_t*)c.X, c.ldx, w.codes, w.scales, nullptr, 0, c.offsets, c.rows, c.m, c.n, c.groups, mx4::units(c.m), 0, p.ranges, (float*)sums}, c.out};
   if (p.ranges > 1) {
     a.n = 2 * c.n;
     grouped::parts_launch(p.tile, a, st);
