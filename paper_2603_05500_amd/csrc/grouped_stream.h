@@ -442,10 +442,13 @@ __global__ __launch_bounds__(256) void grouped_stream_kernel(StreamArgsOf<C> g) 
   // The last round has tiles for some workgroups only.  After few rounds they are those that come first, which the eight XCDs and their CUs have alike, each XCD with a run of tiles as before: in the
   // order of the other rounds they are all of the first XCDs' (bf16, 3000 rows of 4096 x 4096, 192 tiles, 107 us so, 91 as it is; fp32, 1000 rows of the gated block 512 -> 1376,
   // 49 and 39).  Over more rounds that order is kept, in which an XCD goes on with the columns it is at (16384 rows over 8 groups of 4096 x 8192, 9 rounds, 978 us so, 994 the
-  // other way; gated block, 8190 rows over 57 groups, 4 rounds, 203 and 208), and for WEIGHT, whose times were the same.
+  // other way; gated block, 8190 rows over 57 groups, 4 rounds, 203 and 208), and for WEIGHT, whose times were the same.  Few are two rounds, of bf16 products no more (input gradient, 5720 rows over 8
+  // groups of 1312 x 5024, 2.1 rounds, 102 us in the old order, 109 so), of fp32 ones and gated blocks three (fp32 gated block, 1282 rows, 1056 -> 1856, 2.4 rounds, 111 and 92; bf16, 5654 rows,
+  // 256 -> 3584, 2.5 rounds, 57.0 and 55.5).
   const int rounds = T / G, rest = T % G;
   auto turn = [&](int ti) { return DIR == WEIGHT && (ti & 1) ? G - 1 - wq : wq; };
-  int last = DIR == WEIGHT || T >= 3 * G ? turn(rounds) : (int)blockIdx.x < rest ? xcd_run(blockIdx.x, rest) : rest;
+  constexpr int FEW = FP32 || GATED ? 3 : 2;
+  int last = DIR == WEIGHT || T >= FEW * G ? turn(rounds) : (int)blockIdx.x < rest ? xcd_run(blockIdx.x, rest) : rest;
   const int n_my = rounds + (last < rest);
   if (n_my == 0) return;
   if (DIR != WEIGHT) asm volatile("" : "+v"(last));      // scalar registers are short
